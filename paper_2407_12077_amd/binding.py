@@ -1,6 +1,7 @@
 """Thin binding of ``libwkv6.so``: argument marshalling only.
 
-Every entry point has the name and argument order of ``include/wkv6.h``.  Tensors are
+Every entry point has the name and argument order of ``include/wkv6.h``, ``include/wkv6_head_decay.h`` and
+``include/wkv6_layernorm.h``.  Tensors are
 PyTorch-ROCm tensors used purely as device memory (``data_ptr``) and the current HIP
 stream; nothing is computed here.  Calls that enqueue work go through the extension ``_call``
 (csrc/binding_call.cpp), the others through ctypes.  There is no fallback: if the library or the
@@ -27,6 +28,11 @@ EXPORTS = ("wkv6_prefill_bf16", "wkv6_prefill_bf16_f32out", "wkv6_prefill_bf16_s
            "wkv6_decode_bf16", "wkv6_finch_c2_decode_bf16", "wkv6_append_bf16",
            "wkv6_finch_c2_append_bf16", "wkv6_key_compress_bf16", "wkv6_arena_layout", "wkv6_status_string",
            "wkv6_version")
+
+# of include/wkv6_head_decay.h and include/wkv6_layernorm.h
+OPERATOR_EXPORTS = ("wkv6_head_decay_prefill", "wkv6_head_decay_workspace_bytes", "wkv6_head_decay_decode",
+                    "wkv6_head_decay_backward", "wkv6_head_decay_backward_workspace_bytes", "wkv6_layernorm_forward",
+                    "wkv6_layernorm_backward", "wkv6_layernorm_backward_workspace_bytes")
 
 _lib = None
 _call = None               # the extension, bound to _lib
@@ -91,6 +97,22 @@ def load():
         lib.wkv6_split_workspace_bytes.argtypes = [i, i, i, i, i]
         lib.wkv6_split_segments.restype = i
         lib.wkv6_split_segments.argtypes = [i, i, i, i]
+        lib.wkv6_head_decay_prefill.restype = i
+        lib.wkv6_head_decay_prefill.argtypes = [i, i, i, i, ll, vp, vp, vp, ll, vp, ll, vp, vp, vp, vp, i, i, vp, ll, vp]
+        lib.wkv6_head_decay_decode.restype = i
+        lib.wkv6_head_decay_decode.argtypes = [i, i, i, vp, vp, vp, ll, vp, ll, vp, vp, vp, i, i, vp]
+        lib.wkv6_head_decay_backward.restype = i
+        lib.wkv6_head_decay_backward.argtypes = [i, i, i, i, ll, vp, vp, vp, ll, vp, ll] + [vp] * 9 + [i, vp, ll, vp]
+        lib.wkv6_head_decay_workspace_bytes.restype = ll
+        lib.wkv6_head_decay_workspace_bytes.argtypes = [i, i, i, i]
+        lib.wkv6_head_decay_backward_workspace_bytes.restype = ll
+        lib.wkv6_head_decay_backward_workspace_bytes.argtypes = [i, i, i, i, ll]
+        lib.wkv6_layernorm_forward.restype = i
+        lib.wkv6_layernorm_forward.argtypes = [ll, i, vp, vp, vp, ctypes.c_float, vp, vp, i, i, vp]
+        lib.wkv6_layernorm_backward.restype = i
+        lib.wkv6_layernorm_backward.argtypes = [ll, i] + [vp] * 7 + [i, i, vp, ll, vp]
+        lib.wkv6_layernorm_backward_workspace_bytes.restype = ll
+        lib.wkv6_layernorm_backward_workspace_bytes.argtypes = [ll, i]
         lib.wkv6_arena_layout.restype = ctypes.c_longlong
         lib.wkv6_arena_layout.argtypes = [i, ctypes.POINTER(ctypes.c_longlong), ctypes.POINTER(ctypes.c_longlong)]
         lib.wkv6_status_string.restype = ctypes.c_char_p
@@ -253,6 +275,46 @@ def wkv6_finch_c2_decode_bf16(B, H, N, r, kbar, v, x, uprime, state, out, stream
 
 def wkv6_key_compress_bf16(M, D, x, w_kd, c, out_dtype, stream=None):
     (_call or _bound()).wkv6_key_compress_bf16(M, D, x, w_kd, c, int(out_dtype), stream)
+
+
+def wkv6_head_decay_prefill(B, T, H, N, rows, r, k, v, token_stride, g, g_stride, offsets, state_in, out, state_out, dtype,
+                            out_dtype, workspace, workspace_bytes, stream=None):
+    (_call or _bound()).wkv6_head_decay_prefill(B, T, H, N, rows, r, k, v, token_stride, g, g_stride, offsets, state_in, out,
+                                                state_out, int(dtype), int(out_dtype), workspace, workspace_bytes, stream)
+
+
+def wkv6_head_decay_workspace_bytes(B, T, H, N):
+    return load().wkv6_head_decay_workspace_bytes(B, T, H, N)
+
+
+def wkv6_head_decay_decode(B, H, N, r, k, v, token_stride, g, g_stride, state_in, out, state_out, dtype, out_dtype, stream=None):
+    (_call or _bound()).wkv6_head_decay_decode(B, H, N, r, k, v, token_stride, g, g_stride, state_in, out, state_out, int(dtype),
+                                               int(out_dtype), stream)
+
+
+def wkv6_head_decay_backward(B, T, H, N, rows, r, k, v, token_stride, g, g_stride, offsets, state_in, dout, dstate_out, dr, dk,
+                             dv, dg, dstate_in, dtype, workspace, workspace_bytes, stream=None):
+    (_call or _bound()).wkv6_head_decay_backward(B, T, H, N, rows, r, k, v, token_stride, g, g_stride, offsets, state_in, dout,
+                                                 dstate_out, dr, dk, dv, dg, dstate_in, int(dtype), workspace, workspace_bytes,
+                                                 stream)
+
+
+def wkv6_head_decay_backward_workspace_bytes(B, T, H, N, rows):
+    return load().wkv6_head_decay_backward_workspace_bytes(B, T, H, N, rows)
+
+
+def wkv6_layernorm_forward(M, D, x, gamma, beta, eps, y, mean_rstd, dtype, out_dtype, stream=None):
+    (_call or _bound()).wkv6_layernorm_forward(M, D, x, gamma, beta, eps, y, mean_rstd, int(dtype), int(out_dtype), stream)
+
+
+def wkv6_layernorm_backward(M, D, x, mean_rstd, gamma, dy, dx, dgamma, dbeta, dtype, out_dtype, workspace, workspace_bytes,
+                            stream=None):
+    (_call or _bound()).wkv6_layernorm_backward(M, D, x, mean_rstd, gamma, dy, dx, dgamma, dbeta, int(dtype), int(out_dtype),
+                                                workspace, workspace_bytes, stream)
+
+
+def wkv6_layernorm_backward_workspace_bytes(M, D):
+    return load().wkv6_layernorm_backward_workspace_bytes(M, D)
 
 
 def wkv6_version():

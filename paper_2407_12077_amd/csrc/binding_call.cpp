@@ -18,6 +18,8 @@
 #include <utility>
 
 #include "wkv6.h"
+#include "wkv6_head_decay.h"
+#include "wkv6_layernorm.h"
 
 namespace {
 
@@ -143,7 +145,9 @@ PyObject* invoke(int (*fn)(A...), const char* name, PyObject* const* args, Py_ss
     X(wkv6_finch_c2_prefill_bf16_f32out) X(wkv6_finch_c2_prefill_bf16_strided) X(wkv6_finch_c2_prefill_bf16_split)            \
     X(wkv6_finch_c2_prefill_bf16_moments) X(wkv6_layernorm_finalize) X(wkv6_layernorm_apply_bf16)                             \
     X(wkv6_decay_lora_input_bf16) X(wkv6_finch_c2_prefill_lora_bf16) X(wkv6_prefill_lora_bf16) X(wkv6_decode_bf16)            \
-    X(wkv6_finch_c2_decode_bf16) X(wkv6_append_bf16) X(wkv6_finch_c2_append_bf16) X(wkv6_key_compress_bf16)
+    X(wkv6_finch_c2_decode_bf16) X(wkv6_append_bf16) X(wkv6_finch_c2_append_bf16) X(wkv6_key_compress_bf16)                   \
+    X(wkv6_head_decay_prefill) X(wkv6_head_decay_decode) X(wkv6_head_decay_backward)                                          \
+    X(wkv6_layernorm_forward) X(wkv6_layernorm_backward)
 
 #define X(name)                                                                                    \
     decltype(&::name) fn_##name = nullptr;                                                         \

@@ -1,0 +1,760 @@
+// The head-decay time mix over whole sequences (one decay w_t = exp(g_t) per head and token) and its gradients for gfx950:
+//
+//     S_t = w_t S_{t-1} + k_t^T v_t        o_t = q_t S_t
+//
+// in chunks of kC tokens.  With A_t the decays from the chunk's first token to t and S_0 the state in front of the chunk
+//
+//     o_t = A_t q_t S_0 + sum_{i <= t} P_ti v_i        P_ti = (q_t . k_i) exp(g_{i+1} + .. + g_t)
+//     S   = A_last S_0 + sum_i k_i^T (exp(g_{i+1} + .. + g_last) v_i)
+//
+// four products on the matrix cores.  Decays are only ever exponentials of sums of g inside a block of 16 tokens and products of
+// such, never a quotient, so nothing overflows and nothing but a difference inside a block is subtracted.
+//
+// The gradients are products of the same form (o, S as above, do the gradient of o):
+//     dr = mix(q = do, k = v, v = k; S_0 transposed)     dv = reversed mix(q = k, k = r, v = do)     dk = reversed mix(q = v, k = do, v = r)
+// and that of g_t is the sum of r.dr - k.dk from t to the end of any later block plus <dS, S> there: see decay_gradient_kernel.
+//
+// A workgroup of four waves takes one segment of one (sequence, head) and walks its chunks.  Rows go straight from memory into LDS,
+// kStages - 1 chunks ahead; a wave owns 16 of the 64 value columns: the state's [64][16] columns stay in its registers for the whole
+// walk, and the transposed products leave every operand where the next one needs it:
+//     P^T (keys x queries)  from rows of k and q as they lie; its accumulators are, lane by lane, the operand of the next product.  The
+//                           waves share the blocks on and below the diagonal, one chunk ahead of their use
+//     o^T (values x queries) = v^T P^T + S^T q^T: v through transposing reads, the state straight from the accumulators
+//     S (keys x values)      = k^T (decayed v)
+// One barrier a chunk.
+//
+// bf16 rows: products of rows are exact in fp32; the computed operands (P, S, decayed v) are kept as a sum of two bf16, 16 significant
+// bits and the whole exponent range, each product twice.  So nothing has to stay inside the range of fp16, and the fp32 results
+// are good to about 2^-17 of their size.  fp32 rows: fp32 matrix instructions throughout.
+#include "head_decay.h"
+#include "wkv6_lds_loads.h"
+#include "wkv6_math.h"
+
+#include <type_traits>
+
+namespace wkv6 {
+namespace {
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned uint2v __attribute__((ext_vector_type(2)));
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+
+struct Bf16 {};
+
+// What differs between the types of rows.  Raw: four consecutive contraction indices of an operand as they lie in a tile.  Fine: four
+// computed ones.  A tile is kC rows of kHeadSize values in places of 16 bytes, which a row's number permutes so that the reads below
+// take every bank equally often.
+template <typename T>
+struct Elem;
+
+template <>
+struct Elem<Bf16> {
+    static constexpr int kSize = 2, kRow = kHeadSize * kSize, kPlaces = kRow / 16;
+    typedef short4v Raw;
+    struct Fine {
+        short4v hi, lo;
+    };
+    __device__ static __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
+    __device__ static __forceinline__ int at(int row, int place) { return row * kRow + 16 * (place ^ swizzle(row)); }
+    // lanes are rows, contraction indices columns 16 q + 4 g4 ..
+    __device__ static __forceinline__ Raw row_piece(const char* tile, int row, int q, int g4) {
+        return *reinterpret_cast<const Raw*>(tile + at(row, 2 * q + (g4 >> 1)) + 8 * (g4 & 1));
+    }
+    // lanes are columns c0 + l16, contraction indices rows r0 + 4 g4 ..: a transposing read, in which lane i of sixteen passes the
+    // address of four columns of row i / 4 and gets column i of the four rows
+    __device__ static __forceinline__ Raw column_piece(const char* tile, int r0, int c0, int l16, int g4) {
+        typedef short4v __attribute__((address_space(3))) * lds_ptr;
+        const int row = r0 + 4 * g4 + (l16 >> 2), col = c0 + 4 * (l16 & 3);
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + at(row, col >> 3) + 8 * (col >> 2 & 1)));
+    }
+    __device__ static __forceinline__ float4v floats(Raw r) {
+        const uint2v u = __builtin_bit_cast(uint2v, r);
+        return float4v{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+    }
+    // the sum of two bf16 nearest to x: 2^-17 of x, where one would be 2^-9
+    __device__ static __forceinline__ Fine fine(float4v x) {
+        Fine f;
+        f.hi = __builtin_bit_cast(short4v, __builtin_convertvector(x, bf16x4));
+        f.lo = __builtin_bit_cast(short4v, __builtin_convertvector(x - floats(f.hi), bf16x4));
+        return f;
+    }
+    __device__ static __forceinline__ bf16x8 both(Raw a, Raw b) {
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // acc += A B over 32 contraction indices (two pieces) or 16
+    __device__ static __forceinline__ float4v mul(Raw a0, Raw a1, const Fine& b0, const Fine& b1, float4v acc) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0.lo, b1.lo), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0.hi, b1.hi), acc, 0, 0, 0);
+    }
+    __device__ static __forceinline__ float4v mul(const Fine& a0, const Fine& a1, Raw b0, Raw b1, float4v acc) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0.lo, a1.lo), both(b0, b1), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0.hi, a1.hi), both(b0, b1), acc, 0, 0, 0);
+    }
+    __device__ static __forceinline__ float4v mul(Raw a, const Fine& b, float4v acc) {
+        const short4v none = {0, 0, 0, 0};
+        return mul(a, none, b, Fine{none, none}, acc);
+    }
+    // rows a of one tile times rows b of another over all columns
+    __device__ static __forceinline__ float4v row_products(const char* ta, int ra, const char* tb, int rb, int g4) {
+        float4v acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(ta + at(ra, 4 * m + g4)),
+                                                          *reinterpret_cast<const bf16x8*>(tb + at(rb, 4 * m + g4)), acc, 0, 0, 0);
+        return acc;
+    }
+};
+
+template <>
+struct Elem<float> {
+    static constexpr int kSize = 4, kRow = kHeadSize * kSize, kPlaces = kRow / 16;
+    typedef float4v Raw;
+    typedef float4v Fine;
+    __device__ static __forceinline__ int swizzle(int row) { return row & 15; }
+    __device__ static __forceinline__ int at(int row, int place) { return row * kRow + 16 * (place ^ swizzle(row)); }
+    __device__ static __forceinline__ Raw row_piece(const char* tile, int row, int q, int g4) {
+        return *reinterpret_cast<const Raw*>(tile + at(row, 4 * q + g4));
+    }
+    __device__ static __forceinline__ Raw column_piece(const char* tile, int r0, int c0, int l16, int g4) {
+        Raw r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = r0 + 4 * g4 + e, col = c0 + l16;
+            r[e] = *reinterpret_cast<const float*>(tile + at(row, col >> 2) + 4 * (col & 3));
+        }
+        return r;
+    }
+    __device__ static __forceinline__ float4v floats(Raw r) { return r; }
+    __device__ static __forceinline__ Fine fine(float4v x) { return x; }
+    __device__ static __forceinline__ float4v mul(float4v a, float4v b, float4v acc) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc, 0, 0, 0);
+        return acc;
+    }
+    __device__ static __forceinline__ float4v mul(float4v a0, float4v a1, float4v b0, float4v b1, float4v acc) {
+        return mul(a1, b1, mul(a0, b0, acc));
+    }
+    __device__ static __forceinline__ float4v row_products(const char* ta, int ra, const char* tb, int rb, int g4) {
+        float4v acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc = mul(row_piece(ta, ra, q, g4), row_piece(tb, rb, q, g4), acc);
+        return acc;
+    }
+};
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kStages = 4;             // places for a chunk's tiles: the chunk at hand, the next, and two on their way
+constexpr int kDecayPlaces = 8;        // places for a chunk's g: asked for a chunk earlier than the rows
+constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
+
+// A chunk's decays by token, in LDS.  In logarithms to base 2 (pre) or as factors (the others)
+template <int kC>
+struct Decays {
+    float pre[kC];                     // sum of g from the block's first token to this
+    float pre_key[kC];                 // the same of tokens that are there, +inf of others
+    float in_block[kC];                // exp2(pre)
+    float to_block[kC];                // from behind this token to the block's end; nought for tokens that are not there
+    float in_chunk[kC];                // from the chunk's first token to this
+    float to_chunk[kC];                // from behind this token to the chunk's end; nought for tokens that are not there
+    float block[kC / 16];              // of whole blocks
+    float whole[4];                    // of the whole chunk (one value)
+};
+
+template <typename T, int kC, bool kStates, bool kSums>
+struct Layout {
+    static constexpr int kTile = kC * Elem<T>::kRow;
+    static constexpr int kTiles = kStates ? 2 : 3;               // k, v, q
+    static constexpr int kStage = kTile * kTiles;
+    static constexpr int kBlocks = kC / 16, kPairs = kBlocks * (kBlocks + 1) / 2;
+    static constexpr int kScores = kStates ? 0 : kPairs * 1024;  // four Fine values a lane and pair of blocks
+    static constexpr int kOffG = kStages * kStage;
+    static constexpr int kOffDecays = kOffG + kDecayPlaces * 256;
+    static constexpr int kOffScores = kOffDecays + 4 * static_cast<int>(sizeof(Decays<kC>));
+    static constexpr int kOffSums = kOffScores + 2 * kScores;    // [chunk parity][token][wave][g4]
+    static constexpr int kLds = kOffSums + (kSums ? 2 * kC * 64 : 0);
+    static constexpr int kLoads = kTile / 1024 / kWaves;         // of a wave, tile and chunk
+    static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
+};
+
+struct Span {                          // a workgroup's tokens
+    int b, h, len;                     // sequence, head, the sequence's tokens
+    long long first;                   // its first row
+    int seg, segs;                     // segment, and how many the sequence has
+    int begin, end;                    // the segment's tokens
+};
+
+// Offsets are taken as they are as far as they lie inside the rows: nothing outside the tensors is touched, whatever they hold.
+__device__ __forceinline__ Span span_of(const MixArgs& a, int unit, int seg) {
+    Span s;
+    s.b = unit / a.H;
+    s.h = unit - s.b * a.H;
+    if (a.offsets) {
+        long long lo = a.offsets[s.b], hi = a.offsets[s.b + 1];
+        lo = lo < 0 ? 0 : lo > a.rows ? a.rows : lo;
+        hi = hi < lo ? lo : hi > a.rows ? a.rows : hi;
+        s.first = lo;
+        s.len = static_cast<int>(hi - lo > a.T ? a.T : hi - lo);
+    } else {
+        s.first = static_cast<long long>(s.b) * a.T;
+        s.len = a.T;
+    }
+    s.seg = seg;
+    s.segs = s.len > 0 ? (s.len + a.seg_len - 1) / a.seg_len : 1;
+    s.begin = seg * a.seg_len;
+    s.end = s.begin + a.seg_len < s.len ? s.begin + a.seg_len : s.len;
+    return s;
+}
+
+// exp of a log-decay from memory
+__device__ __forceinline__ float decay_factor(float g) {
+    g = g < kLowest ? kLowest : g;                              // (NaN stays)
+    return __builtin_amdgcn_exp2f(g * kLog2e);
+}
+
+// Sum over the lanes of a row of sixteen up to this one
+__device__ __forceinline__ float prefix16(float v) {
+    auto shifted = [](float x, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v += shifted(v, std::integral_constant<int, 0x111>{});     // row_shr
+    v += shifted(v, std::integral_constant<int, 0x112>{});
+    v += shifted(v, std::integral_constant<int, 0x114>{});
+    v += shifted(v, std::integral_constant<int, 0x118>{});
+    return v;
+}
+
+template <typename T, typename Out, int kC, bool kStates, bool kSums>
+struct Walk {
+    using E = Elem<T>;
+    using L = Layout<T, kC, kStates, kSums>;
+    static constexpr int kBlocks = L::kBlocks;
+
+    const MixArgs& a;
+    const Sweep& w;
+    const Span s;
+    char* const lds;
+    const int lane, wave, l16, g4;
+    const int first_chunk, chunks;                              // of the segment
+    float4v state[4];                                           // S[16 i + 4 g4 + e][16 wave + l16]
+    float total = 1.f;                                          // kStates: decay of all chunks so far
+
+    // token of the chunk's first place, by the chunk's number on the walk
+    __device__ __forceinline__ int chunk_token(int n) const { return (first_chunk + (w.reverse ? chunks - 1 - n : n)) * kC; }
+
+    __device__ __forceinline__ void ask_tile(const char* base, long long row_bytes, int tokens, int token, int to) const {
+        // rows behind the sequence's last token are that token's again: their factors are nought
+        const long long first = s.first + token;
+        const int bytes = static_cast<int>((tokens - 1) * row_bytes) + E::kRow;
+        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(base) + first * row_bytes + static_cast<long long>(s.h) * E::kRow, 0, bytes, 0x00020000);
+        typedef __attribute__((address_space(3))) char* lds_ptr;
+        constexpr int kRowsALoad = 1024 / E::kRow;
+#pragma unroll
+        for (int i = 0; i < L::kLoads; ++i) {
+            const int r = (wave * L::kLoads + i) * kRowsALoad + lane / E::kPlaces;
+            int t = w.reverse ? kC - 1 - r : r;
+            t = t < tokens ? t : tokens - 1;
+            const int off = t * static_cast<int>(row_bytes) + 16 * ((lane % E::kPlaces) ^ E::swizzle(r));
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(lds + to + (wave * L::kLoads + i) * 1024), 16, off, 0, 0, 0);
+        }
+    }
+    // a chunk's rows, always the same number of loads: past the segment's last chunk it is that one again
+    __device__ __forceinline__ void ask_rows(int n) const {
+        const int to = (n & (kStages - 1)) * L::kStage;
+        const int token = chunk_token(n < chunks ? n : chunks - 1);
+        const int left = s.len - token, tokens = left < kC ? left : kC;
+        ask_tile(w.k, w.k_row, tokens, token, to);
+        ask_tile(w.v, w.v_row, tokens, token, to + L::kTile);
+        if constexpr (!kStates) ask_tile(w.q, w.q_row, tokens, token, to + 2 * L::kTile);
+    }
+    // and its g by place (each wave's sixteen lanes of it, so that all waves have asked for as many loads).  In reverse a token's is that of
+    // the token behind it; places without one are cleared where they are read
+    __device__ __forceinline__ void ask_decays(int n) const {
+        const int token = chunk_token(n < chunks ? n : chunks - 1);
+        typedef __attribute__((address_space(3))) char* lds_ptr;
+        int t = token + (w.reverse ? kC - lane : lane);
+        t = t < 0 ? 0 : t < s.len ? t : s.len - 1;
+        const float* from = a.g + (s.first + t) * a.g_row + s.h;
+        const bool mine = (lane >> 4) == wave;
+        if (mine)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                             (lds_ptr)(lds + L::kOffG + (n & (kDecayPlaces - 1)) * 256), 4, 0, 0);
+    }
+    static constexpr int kAsked = L::kLoads * L::kTiles + 1;    // loads of a wave and chunk
+
+    __device__ __forceinline__ Decays<kC>& decays(int n) const {
+        return *reinterpret_cast<Decays<kC>*>(lds + L::kOffDecays + (n & 3) * static_cast<int>(sizeof(Decays<kC>)));
+    }
+
+    // the chunk's decays, by one wave, a lane a token
+    __device__ __forceinline__ void form_decays(int n) const {
+        Decays<kC>& d = decays(n);
+        const int token = chunk_token(n);
+        const int at = lane < kC ? lane : 0;
+        const int t = token + (w.reverse ? kC - 1 - at : at);
+        float g = *reinterpret_cast<const float*>(lds + L::kOffG + (n & (kDecayPlaces - 1)) * 256 + 4 * at);
+        const bool there = t < s.len;
+        const bool has = w.reverse ? t + 1 < s.len : there;
+        g = g < kLowest ? kLowest : g;                          // (NaN stays)
+        g = has ? g * kLog2e : 0.f;
+        const float pre = prefix16(g);
+        const float block = __shfl(pre, lane | 15);             // the block's sum
+        // behind this token: from the other end, so that nothing is subtracted
+        float behind = __shfl(g, (lane & 48) | (15 - (lane & 15)));
+        behind = prefix16(behind);
+        behind = __shfl(behind, (lane & 48) | ((14 - (lane & 15)) & 15));
+        behind = (lane & 15) == 15 ? 0.f : behind;
+        float before = 0.f, after = 0.f, all = 0.f;             // sums over the blocks in front of and behind this one
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            const float sum = __shfl(block, 16 * i);
+            before += i < (lane >> 4) ? sum : 0.f;
+            after += i > (lane >> 4) ? sum : 0.f;
+            all += sum;
+        }
+        if (lane < kC) {
+            d.pre[lane] = pre;
+            d.pre_key[lane] = there ? pre : __builtin_inff();
+            d.in_block[lane] = __builtin_amdgcn_exp2f(pre);
+            d.to_block[lane] = there ? __builtin_amdgcn_exp2f(behind) : 0.f;
+            d.in_chunk[lane] = __builtin_amdgcn_exp2f(before + pre);
+            d.to_chunk[lane] = there ? __builtin_amdgcn_exp2f(behind + after) : 0.f;
+            if ((lane & 15) == 0) d.block[lane >> 4] = __builtin_amdgcn_exp2f(block);
+            if (lane == 0) d.whole[0] = __builtin_amdgcn_exp2f(all);
+        }
+    }
+
+    // P^T of the wave's share of the chunk's pairs of blocks
+    __device__ __forceinline__ void form_scores(int n) const {
+        const char* tile = lds + (n & (kStages - 1)) * L::kStage;
+        const Decays<kC>& d = decays(n);
+        char* to = lds + L::kOffScores + (n & 1) * L::kScores;
+#pragma unroll
+        for (int x = 0; x * kWaves < L::kPairs; ++x) {
+            const int p = x * kWaves + wave;
+            if (p >= L::kPairs) break;
+            const int qb = static_cast<int>(0x3333222110ull >> 4 * p & 15), kb = static_cast<int>(0x3210210100ull >> 4 * p & 15);
+            const int query = 16 * qb + l16, key = 16 * kb + 4 * g4;
+            float4v sc = E::row_products(tile, 16 * kb + l16, tile + 2 * L::kTile, query, g4);
+            if (qb == kb) {
+                const float pre = d.pre[query];
+                const float4v pk = *reinterpret_cast<const float4v*>(&d.pre_key[key]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[e] = key + e <= query ? sc[e] * __builtin_amdgcn_exp2f(pre - pk[e]) : 0.f;
+            } else {
+                float f = d.in_block[query];
+                for (int i = kb + 1; i < qb; ++i) f *= d.block[i];
+                const float4v tb = *reinterpret_cast<const float4v*>(&d.to_block[key]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[e] = sc[e] * (tb[e] * f);
+            }
+            *reinterpret_cast<typename E::Fine*>(to + p * 1024 + lane * 16) = E::fine(sc);
+        }
+    }
+
+    // read-outs of the chunk and the state behind it
+    __device__ __forceinline__ void advance(int n, float4v* out) {
+        const char* tile = lds + (n & (kStages - 1)) * L::kStage;
+        const Decays<kC>& d = decays(n);
+        typename E::Raw v[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) v[b] = E::column_piece(tile + L::kTile, 16 * b, 16 * wave, l16, g4);
+        if constexpr (!kStates) {
+            typename E::Fine st[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st[i] = E::fine(state[i]);
+            const char* q = tile + 2 * L::kTile;
+            const char* sc = lds + L::kOffScores + (n & 1) * L::kScores + lane * 16;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                const int query = 16 * b + l16;
+                float4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+                    o = E::mul(st[2 * m], st[2 * m + 1], E::row_piece(q, query, 2 * m, g4), E::row_piece(q, query, 2 * m + 1, g4), o);
+                o *= d.in_chunk[query];
+                const int p0 = b * (b + 1) / 2;
+#pragma unroll
+                for (int i = 0; i < b; i += 2)
+                    o = E::mul(v[i], v[i + 1 < kBlocks ? i + 1 : i], *reinterpret_cast<const typename E::Fine*>(sc + (p0 + i) * 1024),
+                               *reinterpret_cast<const typename E::Fine*>(sc + (p0 + i + 1) * 1024), o);
+                if (b % 2 == 0) o = E::mul(v[b], *reinterpret_cast<const typename E::Fine*>(sc + (p0 + b) * 1024), o);
+                out[b] = o;
+            }
+        }
+        typename E::Fine vd[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+            vd[b] = E::fine(E::floats(v[b]) * *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]));
+        const float whole = d.whole[0];
+        if constexpr (kStates) total *= whole;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float4v st = state[i] * whole;
+#pragma unroll
+            for (int b = 0; b < kBlocks; b += 2)
+                st = E::mul(E::column_piece(tile, 16 * b, 16 * i, l16, g4), E::column_piece(tile, 16 * (b + 1), 16 * i, l16, g4), vd[b], vd[b + 1], st);
+            state[i] = st;
+        }
+    }
+
+    __device__ __forceinline__ void store(int n, const float4v (&out)[kBlocks]) const {
+        constexpr int kOutSize = sizeof(Out) == 4 ? 4 : 2;
+        const int token = chunk_token(n);
+        const int left = s.len - token, tokens = left < kC ? left : kC;
+        const int row = static_cast<int>(w.out_row);
+        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
+            w.out + (s.first + token) * w.out_row + static_cast<long long>(s.h) * (kHeadSize * kOutSize), 0,
+            (tokens - 1) * row + kHeadSize * kOutSize, 0x00020000);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const int r = 16 * b + l16, t = w.reverse ? kC - 1 - r : r;
+            // (a row that is not there lies behind the descriptor's end)
+            const int off = t < tokens ? t * row + (16 * wave + 4 * g4) * kOutSize : 0x7ffffff0;
+            if constexpr (kOutSize == 4) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, out[b]), rows, off, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uint2v, __builtin_convertvector(out[b], bf16x4)), rows, off, 0, 0);
+            }
+        }
+    }
+
+    // the state's place in memory: [key][value], or turned
+    __device__ __forceinline__ int state_at(int i, int e, bool turned) const {
+        const int c = 16 * i + 4 * g4 + e, j = 16 * wave + l16;
+        return turned ? j * kHeadSize + c : c * kHeadSize + j;
+    }
+    __device__ __forceinline__ void read_state(const float* from, bool turned, float4v (&to)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (turned) {
+                to[i] = *reinterpret_cast<const float4v*>(from + state_at(i, 0, true));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[i][e] = from[state_at(i, e, false)];
+            }
+    }
+    __device__ __forceinline__ void write_state(float* to, bool turned, float factor) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (turned) {
+                *reinterpret_cast<float4v*>(to + state_at(i, 0, true)) = state[i] * factor;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[state_at(i, e, false)] = state[i][e] * factor;
+            }
+    }
+    // the state next to the end of chunk n, if a block of anchor_len tokens ends there
+    __device__ __forceinline__ void keep_anchor(int n) const {
+        const int end = chunk_token(n) + kC;
+        if (end % a.anchor_len != 0 && end < s.len) return;
+        const int blocks = (a.T + a.anchor_len - 1) / a.anchor_len;
+        float4v* to = reinterpret_cast<float4v*>(w.anchors) +
+                      ((static_cast<long long>(s.b) * a.H + s.h) * blocks + (end - 1) / a.anchor_len) * (kHeadSize * kHeadSize / 4) + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i * kThreads] = state[i];
+    }
+
+    // kSums: the rows that the read-outs are multiplied with, in their layout
+    typedef std::conditional_t<E::kSize == 4, uint4v, uint2v> WithPiece;
+    struct With {
+        WithPiece piece[kBlocks];
+    };
+    __device__ __forceinline__ void ask_with(int n, With& to) const {
+        if (!w.with) return;
+        const int token = chunk_token(n), left = s.len - token, tokens = left < kC ? left : kC;
+        const char* rows = w.with + (s.first + token) * w.with_row + static_cast<long long>(s.h) * E::kRow + (16 * wave + 4 * g4) * E::kSize;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const int r = 16 * b + l16;
+            int t = w.reverse ? kC - 1 - r : r;
+            t = t < tokens ? t : tokens - 1;
+            to.piece[b] = *reinterpret_cast<const WithPiece*>(rows + t * w.with_row);
+        }
+    }
+    __device__ __forceinline__ void part_sums(int n, const float4v (&out)[kBlocks], const With& with) const {
+        if (!w.with) return;
+        float* to = reinterpret_cast<float*>(lds + L::kOffSums + (n & 1) * (kC * 64));
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const float4v p = out[b] * E::floats(__builtin_bit_cast(typename E::Raw, with.piece[b]));
+            to[(16 * b + l16) * 16 + 4 * wave + g4] = (p[0] + p[1]) + (p[2] + p[3]);
+        }
+    }
+    __device__ __forceinline__ void fold_sums(int n) const {
+        if (!w.with || lane >= kC) return;
+        const float4v* part = reinterpret_cast<const float4v*>(lds + L::kOffSums + (n & 1) * (kC * 64) + lane * 64);
+        const float4v p = (part[0] + part[1]) + (part[2] + part[3]);
+        const int t = chunk_token(n) + (w.reverse ? kC - 1 - lane : lane);
+        if (t < s.len) w.sums[s.h * a.rows + s.first + t] = (p[0] + p[1]) + (p[2] + p[3]);
+    }
+};
+
+constexpr int kStateFloats = kHeadSize * kHeadSize;
+
+// Runs of consecutive indices on one XCD each, so that heads of the same rows, and the sweeps over the same rows, meet in its L2.
+__device__ __forceinline__ int index_on_xcd() {
+    const int n = gridDim.x, x = blockIdx.x & 7, each = n >> 3, rest = n & 7;
+    return x * each + (x < rest ? x : rest) + (blockIdx.x >> 3);
+}
+
+// Index: unit outermost, then segment, then sweep.
+template <typename T, typename Out, int kC, bool kStates, bool kSums>
+__global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
+    using L = Layout<T, kC, kStates, kSums>;
+    extern __shared__ __align__(16) char lds[];
+    int at = index_on_xcd();
+    const int sweep = at % a.sweeps;
+    at /= a.sweeps;
+    const int unit = at / a.segs, seg = at - unit * a.segs;
+    const Sweep& w = a.sweep[sweep];
+    const Span s = span_of(a, unit, seg);
+    if (seg >= s.segs) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int chunks = s.end > s.begin ? (s.end - s.begin + kC - 1) / kC : 0;
+    Walk<T, Out, kC, kStates, kSums> walk{a, w, s, lds, lane, wave, lane & 15, lane >> 4, s.begin / kC, chunks, {}};
+
+    const long long units = static_cast<long long>(a.B) * a.H;
+    float* const locals = w.locals + unit * static_cast<long long>(kStateFloats);
+    float* const totals = w.locals + a.segs * units * kStateFloats + unit;
+    if constexpr (kStates) {
+        // the segment that nothing follows on the walk hands nothing over
+        if (chunks == 0 || seg == (w.reverse ? 0 : s.segs - 1)) return;
+    }
+    if (chunks > 0) {
+        walk.ask_decays(0);
+        walk.ask_decays(1);
+        walk.ask_rows(0);
+        walk.ask_rows(1);
+        walk.ask_decays(2);
+        walk.ask_rows(2);
+        walk.ask_decays(3);
+    }
+    const float4v zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) walk.state[i] = zero;
+    if constexpr (!kStates) {
+        if (w.state_in) walk.read_state(w.state_in + unit * static_cast<long long>(kStateFloats), w.turned, walk.state);
+        // and what the segments in front of this one hand over, in the walk's order
+        const int count = w.reverse ? s.segs - 1 - seg : seg;
+        for (int x = 0; x < count; ++x) {
+            const int other = w.reverse ? s.segs - 1 - x : x;
+            float4v add[4];
+            walk.read_state(locals + other * units * kStateFloats, w.locals_turned, add);
+            const float decay = totals[other * units];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) walk.state[i] = walk.state[i] * decay + add[i];
+        }
+    }
+    if (chunks > 0) {
+        wait_loads<0>();
+        __syncthreads();
+        if (wave < 2 && wave < chunks) walk.form_decays(wave);
+        __syncthreads();
+        if constexpr (!kStates) walk.form_scores(0);
+        for (int n = 0; n < chunks; ++n) {
+            // every wave's rows of chunk n + 1 are there, chunk n - 1 is done with, and the scores and decays that the last round formed
+            // can be read
+            __syncthreads();
+            typename Walk<T, Out, kC, kStates, kSums>::With with;
+            if constexpr (kSums) {
+                if (n > 0 && wave == (n & 3)) walk.fold_sums(n - 1);
+                walk.ask_with(n, with);
+            }
+            walk.ask_rows(n + 3);
+            walk.ask_decays(n + 4);
+            if (n + 2 < chunks && wave == (n & 3)) walk.form_decays(n + 2);
+            if constexpr (kStates) {
+                walk.advance(n, nullptr);
+                wait_loads<0>();
+            } else {
+                if (w.anchors && w.reverse) walk.keep_anchor(n);
+                if (n + 1 < chunks) walk.form_scores(n + 1);
+                float4v out[L::kBlocks];
+                walk.advance(n, out);
+                wait_loads<0>();
+                walk.store(n, out);
+                if constexpr (kSums) walk.part_sums(n, out, with);
+                if (w.anchors && !w.reverse) walk.keep_anchor(n);
+            }
+        }
+        if constexpr (kSums) {
+            __syncthreads();
+            if (wave == (chunks & 3)) walk.fold_sums(chunks - 1);
+        }
+    }
+    if constexpr (kStates) {
+        walk.write_state(locals + seg * units * kStateFloats, w.locals_turned, 1.f);
+        if (threadIdx.x == 0) totals[seg * units] = walk.total;
+    } else if (w.state_out && seg == (w.reverse ? 0 : s.segs - 1)) {
+        float factor = 1.f;
+        if (w.reverse && s.len > 0) factor = decay_factor(a.g[s.first * a.g_row + s.h]);
+        walk.write_state(w.state_out + unit * static_cast<long long>(kStateFloats), w.turned, factor);
+    }
+}
+
+// dg.  exp(G_t - G_i) with G the running sum of g makes dL/dG_t = r_t . dr_t - k_t . dk_t, plus <dS, S> for a state handed on, so
+//     dg_t = sum_{t <= s <= a} (r_s . dr_s - k_s . dk_s) + w_{a+1} <dS_{a+1}, S_a>
+// for any a >= t; dS_{a+1} is the gradient of the state behind token a + 1, and behind the last token that of state_out.  The sums nearly
+// cancel, so a is the end of t's block of anchor_len tokens and not of the sequence, and they are taken in 64 bits.
+// A workgroup per unit and block.
+__global__ __launch_bounds__(256) void decay_gradient_kernel(const MixArgs a, int blocks, const float* r_sums, const float* k_sums,
+                                                             const float* behind, const float* front, float* head_sums, float* dg) {
+    __shared__ double part[4];
+    int at = index_on_xcd();
+    const int h = at % a.H;
+    at /= a.H;
+    const int b = at / blocks, block = at - b * blocks;
+    const int unit = b * a.H + h;
+    const Span s = span_of(a, unit, 0);
+    const int t0 = block * a.anchor_len, t1 = t0 + a.anchor_len < s.len ? t0 + a.anchor_len : s.len;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (t0 >= t1) {
+        if (head_sums && threadIdx.x == 0) head_sums[(static_cast<long long>(b) * blocks + block) * a.H + h] = 0.f;
+        return;
+    }
+    const long long place = (static_cast<long long>(unit) * blocks + block) * (kStateFloats / 4);
+    const float4v* x = reinterpret_cast<const float4v*>(behind) + place;
+    const float4v* y = reinterpret_cast<const float4v*>(front) + place;
+    double dot = 0.;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4v p = x[i * 256 + threadIdx.x] * y[i * 256 + threadIdx.x];
+        dot += static_cast<double>((p[0] + p[1]) + (p[2] + p[3]));
+    }
+    auto wave_sum = [](double v) {
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
+        return v;
+    };
+    dot = wave_sum(dot);
+    if (lane == 0) part[wave] = dot;
+    __syncthreads();
+    double after = (part[0] + part[1]) + (part[2] + part[3]);
+    if (t1 < s.len) after *= static_cast<double>(decay_factor(a.g[(s.first + t1) * a.g_row + h]));
+    __syncthreads();
+    // from the block's end, 256 tokens at a time
+    double all = 0.;
+    const long long base = h * a.rows + s.first;
+    for (int e = t1; e > t0; e -= 256) {
+        const int t = e - 1 - static_cast<int>(threadIdx.x);
+        double v = t >= t0 ? static_cast<double>(r_sums[base + t]) - static_cast<double>(k_sums[base + t]) : 0.;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const double from = __shfl_up(v, m);
+            if (lane >= m) v += from;
+        }
+        if (lane == 63) part[wave] = v;
+        __syncthreads();
+        double before = after;
+        for (int i = 0; i < wave; ++i) before += part[i];
+        after += (part[0] + part[1]) + (part[2] + part[3]);
+        v += before;
+        if (t >= t0) {
+            if (head_sums) all += v;
+            else dg[(s.first + t) * a.H + h] = static_cast<float>(v);
+        }
+        __syncthreads();
+    }
+    if (head_sums) {
+        all = wave_sum(all);
+        if (lane == 0) part[wave] = all;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            head_sums[(static_cast<long long>(b) * blocks + block) * a.H + h] = static_cast<float>((part[0] + part[1]) + (part[2] + part[3]));
+    }
+}
+
+// dg of one decay a head: the partial sums of a head, always in the same order.  A wave a head.
+__global__ __launch_bounds__(64) void head_sums_kernel(long long count, int H, const float* head_sums, float* dg) {
+    double v = 0.;
+    for (long long i = threadIdx.x; i < count; i += 64) v += static_cast<double>(head_sums[i * H + blockIdx.x]);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
+    if (threadIdx.x == 0) dg[blockIdx.x] = static_cast<float>(v);
+}
+
+constexpr int kChunkBf16 = 64, kChunkF32 = 32;
+
+// f(kernel, LDS bytes) for the kernel of these rows
+template <bool kStates, bool kSums, typename F>
+hipError_t with_mix(bool f32_rows, bool f32_out, F f) {
+    if (f32_rows) return f(&mix_kernel<float, float, kChunkF32, kStates, kSums>, Layout<float, kChunkF32, kStates, kSums>::kLds);
+    if constexpr (!kStates && !kSums)
+        if (f32_out) return f(&mix_kernel<Bf16, float, kChunkBf16, kStates, kSums>, Layout<Bf16, kChunkBf16, kStates, kSums>::kLds);
+    return f(&mix_kernel<Bf16, Bf16, kChunkBf16, kStates, kSums>, Layout<Bf16, kChunkBf16, kStates, kSums>::kLds);
+}
+
+template <bool kStates, bool kSums>
+hipError_t launch(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t stream) {
+    const unsigned grid = static_cast<unsigned>(static_cast<long long>(a.B) * a.H * a.segs * a.sweeps);
+    return with_mix<kStates, kSums>(f32_rows, f32_out, [&](auto kernel, int lds) {
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), lds, stream, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+MixPlan plan_mix(int B, int T, int H, bool backward) {
+    const long long units = static_cast<long long>(B) * H * (backward ? 3 : 1);
+    MixPlan p;
+    p.segs = 1;
+    if (units < 256) {
+        long long segs = 512 / units;
+        const long long most = T / 256;
+        if (segs > most) segs = most;
+        if (segs > 32) segs = 32;
+        if (segs > 1) p.segs = static_cast<int>(segs);
+    }
+    const long long step = T > 1024LL * p.segs ? 1024 : kMixBlock;
+    const long long each = (static_cast<long long>(T > 0 ? T : 1) + p.segs - 1) / p.segs;
+    p.seg_len = static_cast<int>((each + step - 1) / step * step);
+    p.segs = T > 0 ? (T + p.seg_len - 1) / p.seg_len : 1;
+    p.anchor_len = p.seg_len > 1024 ? 1024 : p.seg_len;
+    return p;
+}
+
+hipError_t raise_mix_limits() {
+    struct Raised;
+    return once_per_device<Raised>([] {
+        auto raise = [](auto kernel, int lds) { return set_lds_limit(kernel, lds); };
+        for (int i = 0; i < 3; ++i) {
+            const bool f32_rows = i == 2, f32_out = i > 0;
+            hipError_t err = with_mix<false, false>(f32_rows, f32_out, raise);
+            if (err == hipSuccess) err = with_mix<true, false>(f32_rows, f32_out, raise);
+            if (err == hipSuccess) err = with_mix<false, true>(f32_rows, f32_out, raise);
+            if (err != hipSuccess) return err;
+        }
+        return hipSuccess;
+    });
+}
+
+hipError_t launch_mix(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t stream) {
+    return a.sweeps > 1 ? launch<false, true>(a, f32_rows, f32_rows, stream) : launch<false, false>(a, f32_rows, f32_out, stream);
+}
+
+hipError_t launch_mix_locals(const MixArgs& a, int count, bool f32_rows, hipStream_t stream) {
+    MixArgs part = a;
+    part.sweeps = count;
+    return launch<true, false>(part, f32_rows, f32_rows, stream);
+}
+
+hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const float* k_sums, const float* behind, const float* front,
+                                 float* head_sums, float* dg, hipStream_t stream) {
+    const int blocks = (a.T + a.anchor_len - 1) / a.anchor_len;
+    const long long count = static_cast<long long>(a.B) * blocks;
+    if (count > 0)
+        hipLaunchKernelGGL(decay_gradient_kernel, dim3(static_cast<unsigned>(count * a.H)), dim3(256), 0, stream, a, blocks, r_sums, k_sums,
+                           behind, front, head_sums, dg);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess || !head_sums) return err;
+    hipLaunchKernelGGL(head_sums_kernel, dim3(static_cast<unsigned>(a.H)), dim3(64), 0, stream, count, a.H, head_sums, dg);
+    return hipGetLastError();
+}
+
+}  // namespace wkv6

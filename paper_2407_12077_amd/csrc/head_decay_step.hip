@@ -1,0 +1,97 @@
+// The head-decay time mix for one token of every sequence: S = exp(g) S_in + k^T v, o = r S.
+//
+// Bound by the states, which are read and written once.  A lane holds four columns of sixteen key rows (or of four, with four waves a
+// unit), so that a load takes whole lines, r and k of a lane's rows are consecutive, and all of its state is on its way at once.
+#include "head_decay.h"
+#include "wkv6_math.h"
+
+namespace wkv6 {
+namespace {
+
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef unsigned uint2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+template <bool kF32>
+__device__ __forceinline__ float4v four(const char* p) {
+    if constexpr (kF32) {
+        return *reinterpret_cast<const float4v*>(p);
+    } else {
+        const uint2v u = *reinterpret_cast<const uint2v*>(p);
+        return float4v{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+    }
+}
+
+// kWaves of a unit; a workgroup is always four
+template <bool kF32, bool kOutF32, int kWaves>
+__global__ __launch_bounds__(256) void mix_step_kernel(int units, int H, const char* r, const char* k, const char* v, long long row_bytes,
+                                                       const float* g, long long g_row, const float* state_in, void* out, float* state_out) {
+    constexpr int kSize = kF32 ? 4 : 2, kRows = 16 / kWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int unit = kWaves == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
+    if (kWaves == 1 && unit >= units) return;
+    const int b = unit / H, h = unit - b * H;
+    const int j = 4 * (lane & 15), c0 = (lane >> 4) * 16 + (kWaves == 4 ? 4 * wave : 0);
+    const long long state = static_cast<long long>(unit) * (kHeadSize * kHeadSize) + c0 * kHeadSize + j;
+    float4v s[kRows];
+    if (state_in) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) s[i] = __builtin_nontemporal_load(reinterpret_cast<const float4v*>(state_in + state + i * kHeadSize));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) s[i] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+    const long long row = b * row_bytes + h * (kHeadSize * kSize);
+    const float4v vj = four<kF32>(v + row + j * kSize);
+    float4v rc[kRows / 4], kc[kRows / 4];
+#pragma unroll
+    for (int i = 0; i < kRows / 4; ++i) {
+        rc[i] = four<kF32>(r + row + (c0 + 4 * i) * kSize);
+        kc[i] = four<kF32>(k + row + (c0 + 4 * i) * kSize);
+    }
+    const float decay = expf(g[b * g_row + h]);
+    float4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        s[i] = s[i] * decay + vj * kc[i / 4][i % 4];
+        o += s[i] * rc[i / 4][i % 4];
+        if (state_out) __builtin_nontemporal_store(s[i], reinterpret_cast<float4v*>(state_out + state + i * kHeadSize));
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        o[e] += __shfl_xor(o[e], 16);
+        o[e] += __shfl_xor(o[e], 32);
+    }
+    if constexpr (kWaves == 4) {
+        __shared__ float4v part[4][16];
+        if (lane < 16) part[wave][lane] = o;
+        __syncthreads();
+        if (wave > 0) return;
+        o = (part[0][lane & 15] + part[1][lane & 15]) + (part[2][lane & 15] + part[3][lane & 15]);
+    }
+    if (lane < 16) {
+        const long long to = static_cast<long long>(unit) * kHeadSize + j;
+        if constexpr (kOutF32) *reinterpret_cast<float4v*>(static_cast<float*>(out) + to) = o;
+        else *reinterpret_cast<uint2v*>(static_cast<char*>(out) + 2 * to) = __builtin_bit_cast(uint2v, __builtin_convertvector(o, bf16x4));
+    }
+}
+
+}  // namespace
+
+hipError_t launch_mix_step(int B, int H, const void* r, const void* k, const void* v, long long row_stride, const float* g,
+                           long long g_row, const float* state_in, void* out, float* state_out, bool f32_rows, bool f32_out,
+                           hipStream_t stream) {
+    const int units = B * H;
+    const bool four_waves = units <= 1024;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(four_waves ? units : (units + 3) / 4), dim3(256), 0, stream, units, H, static_cast<const char*>(r),
+                           static_cast<const char*>(k), static_cast<const char*>(v), row_stride * (f32_rows ? 4 : 2), g, g_row, state_in, out,
+                           state_out);
+        return hipGetLastError();
+    };
+    if (f32_rows) return four_waves ? go(&mix_step_kernel<true, true, 4>) : go(&mix_step_kernel<true, true, 1>);
+    if (f32_out) return four_waves ? go(&mix_step_kernel<false, true, 4>) : go(&mix_step_kernel<false, true, 1>);
+    return four_waves ? go(&mix_step_kernel<false, false, 4>) : go(&mix_step_kernel<false, false, 1>);
+}
+
+}  // namespace wkv6
