@@ -29,7 +29,8 @@
  * rows with fp32.
  *
  * Arithmetic: fp32 states, sums and decays.  Of bf16 rows the products are formed on the bf16 matrix cores; operands that are no rows
- * (states, scores, decayed values) enter as the sum of two bf16, 2^-17 of their size, and keep fp32's range.  fp32 rows: fp32 throughout.
+ * (states, scores, decayed values) enter as sums of bf16 that hold fp32 values whole, over fp32's range (2^-17 of them where only bf16
+ * read-outs depend on it).  fp32 rows: fp32 throughout.
  * Values have to be finite: a NaN or infinity in a row reaches other tokens of its sequence, also earlier ones, not other sequences.
  *
  * Workspace: device memory of the caller, 16-byte aligned, as many bytes as the function beside the call says (none where that is 0),

@@ -14,18 +14,17 @@
 //     dr = mix(q = do, k = v, v = k; S_0 transposed)     dv = reversed mix(q = k, k = r, v = do)     dk = reversed mix(q = v, k = do, v = r)
 // and that of g_t is the sum of r.dr - k.dk from t to the end of any later block plus <dS, S> there: see decay_gradient_kernel.
 //
-// A workgroup of four waves takes one segment of one (sequence, head) and walks its chunks.  Rows go straight from memory into LDS,
-// kStages - 1 chunks ahead; a wave owns 16 of the 64 value columns: the state's [64][16] columns stay in its registers for the whole
-// walk, and the transposed products leave every operand where the next one needs it:
-//     P^T (keys x queries)  from rows of k and q as they lie; its accumulators are, lane by lane, the operand of the next product.  The
-//                           waves share the blocks on and below the diagonal, one chunk ahead of their use
-//     o^T (values x queries) = v^T P^T + S^T q^T: v through transposing reads, the state straight from the accumulators
-//     S (keys x values)      = k^T (decayed v)
-// One barrier a chunk.
+// A workgroup takes one segment of one (sequence, head) and walks its chunks.  Its eight waves have two parts, one of each on a SIMD, so that
+// one's matrix products run beside the other's vector instructions and waits; they meet at one barrier a chunk:
+//   producers  bring the rows straight from memory into LDS, kStages - 1 chunks ahead, form the decays two chunks ahead, and one chunk ahead
+//              the part of the read-outs that needs no state: a producer takes 16 queries, P^T (keys x queries) from the rows of k and q as
+//              they lie, whose accumulators are, lane by lane, the operand of v^T P^T (v through transposing reads); so P never
+//              leaves the registers, and the sums go to the consumers through LDS
+//   consumers  own 16 of the 64 value columns each: the state's [64][16] columns stay in registers for the whole walk, and as accumulators
+//              of k^T (decayed v) they lie as S^T q^T wants them.  They store the read-outs
 //
-// bf16 rows: products of rows are exact in fp32; the computed operands (P, S, decayed v) are kept as a sum of two bf16, 16 significant
-// bits and the whole exponent range, each product twice.  So nothing has to stay inside the range of fp16, and the fp32 results
-// are good to about 2^-17 of their size.  fp32 rows: fp32 matrix instructions throughout.
+// bf16 rows: products of rows are exact in fp32; the computed operands (P, S, decayed v) enter as sums of three bf16, which hold an
+// fp32 value whole over its whole range, one product for each; two where only bf16 read-outs come of them.  fp32 rows: fp32 matrix instructions.
 #include "head_decay.h"
 #include "wkv6_lds_loads.h"
 #include "wkv6_math.h"
@@ -43,7 +42,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned uint2v __attribute__((ext_vector_type(2)));
 typedef unsigned uint4v __attribute__((ext_vector_type(4)));
 
-struct Bf16 {};
+struct Bf16 {
+    short bits;
+};
 
 // What differs between the types of rows.  Raw: four consecutive contraction indices of an operand as they lie in a tile.  Fine: four
 // computed ones.  A tile is kC rows of kHeadSize values in places of 16 bytes, which a row's number permutes so that the reads below
@@ -55,8 +56,9 @@ template <>
 struct Elem<Bf16> {
     static constexpr int kSize = 2, kRow = kHeadSize * kSize, kPlaces = kRow / 16;
     typedef short4v Raw;
+    template <int kTerms>
     struct Fine {
-        short4v hi, lo;
+        short4v term[kTerms];
     };
     __device__ static __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
     __device__ static __forceinline__ int at(int row, int place) { return row * kRow + 16 * (place ^ swizzle(row)); }
@@ -64,39 +66,81 @@ struct Elem<Bf16> {
     __device__ static __forceinline__ Raw row_piece(const char* tile, int row, int q, int g4) {
         return *reinterpret_cast<const Raw*>(tile + at(row, 2 * q + (g4 >> 1)) + 8 * (g4 & 1));
     }
-    // lanes are columns c0 + l16, contraction indices rows r0 + 4 g4 ..: a transposing read, in which lane i of sixteen passes the
-    // address of four columns of row i / 4 and gets column i of the four rows
-    __device__ static __forceinline__ Raw column_piece(const char* tile, int r0, int c0, int l16, int g4) {
-        typedef short4v __attribute__((address_space(3))) * lds_ptr;
-        const int row = r0 + 4 * g4 + (l16 >> 2), col = c0 + 4 * (l16 & 3);
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + at(row, col >> 3) + 8 * (col >> 2 & 1)));
+    // lanes are columns c0 + l16, contraction indices rows 16 b + 4 g4 ..: transposing reads, in which lane i of sixteen passes the
+    // address of four columns of row i / 4 and gets column i of the four rows.  Rows sixteen apart are permuted alike.
+    // (In assembly with their wait: in front of the builtin the compiler waits for all loads into LDS, the ones on their way to other places
+    // included.)
+    __device__ static __forceinline__ int column_at(int c0, int l16, int g4) {
+        const int row = 4 * g4 + (l16 >> 2), col = c0 + 4 * (l16 & 3);
+        return at(row, col >> 3) + 8 * (col >> 2 & 1);
+    }
+    __device__ static __forceinline__ void column(const char* tile, int c0, int l16, int g4, Raw (&to)[4]) {
+        typedef __attribute__((address_space(3))) const char* lds_ptr;
+#if defined(__HIP_DEVICE_COMPILE__)
+        const unsigned from = static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_ptr)tile)) + column_at(c0, l16, g4);
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %4\n"
+            "ds_read_b64_tr_b16 %1, %4 offset:2048\n"
+            "ds_read_b64_tr_b16 %2, %4 offset:4096\n"
+            "ds_read_b64_tr_b16 %3, %4 offset:6144\n"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(to[0]), "=&v"(to[1]), "=&v"(to[2]), "=&v"(to[3]) : "v"(from) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+#endif
+    }
+    // columns 32 i + l16 and those sixteen further
+    __device__ static __forceinline__ void columns(const char* tile, int i, int l16, int g4, Raw (&to)[2][4]) {
+        typedef __attribute__((address_space(3))) const char* lds_ptr;
+#if defined(__HIP_DEVICE_COMPILE__)
+        const unsigned base = static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_ptr)tile));
+        const unsigned p = base + column_at(32 * i, l16, g4), q = base + column_at(32 * i + 16, l16, g4);
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %8\n"
+            "ds_read_b64_tr_b16 %1, %8 offset:2048\n"
+            "ds_read_b64_tr_b16 %2, %8 offset:4096\n"
+            "ds_read_b64_tr_b16 %3, %8 offset:6144\n"
+            "ds_read_b64_tr_b16 %4, %9\n"
+            "ds_read_b64_tr_b16 %5, %9 offset:2048\n"
+            "ds_read_b64_tr_b16 %6, %9 offset:4096\n"
+            "ds_read_b64_tr_b16 %7, %9 offset:6144\n"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(to[0][0]), "=&v"(to[0][1]), "=&v"(to[0][2]), "=&v"(to[0][3]), "=&v"(to[1][0]), "=&v"(to[1][1]), "=&v"(to[1][2]),
+              "=&v"(to[1][3]) : "v"(p), "v"(q) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+#endif
     }
     __device__ static __forceinline__ float4v floats(Raw r) {
         const uint2v u = __builtin_bit_cast(uint2v, r);
         return float4v{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
     }
-    // the sum of two bf16 nearest to x: 2^-17 of x, where one would be 2^-9
-    __device__ static __forceinline__ Fine fine(float4v x) {
-        Fine f;
-        f.hi = __builtin_bit_cast(short4v, __builtin_convertvector(x, bf16x4));
-        f.lo = __builtin_bit_cast(short4v, __builtin_convertvector(x - floats(f.hi), bf16x4));
+    // x as a sum of bf16, largest first: three hold all 24 bits of it, two are 2^-17 off
+    template <int kTerms>
+    __device__ static __forceinline__ Fine<kTerms> fine(float4v x) {
+        Fine<kTerms> f;
+#pragma unroll
+        for (int i = 0; i < kTerms; ++i) {
+            f.term[i] = __builtin_bit_cast(short4v, __builtin_convertvector(x, bf16x4));
+            if (i + 1 < kTerms) x -= floats(f.term[i]);
+        }
         return f;
     }
     __device__ static __forceinline__ bf16x8 both(Raw a, Raw b) {
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-    // acc += A B over 32 contraction indices (two pieces) or 16
-    __device__ static __forceinline__ float4v mul(Raw a0, Raw a1, const Fine& b0, const Fine& b1, float4v acc) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0.lo, b1.lo), acc, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0.hi, b1.hi), acc, 0, 0, 0);
+    // acc += A B over 32 contraction indices (two pieces)
+    template <int kTerms>
+    __device__ static __forceinline__ float4v mul(Raw a0, Raw a1, const Fine<kTerms>& b0, const Fine<kTerms>& b1, float4v acc) {
+#pragma unroll
+        for (int i = kTerms - 1; i >= 0; --i)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0.term[i], b1.term[i]), acc, 0, 0, 0);
+        return acc;
     }
-    __device__ static __forceinline__ float4v mul(const Fine& a0, const Fine& a1, Raw b0, Raw b1, float4v acc) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0.lo, a1.lo), both(b0, b1), acc, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0.hi, a1.hi), both(b0, b1), acc, 0, 0, 0);
-    }
-    __device__ static __forceinline__ float4v mul(Raw a, const Fine& b, float4v acc) {
-        const short4v none = {0, 0, 0, 0};
-        return mul(a, none, b, Fine{none, none}, acc);
+    template <int kTerms>
+    __device__ static __forceinline__ float4v mul(const Fine<kTerms>& a0, const Fine<kTerms>& a1, Raw b0, Raw b1, float4v acc) {
+#pragma unroll
+        for (int i = kTerms - 1; i >= 0; --i)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0.term[i], a1.term[i]), both(b0, b1), acc, 0, 0, 0);
+        return acc;
     }
     // rows a of one tile times rows b of another over all columns
     __device__ static __forceinline__ float4v row_products(const char* ta, int ra, const char* tb, int rb, int g4) {
@@ -113,23 +157,31 @@ template <>
 struct Elem<float> {
     static constexpr int kSize = 4, kRow = kHeadSize * kSize, kPlaces = kRow / 16;
     typedef float4v Raw;
-    typedef float4v Fine;
+    template <int kTerms>
+    using Fine = float4v;
     __device__ static __forceinline__ int swizzle(int row) { return row & 15; }
     __device__ static __forceinline__ int at(int row, int place) { return row * kRow + 16 * (place ^ swizzle(row)); }
     __device__ static __forceinline__ Raw row_piece(const char* tile, int row, int q, int g4) {
         return *reinterpret_cast<const Raw*>(tile + at(row, 4 * q + g4));
     }
-    __device__ static __forceinline__ Raw column_piece(const char* tile, int r0, int c0, int l16, int g4) {
-        Raw r;
+    template <int kBlocks>
+    __device__ static __forceinline__ void column(const char* tile, int c0, int l16, int g4, Raw (&to)[kBlocks]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = r0 + 4 * g4 + e, col = c0 + l16;
-            r[e] = *reinterpret_cast<const float*>(tile + at(row, col >> 2) + 4 * (col & 3));
-        }
-        return r;
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = 16 * b + 4 * g4 + e, col = c0 + l16;
+                to[b][e] = *reinterpret_cast<const float*>(tile + at(row, col >> 2) + 4 * (col & 3));
+            }
+    }
+    template <int kBlocks>
+    __device__ static __forceinline__ void columns(const char* tile, int i, int l16, int g4, Raw (&to)[2][kBlocks]) {
+        column(tile, 32 * i, l16, g4, to[0]);
+        column(tile, 32 * i + 16, l16, g4, to[1]);
     }
     __device__ static __forceinline__ float4v floats(Raw r) { return r; }
-    __device__ static __forceinline__ Fine fine(float4v x) { return x; }
+    template <int kTerms>
+    __device__ static __forceinline__ float4v fine(float4v x) { return x; }
     __device__ static __forceinline__ float4v mul(float4v a, float4v b, float4v acc) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc, 0, 0, 0);
@@ -146,9 +198,9 @@ struct Elem<float> {
     }
 };
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kStages = 4;             // places for a chunk's tiles: the chunk at hand, the next, and two on their way
-constexpr int kDecayPlaces = 8;        // places for a chunk's g: asked for a chunk earlier than the rows
+constexpr int kWaves = 4, kThreads = 2 * 64 * kWaves;          // waves of either part
+constexpr int kGPlaces = 8;            // places for a chunk's g, asked for a chunk earlier than the rows,
+constexpr int kDecayPlaces = 3;        // and for its decays: being formed, the producers', the consumers'
 constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
 
 // A chunk's decays by token, in LDS.  In logarithms to base 2 (pre) or as factors (the others)
@@ -161,24 +213,63 @@ struct Decays {
     float in_chunk[kC];                // from the chunk's first token to this
     float to_chunk[kC];                // from behind this token to the chunk's end; nought for tokens that are not there
     float block[kC / 16];              // of whole blocks
-    float whole[4];                    // of the whole chunk (one value)
+    float less[4];                     // of the whole chunk, less one (one value)
 };
 
-template <typename T, int kC, bool kStates, bool kSums>
+template <typename T, typename Out, int kC, bool kStates, bool kSums>
 struct Layout {
     static constexpr int kTile = kC * Elem<T>::kRow;
     static constexpr int kTiles = kStates ? 2 : 3;               // k, v, q
     static constexpr int kStage = kTile * kTiles;
-    static constexpr int kBlocks = kC / 16, kPairs = kBlocks * (kBlocks + 1) / 2;
-    static constexpr int kScores = kStates ? 0 : kPairs * 1024;  // four Fine values a lane and pair of blocks
+    // places for a chunk's tiles: the consumers', the producers', and as many on their way as fit
+    static constexpr int kStages = kSums ? 4 : 5;
+    static constexpr int kBlocks = kC / 16;
+    // terms of a bf16 operand that is no row.  What reaches fp32 results (states, gradients of decays, fp32 read-outs) keeps
+    // all bits; for read-outs that are rounded to bf16, 2^-17 is far below that rounding
+    static constexpr int kStateTerms = 3, kOutTerms = sizeof(Out) == 4 || kSums ? 3 : 2;
+    static constexpr int kInner = kStates ? 0 : kC * kHeadSize * 4;    // the producers' read-outs
     static constexpr int kOffG = kStages * kStage;
-    static constexpr int kOffDecays = kOffG + kDecayPlaces * 256;
-    static constexpr int kOffScores = kOffDecays + 4 * static_cast<int>(sizeof(Decays<kC>));
-    static constexpr int kOffSums = kOffScores + 2 * kScores;    // [chunk parity][token][wave][g4]
+    static constexpr int kOffDecays = kOffG + kGPlaces * 256;
+    static constexpr int kOffInner = kOffDecays + kDecayPlaces * static_cast<int>(sizeof(Decays<kC>));
+    static constexpr int kOffSums = kOffInner + 2 * kInner;      // [chunk parity][token][wave][g4]
     static constexpr int kLds = kOffSums + (kSums ? 2 * kC * 64 : 0);
-    static constexpr int kLoads = kTile / 1024 / kWaves;         // of a wave, tile and chunk
+    static constexpr int kLoads = kTile / 1024 / kWaves;         // of a producer, tile and chunk
+    static constexpr int kAsked = kLoads * kTiles + 1;           // and g
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
+
+__device__ __forceinline__ void lds_barrier() {                // all waves; loads and stores stay on their way
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);         // the wave's own LDS reads and writes
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// A value that is the same in all lanes, in a scalar register: what depends on the kernel's argument or on memory through a computed
+// index is not known to be, and a descriptor of such would be read lane by lane.
+template <typename V>
+__device__ __forceinline__ V uniform(V v) {
+    if constexpr (sizeof(V) == 8) {
+        const uint2v u = __builtin_bit_cast(uint2v, v);
+        return __builtin_bit_cast(V, uint2v{static_cast<unsigned>(__builtin_amdgcn_readfirstlane(u.x)), static_cast<unsigned>(__builtin_amdgcn_readfirstlane(u.y))});
+    } else {
+        return static_cast<V>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
+    }
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const char* base, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(uniform(base)), 0, uniform(bytes), 0x00020000);
+}
+__device__ __forceinline__ Sweep uniform_sweep(const Sweep& w) {
+    Sweep u;
+    u.q = uniform(w.q); u.k = uniform(w.k); u.v = uniform(w.v);
+    u.q_row = uniform(w.q_row); u.k_row = uniform(w.k_row); u.v_row = uniform(w.v_row);
+    u.out = uniform(w.out); u.out_row = uniform(w.out_row);
+    u.with = uniform(w.with); u.with_row = uniform(w.with_row); u.sums = uniform(w.sums);
+    u.state_in = uniform(w.state_in); u.state_out = uniform(w.state_out);
+    u.locals = uniform(w.locals); u.anchors = uniform(w.anchors);
+    u.reverse = uniform(w.reverse); u.turned = uniform(w.turned); u.locals_turned = uniform(w.locals_turned);
+    return u;
+}
 
 struct Span {                          // a workgroup's tokens
     int b, h, len;                     // sequence, head, the sequence's tokens
@@ -190,10 +281,10 @@ struct Span {                          // a workgroup's tokens
 // Offsets are taken as they are as far as they lie inside the rows: nothing outside the tensors is touched, whatever they hold.
 __device__ __forceinline__ Span span_of(const MixArgs& a, int unit, int seg) {
     Span s;
-    s.b = unit / a.H;
+    s.b = uniform(unit / a.H);
     s.h = unit - s.b * a.H;
     if (a.offsets) {
-        long long lo = a.offsets[s.b], hi = a.offsets[s.b + 1];
+        long long lo = uniform(a.offsets[s.b]), hi = uniform(a.offsets[s.b + 1]);
         lo = lo < 0 ? 0 : lo > a.rows ? a.rows : lo;
         hi = hi < lo ? lo : hi > a.rows ? a.rows : hi;
         s.first = lo;
@@ -230,16 +321,16 @@ __device__ __forceinline__ float prefix16(float v) {
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
 struct Walk {
     using E = Elem<T>;
-    using L = Layout<T, kC, kStates, kSums>;
+    using L = Layout<T, Out, kC, kStates, kSums>;
     static constexpr int kBlocks = L::kBlocks;
 
     const MixArgs& a;
-    const Sweep& w;
+    const Sweep w;
     const Span s;
     char* const lds;
-    const int lane, wave, l16, g4;
+    const int lane, wave, l16, g4;                              // wave of its part
     const int first_chunk, chunks;                              // of the segment
-    float4v state[4];                                           // S[16 i + 4 g4 + e][16 wave + l16]
+    float4v state[4];                                           // consumers: S[16 i + 4 g4 + e][16 wave + l16]
     float total = 1.f;                                          // kStates: decay of all chunks so far
 
     // token of the chunk's first place, by the chunk's number on the walk
@@ -249,8 +340,7 @@ struct Walk {
         // rows behind the sequence's last token are that token's again: their factors are nought
         const long long first = s.first + token;
         const int bytes = static_cast<int>((tokens - 1) * row_bytes) + E::kRow;
-        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<char*>(base) + first * row_bytes + static_cast<long long>(s.h) * E::kRow, 0, bytes, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rows = descriptor(base + first * row_bytes + static_cast<long long>(s.h) * E::kRow, bytes);
         typedef __attribute__((address_space(3))) char* lds_ptr;
         constexpr int kRowsALoad = 1024 / E::kRow;
 #pragma unroll
@@ -262,18 +352,16 @@ struct Walk {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(lds + to + (wave * L::kLoads + i) * 1024), 16, off, 0, 0, 0);
         }
     }
-    // a chunk's rows, always the same number of loads: past the segment's last chunk it is that one again
     __device__ __forceinline__ void ask_rows(int n) const {
-        const int to = (n & (kStages - 1)) * L::kStage;
-        const int token = chunk_token(n < chunks ? n : chunks - 1);
-        const int left = s.len - token, tokens = left < kC ? left : kC;
+        const int to = n % L::kStages * L::kStage;
+        const int token = chunk_token(n), left = s.len - token, tokens = left < kC ? left : kC;
         ask_tile(w.k, w.k_row, tokens, token, to);
         ask_tile(w.v, w.v_row, tokens, token, to + L::kTile);
         if constexpr (!kStates) ask_tile(w.q, w.q_row, tokens, token, to + 2 * L::kTile);
     }
-    // and its g by place (each wave's sixteen lanes of it, so that all waves have asked for as many loads).  In reverse a token's is that of
+    // g by place (each producer's sixteen lanes of it, so that all have asked for as many loads).  In reverse a token's is that of
     // the token behind it; places without one are cleared where they are read
-    __device__ __forceinline__ void ask_decays(int n) const {
+    __device__ __forceinline__ void ask_g(int n) const {
         const int token = chunk_token(n < chunks ? n : chunks - 1);
         typedef __attribute__((address_space(3))) char* lds_ptr;
         int t = token + (w.reverse ? kC - lane : lane);
@@ -282,12 +370,12 @@ struct Walk {
         const bool mine = (lane >> 4) == wave;
         if (mine)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                             (lds_ptr)(lds + L::kOffG + (n & (kDecayPlaces - 1)) * 256), 4, 0, 0);
+                                             (lds_ptr)(lds + L::kOffG + (n & (kGPlaces - 1)) * 256), 4, 0, 0);
     }
-    static constexpr int kAsked = L::kLoads * L::kTiles + 1;    // loads of a wave and chunk
 
+    __device__ __forceinline__ char* rows_of(int n) const { return lds + n % L::kStages * L::kStage; }
     __device__ __forceinline__ Decays<kC>& decays(int n) const {
-        return *reinterpret_cast<Decays<kC>*>(lds + L::kOffDecays + (n & 3) * static_cast<int>(sizeof(Decays<kC>)));
+        return *reinterpret_cast<Decays<kC>*>(lds + L::kOffDecays + n % kDecayPlaces * static_cast<int>(sizeof(Decays<kC>)));
     }
 
     // the chunk's decays, by one wave, a lane a token
@@ -296,7 +384,7 @@ struct Walk {
         const int token = chunk_token(n);
         const int at = lane < kC ? lane : 0;
         const int t = token + (w.reverse ? kC - 1 - at : at);
-        float g = *reinterpret_cast<const float*>(lds + L::kOffG + (n & (kDecayPlaces - 1)) * 256 + 4 * at);
+        float g = *reinterpret_cast<const float*>(lds + L::kOffG + (n & (kGPlaces - 1)) * 256 + 4 * at);
         const bool there = t < s.len;
         const bool has = w.reverse ? t + 1 < s.len : there;
         g = g < kLowest ? kLowest : g;                          // (NaN stays)
@@ -324,51 +412,64 @@ struct Walk {
             d.in_chunk[lane] = __builtin_amdgcn_exp2f(before + pre);
             d.to_chunk[lane] = there ? __builtin_amdgcn_exp2f(behind + after) : 0.f;
             if ((lane & 15) == 0) d.block[lane >> 4] = __builtin_amdgcn_exp2f(block);
-            if (lane == 0) d.whole[0] = __builtin_amdgcn_exp2f(all);
+            // S + (w - 1) S has one rounding of the size of S where w S has two: with a decay near one, and the same in every chunk, these
+            // would add up over the chunks that the state remembers
+            if (lane == 0) d.less[0] = expm1f(all * 0.6931471805599453f);
         }
     }
 
-    // P^T of the wave's share of the chunk's pairs of blocks
-    __device__ __forceinline__ void form_scores(int n) const {
-        const char* tile = lds + (n & (kStages - 1)) * L::kStage;
+    // A producer's part of sum_{i <= t} P_ti v_i: 16 queries (with fewer blocks than producers, of a share of the columns)
+    __device__ __forceinline__ void form_inner(int n) const {
+        const int qb = wave % kBlocks, j0 = wave / kBlocks * kBlocks;        // blocks of 16
+        const char* tile = rows_of(n);
         const Decays<kC>& d = decays(n);
-        char* to = lds + L::kOffScores + (n & 1) * L::kScores;
+        const int query = 16 * qb + l16;
+        typename E::template Fine<L::kOutTerms> p[kBlocks];
+        float4v acc[kBlocks];
 #pragma unroll
-        for (int x = 0; x * kWaves < L::kPairs; ++x) {
-            const int p = x * kWaves + wave;
-            if (p >= L::kPairs) break;
-            const int qb = static_cast<int>(0x3333222110ull >> 4 * p & 15), kb = static_cast<int>(0x3210210100ull >> 4 * p & 15);
-            const int query = 16 * qb + l16, key = 16 * kb + 4 * g4;
+        for (int j = 0; j < kBlocks; ++j) acc[j] = float4v{0.f, 0.f, 0.f, 0.f};
+        float f = d.in_block[query];                            // from behind block kb to the query
+#pragma unroll
+        for (int kb = kBlocks - 1; kb >= 0; --kb) {
+            if (kb > qb) {
+                p[kb] = {};
+                continue;
+            }
+            const int key = 16 * kb + 4 * g4;
             float4v sc = E::row_products(tile, 16 * kb + l16, tile + 2 * L::kTile, query, g4);
-            if (qb == kb) {
+            if (kb == qb) {
                 const float pre = d.pre[query];
                 const float4v pk = *reinterpret_cast<const float4v*>(&d.pre_key[key]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sc[e] = key + e <= query ? sc[e] * __builtin_amdgcn_exp2f(pre - pk[e]) : 0.f;
             } else {
-                float f = d.in_block[query];
-                for (int i = kb + 1; i < qb; ++i) f *= d.block[i];
-                const float4v tb = *reinterpret_cast<const float4v*>(&d.to_block[key]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[e] = sc[e] * (tb[e] * f);
+                sc *= *reinterpret_cast<const float4v*>(&d.to_block[key]) * f;
+                f *= d.block[kb];
             }
-            *reinterpret_cast<typename E::Fine*>(to + p * 1024 + lane * 16) = E::fine(sc);
+            p[kb] = E::template fine<L::kOutTerms>(sc);
+        }
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+            typename E::Raw v[kBlocks];
+            E::column(tile + L::kTile, 16 * (j0 + j), l16, g4, v);
+#pragma unroll
+            for (int kb = 0; kb < kBlocks; kb += 2)
+                if (kb <= qb) acc[j] = E::mul(v[kb], v[kb + 1], p[kb], p[kb + 1], acc[j]);
+            *reinterpret_cast<float4v*>(lds + L::kOffInner + (n & 1) * L::kInner + (qb * 4 + j0 + j) * 1024 + lane * 16) = acc[j];
         }
     }
 
-    // read-outs of the chunk and the state behind it
+    // A consumer's read-outs of the chunk and the state behind it
     __device__ __forceinline__ void advance(int n, float4v* out) {
-        const char* tile = lds + (n & (kStages - 1)) * L::kStage;
+        const char* tile = rows_of(n);
         const Decays<kC>& d = decays(n);
         typename E::Raw v[kBlocks];
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) v[b] = E::column_piece(tile + L::kTile, 16 * b, 16 * wave, l16, g4);
+        E::column(tile + L::kTile, 16 * wave, l16, g4, v);
         if constexpr (!kStates) {
-            typename E::Fine st[4];
+            typename E::template Fine<L::kOutTerms> st[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) st[i] = E::fine(state[i]);
+            for (int i = 0; i < 4; ++i) st[i] = E::template fine<L::kOutTerms>(state[i]);
             const char* q = tile + 2 * L::kTile;
-            const char* sc = lds + L::kOffScores + (n & 1) * L::kScores + lane * 16;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 const int query = 16 * b + l16;
@@ -376,29 +477,29 @@ struct Walk {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
                     o = E::mul(st[2 * m], st[2 * m + 1], E::row_piece(q, query, 2 * m, g4), E::row_piece(q, query, 2 * m + 1, g4), o);
-                o *= d.in_chunk[query];
-                const int p0 = b * (b + 1) / 2;
+                const float4v inner = *reinterpret_cast<const float4v*>(lds + L::kOffInner + (n & 1) * L::kInner + (b * 4 + wave) * 1024 + lane * 16);
+                const float f = d.in_chunk[query];
 #pragma unroll
-                for (int i = 0; i < b; i += 2)
-                    o = E::mul(v[i], v[i + 1 < kBlocks ? i + 1 : i], *reinterpret_cast<const typename E::Fine*>(sc + (p0 + i) * 1024),
-                               *reinterpret_cast<const typename E::Fine*>(sc + (p0 + i + 1) * 1024), o);
-                if (b % 2 == 0) o = E::mul(v[b], *reinterpret_cast<const typename E::Fine*>(sc + (p0 + b) * 1024), o);
-                out[b] = o;
+                for (int e = 0; e < 4; ++e) out[b][e] = fmaf(o[e], f, inner[e]);
             }
         }
-        typename E::Fine vd[kBlocks];
+        typename E::template Fine<L::kStateTerms> vd[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
-            vd[b] = E::fine(E::floats(v[b]) * *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]));
-        const float whole = d.whole[0];
-        if constexpr (kStates) total *= whole;
+            vd[b] = E::template fine<L::kStateTerms>(E::floats(v[b]) * *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]));
+        const float less = d.less[0];
+        if constexpr (kStates) total = fmaf(total, less, total);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float4v st = state[i] * whole;
+        for (int h = 0; h < 2; ++h) {
+            typename E::Raw k[2][kBlocks];
+            E::columns(tile, h, l16, g4, k);
 #pragma unroll
-            for (int b = 0; b < kBlocks; b += 2)
-                st = E::mul(E::column_piece(tile, 16 * b, 16 * i, l16, g4), E::column_piece(tile, 16 * (b + 1), 16 * i, l16, g4), vd[b], vd[b + 1], st);
-            state[i] = st;
+            for (int i = 0; i < 2; ++i) {
+                float4v st = state[2 * h + i] + state[2 * h + i] * less;
+#pragma unroll
+                for (int b = 0; b < kBlocks; b += 2) st = E::mul(k[i][b], k[i][b + 1], vd[b], vd[b + 1], st);
+                state[2 * h + i] = st;
+            }
         }
     }
 
@@ -407,9 +508,8 @@ struct Walk {
         const int token = chunk_token(n);
         const int left = s.len - token, tokens = left < kC ? left : kC;
         const int row = static_cast<int>(w.out_row);
-        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
-            w.out + (s.first + token) * w.out_row + static_cast<long long>(s.h) * (kHeadSize * kOutSize), 0,
-            (tokens - 1) * row + kHeadSize * kOutSize, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rows = descriptor(w.out + (s.first + token) * w.out_row + static_cast<long long>(s.h) * (kHeadSize * kOutSize),
+                                                       (tokens - 1) * row + kHeadSize * kOutSize);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const int r = 16 * b + l16, t = w.reverse ? kC - 1 - r : r;
@@ -456,7 +556,7 @@ struct Walk {
         float4v* to = reinterpret_cast<float4v*>(w.anchors) +
                       ((static_cast<long long>(s.b) * a.H + s.h) * blocks + (end - 1) / a.anchor_len) * (kHeadSize * kHeadSize / 4) + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i * kThreads] = state[i];
+        for (int i = 0; i < 4; ++i) to[i * 256] = state[i];
     }
 
     // kSums: the rows that the read-outs are multiplied with, in their layout
@@ -505,38 +605,61 @@ __device__ __forceinline__ int index_on_xcd() {
 // Index: unit outermost, then segment, then sweep.
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
 __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
-    using L = Layout<T, kC, kStates, kSums>;
+    using L = Layout<T, Out, kC, kStates, kSums>;
     extern __shared__ __align__(16) char lds[];
     int at = index_on_xcd();
-    const int sweep = at % a.sweeps;
+    const int sweep = uniform(at % a.sweeps);
     at /= a.sweeps;
-    const int unit = at / a.segs, seg = at - unit * a.segs;
-    const Sweep& w = a.sweep[sweep];
+    const int unit = uniform(at / a.segs), seg = uniform(at - unit * a.segs);
+    const Sweep w = uniform_sweep(a.sweep[sweep]);
     const Span s = span_of(a, unit, seg);
     if (seg >= s.segs) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = part % kWaves;
     const int chunks = s.end > s.begin ? (s.end - s.begin + kC - 1) / kC : 0;
-    Walk<T, Out, kC, kStates, kSums> walk{a, w, s, lds, lane, wave, lane & 15, lane >> 4, s.begin / kC, chunks, {}};
+    using W = Walk<T, Out, kC, kStates, kSums>;
+    W walk{a, w, s, lds, lane, wave, lane & 15, lane >> 4, s.begin / kC, chunks, {}};
+    // the segment that nothing follows on the walk hands nothing over
+    if (kStates && (chunks == 0 || seg == (w.reverse ? 0 : s.segs - 1))) return;
+
+    constexpr int kAhead = L::kStages - 1;
+    if (part >= kWaves) {                                       // producers
+        if (chunks == 0) return;
+        for (int n = 0; n <= kAhead; ++n) walk.ask_g(n);
+        for (int n = 0; n < kAhead && n < chunks; ++n) walk.ask_rows(n);
+        wait_loads<0>();
+        lds_barrier();
+        if (wave < 2 && wave < chunks) walk.form_decays(wave);
+        lds_barrier();
+        if constexpr (!kStates) walk.form_inner(0);
+        for (int n = 0; n < chunks; ++n) {
+            // all rows of chunk n + 1 are there, chunk n - 1 is done with, and what the last round formed can be read
+            lds_barrier();
+            const bool more = n + kAhead < chunks;
+            if (more) {
+                walk.ask_g(n + kAhead + 1);
+                walk.ask_rows(n + kAhead);
+            }
+            if constexpr (kSums)
+                if (n > 0 && wave == 1) walk.fold_sums(n - 1);
+            if (n + 2 < chunks && wave == 0) walk.form_decays(n + 2);
+            if constexpr (!kStates)
+                if (n + 1 < chunks) walk.form_inner(n + 1);
+            // rows of chunk n + 2; the younger ones stay on their way
+            if (more) wait_loads<L::kAsked * (L::kStages - 3)>();
+            else wait_loads<0>();
+        }
+        if constexpr (kSums) {
+            lds_barrier();
+            if (wave == 1) walk.fold_sums(chunks - 1);
+        }
+        return;
+    }
 
     const long long units = static_cast<long long>(a.B) * a.H;
     float* const locals = w.locals + unit * static_cast<long long>(kStateFloats);
     float* const totals = w.locals + a.segs * units * kStateFloats + unit;
-    if constexpr (kStates) {
-        // the segment that nothing follows on the walk hands nothing over
-        if (chunks == 0 || seg == (w.reverse ? 0 : s.segs - 1)) return;
-    }
-    if (chunks > 0) {
-        walk.ask_decays(0);
-        walk.ask_decays(1);
-        walk.ask_rows(0);
-        walk.ask_rows(1);
-        walk.ask_decays(2);
-        walk.ask_rows(2);
-        walk.ask_decays(3);
-    }
-    const float4v zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) walk.state[i] = zero;
+    for (int i = 0; i < 4; ++i) walk.state[i] = float4v{0.f, 0.f, 0.f, 0.f};
     if constexpr (!kStates) {
         if (w.state_in) walk.read_state(w.state_in + unit * static_cast<long long>(kStateFloats), w.turned, walk.state);
         // and what the segments in front of this one hand over, in the walk's order
@@ -551,41 +674,30 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
         }
     }
     if (chunks > 0) {
-        wait_loads<0>();
-        __syncthreads();
-        if (wave < 2 && wave < chunks) walk.form_decays(wave);
-        __syncthreads();
-        if constexpr (!kStates) walk.form_scores(0);
+        lds_barrier();
+        lds_barrier();
+        typename W::With with;
+        if constexpr (kSums) walk.ask_with(0, with);
         for (int n = 0; n < chunks; ++n) {
-            // every wave's rows of chunk n + 1 are there, chunk n - 1 is done with, and the scores and decays that the last round formed
-            // can be read
-            __syncthreads();
-            typename Walk<T, Out, kC, kStates, kSums>::With with;
-            if constexpr (kSums) {
-                if (n > 0 && wave == (n & 3)) walk.fold_sums(n - 1);
-                walk.ask_with(n, with);
-            }
-            walk.ask_rows(n + 3);
-            walk.ask_decays(n + 4);
-            if (n + 2 < chunks && wave == (n & 3)) walk.form_decays(n + 2);
+            lds_barrier();
             if constexpr (kStates) {
                 walk.advance(n, nullptr);
-                wait_loads<0>();
             } else {
+                typename W::With next;
+                if constexpr (kSums)
+                    if (n + 1 < chunks) walk.ask_with(n + 1, next);
                 if (w.anchors && w.reverse) walk.keep_anchor(n);
-                if (n + 1 < chunks) walk.form_scores(n + 1);
                 float4v out[L::kBlocks];
                 walk.advance(n, out);
-                wait_loads<0>();
                 walk.store(n, out);
-                if constexpr (kSums) walk.part_sums(n, out, with);
+                if constexpr (kSums) {
+                    walk.part_sums(n, out, with);
+                    with = next;
+                }
                 if (w.anchors && !w.reverse) walk.keep_anchor(n);
             }
         }
-        if constexpr (kSums) {
-            __syncthreads();
-            if (wave == (chunks & 3)) walk.fold_sums(chunks - 1);
-        }
+        if constexpr (kSums) lds_barrier();
     }
     if constexpr (kStates) {
         walk.write_state(locals + seg * units * kStateFloats, w.locals_turned, 1.f);
@@ -683,10 +795,10 @@ constexpr int kChunkBf16 = 64, kChunkF32 = 32;
 // f(kernel, LDS bytes) for the kernel of these rows
 template <bool kStates, bool kSums, typename F>
 hipError_t with_mix(bool f32_rows, bool f32_out, F f) {
-    if (f32_rows) return f(&mix_kernel<float, float, kChunkF32, kStates, kSums>, Layout<float, kChunkF32, kStates, kSums>::kLds);
+    if (f32_rows) return f(&mix_kernel<float, float, kChunkF32, kStates, kSums>, Layout<float, float, kChunkF32, kStates, kSums>::kLds);
     if constexpr (!kStates && !kSums)
-        if (f32_out) return f(&mix_kernel<Bf16, float, kChunkBf16, kStates, kSums>, Layout<Bf16, kChunkBf16, kStates, kSums>::kLds);
-    return f(&mix_kernel<Bf16, Bf16, kChunkBf16, kStates, kSums>, Layout<Bf16, kChunkBf16, kStates, kSums>::kLds);
+        if (f32_out) return f(&mix_kernel<Bf16, float, kChunkBf16, kStates, kSums>, Layout<Bf16, float, kChunkBf16, kStates, kSums>::kLds);
+    return f(&mix_kernel<Bf16, Bf16, kChunkBf16, kStates, kSums>, Layout<Bf16, Bf16, kChunkBf16, kStates, kSums>::kLds);
 }
 
 template <bool kStates, bool kSums>
