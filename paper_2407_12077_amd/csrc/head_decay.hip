@@ -207,7 +207,7 @@ constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smalle
 template <int kC>
 struct Decays {
     float pre[kC];                     // sum of g from the block's first token to this
-    float pre_key[kC];                 // the same of tokens that are there, +inf of others
+    float pre_key[kC];                 // the same of tokens that are there, far above nought of others
     float in_block[kC];                // exp2(pre)
     float to_block[kC];                // from behind this token to the block's end; nought for tokens that are not there
     float in_chunk[kC];                // from the chunk's first token to this
@@ -304,6 +304,20 @@ __device__ __forceinline__ Span span_of(const MixArgs& a, int unit, int seg) {
 __device__ __forceinline__ float decay_factor(float g) {
     g = g < kLowest ? kLowest : g;                              // (NaN stays)
     return __builtin_amdgcn_exp2f(g * kLog2e);
+}
+
+// 2^x for x <= 0, half a unit in the last place off where v_exp_f32 is a whole one: a head's decays are often the same for all tokens, and
+// so would be their error.  2^f by its series, |f| <= 1/2 (first dropped term 5e-9)
+__device__ __forceinline__ float exp2_near(float x) {
+    const float n = __builtin_rintf(x), f = x - n;
+    float q = 1.5252734e-5f;
+    q = fmaf(q, f, 1.5403530e-4f);
+    q = fmaf(q, f, 1.3333558e-3f);
+    q = fmaf(q, f, 9.6181291e-3f);
+    q = fmaf(q, f, 5.5504109e-2f);
+    q = fmaf(q, f, 2.4022651e-1f);
+    q = fmaf(q, f, 6.9314718e-1f);
+    return __builtin_amdgcn_ldexpf(fmaf(q, f, 1.f), static_cast<int>(n));
 }
 
 // Sum over the lanes of a row of sixteen up to this one
@@ -406,12 +420,12 @@ struct Walk {
         }
         if (lane < kC) {
             d.pre[lane] = pre;
-            d.pre_key[lane] = there ? pre : __builtin_inff();
-            d.in_block[lane] = __builtin_amdgcn_exp2f(pre);
-            d.to_block[lane] = there ? __builtin_amdgcn_exp2f(behind) : 0.f;
-            d.in_chunk[lane] = __builtin_amdgcn_exp2f(before + pre);
-            d.to_chunk[lane] = there ? __builtin_amdgcn_exp2f(behind + after) : 0.f;
-            if ((lane & 15) == 0) d.block[lane >> 4] = __builtin_amdgcn_exp2f(block);
+            d.pre_key[lane] = there ? pre : 32768.f;             // 2^-32768 is nought
+            d.in_block[lane] = exp2_near(pre);
+            d.to_block[lane] = there ? exp2_near(behind) : 0.f;
+            d.in_chunk[lane] = exp2_near(before + pre);
+            d.to_chunk[lane] = there ? exp2_near(behind + after) : 0.f;
+            if ((lane & 15) == 0) d.block[lane >> 4] = exp2_near(block);
             // S + (w - 1) S has one rounding of the size of S where w S has two: with a decay near one, and the same in every chunk, these
             // would add up over the chunks that the state remembers
             if (lane == 0) d.less[0] = expm1f(all * 0.6931471805599453f);
@@ -441,7 +455,7 @@ struct Walk {
                 const float pre = d.pre[query];
                 const float4v pk = *reinterpret_cast<const float4v*>(&d.pre_key[key]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[e] = key + e <= query ? sc[e] * __builtin_amdgcn_exp2f(pre - pk[e]) : 0.f;
+                for (int e = 0; e < 4; ++e) sc[e] = key + e <= query ? sc[e] * exp2_near(pre - pk[e]) : 0.f;
             } else {
                 sc *= *reinterpret_cast<const float4v*>(&d.to_block[key]) * f;
                 f *= d.block[kb];
@@ -495,10 +509,18 @@ struct Walk {
             E::columns(tile, h, l16, g4, k);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float4v st = state[2 * h + i] + state[2 * h + i] * less;
+                float4v& st = state[2 * h + i];
+                st += st * less;
+                if constexpr (E::kSize == 4) {
+                    // the chunk's own sum first: eight roundings of its size, and one of the state's, which is the larger with long memories
+                    float4v sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int b = 0; b < kBlocks; b += 2) st = E::mul(k[i][b], k[i][b + 1], vd[b], vd[b + 1], st);
-                state[2 * h + i] = st;
+                    for (int b = 0; b < kBlocks; b += 2) sum = E::mul(k[i][b], k[i][b + 1], vd[b], vd[b + 1], sum);
+                    st += sum;
+                } else {
+#pragma unroll
+                    for (int b = 0; b < kBlocks; b += 2) st = E::mul(k[i][b], k[i][b + 1], vd[b], vd[b + 1], st);
+                }
             }
         }
     }
