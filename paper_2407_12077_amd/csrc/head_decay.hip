@@ -14,14 +14,15 @@
 //     dr = mix(q = do, k = v, v = k; S_0 transposed)     dv = reversed mix(q = k, k = r, v = do)     dk = reversed mix(q = v, k = do, v = r)
 // and that of g_t is the sum of r.dr - k.dk from t to the end of any later block plus <dS, S> there: see decay_gradient_kernel.
 //
-// A workgroup takes one segment of one (sequence, head) and walks its chunks.  Its eight waves have two parts, one of each on a SIMD, so that
-// one's matrix products run beside the other's vector instructions and waits; they meet at one barrier a chunk:
-//   producers  bring the rows straight from memory into LDS, kStages - 1 chunks ahead, form the decays two chunks ahead, and one chunk ahead
-//              the part of the read-outs that needs no state: a producer takes 16 queries, P^T (keys x queries) from the rows of k and q as
-//              they lie, whose accumulators are, lane by lane, the operand of v^T P^T (v through transposing reads); so P never
-//              leaves the registers, and the sums go to the consumers through LDS
-//   consumers  own 16 of the 64 value columns each: the state's [64][16] columns stay in registers for the whole walk, and as accumulators
-//              of k^T (decayed v) they lie as S^T q^T wants them.  They store the read-outs
+// A workgroup takes one segment of one (sequence, head) and walks its chunks.  Its ten waves have three parts, so that one's matrix products
+// run beside another's vector instructions and waits; they meet at one barrier a chunk:
+//   movers     (2) bring the rows straight from memory into LDS, kStages - 1 chunks ahead, form the decays two chunks ahead, and store the
+//              read-outs of the chunk before in whole rows
+//   producers  (4) form, one chunk ahead, the part of the read-outs that needs no state: a producer takes 16 queries, P^T (keys x queries)
+//              from the rows of k and q as they lie, whose accumulators are, lane by lane, the operand of v^T P^T (v through transposing
+//              reads); so P never leaves the registers
+//   consumers  (4) own 16 of the 64 value columns each: the state's [64][16] columns stay in registers for the whole walk, and as accumulators
+//              of k^T (decayed v) they lie as S^T q^T wants them.  They add that to the producers' part, in its place in LDS
 //
 // bf16 rows: products of rows are exact in fp32; the computed operands (P, S, decayed v) enter as sums of three bf16, which hold an
 // fp32 value whole over its whole range, one product for each; two where only bf16 read-outs come of them.  fp32 rows: fp32 matrix instructions.
@@ -67,47 +68,15 @@ struct Elem<Bf16> {
         return *reinterpret_cast<const Raw*>(tile + at(row, 2 * q + (g4 >> 1)) + 8 * (g4 & 1));
     }
     // lanes are columns c0 + l16, contraction indices rows 16 b + 4 g4 ..: transposing reads, in which lane i of sixteen passes the
-    // address of four columns of row i / 4 and gets column i of the four rows.  Rows sixteen apart are permuted alike.
-    // (In assembly with their wait: in front of the builtin the compiler waits for all loads into LDS, the ones on their way to other places
-    // included.)
-    __device__ static __forceinline__ int column_at(int c0, int l16, int g4) {
+    // address of four columns of row i / 4 and gets column i of the four rows.  (A wave with loads into LDS on their way would wait for all
+    // of them here, wherever they go: the movers have no such reads.)
+    template <int kBlocks>
+    __device__ static __forceinline__ void column(const char* tile, int c0, int l16, int g4, Raw (&to)[kBlocks]) {
+        typedef short4v __attribute__((address_space(3))) * lds_ptr;
         const int row = 4 * g4 + (l16 >> 2), col = c0 + 4 * (l16 & 3);
-        return at(row, col >> 3) + 8 * (col >> 2 & 1);
-    }
-    __device__ static __forceinline__ void column(const char* tile, int c0, int l16, int g4, Raw (&to)[4]) {
-        typedef __attribute__((address_space(3))) const char* lds_ptr;
-#if defined(__HIP_DEVICE_COMPILE__)
-        const unsigned from = static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_ptr)tile)) + column_at(c0, l16, g4);
-        asm volatile(
-            "ds_read_b64_tr_b16 %0, %4\n"
-            "ds_read_b64_tr_b16 %1, %4 offset:2048\n"
-            "ds_read_b64_tr_b16 %2, %4 offset:4096\n"
-            "ds_read_b64_tr_b16 %3, %4 offset:6144\n"
-            "s_waitcnt lgkmcnt(0)"
-            : "=&v"(to[0]), "=&v"(to[1]), "=&v"(to[2]), "=&v"(to[3]) : "v"(from) : "memory");
-        __builtin_amdgcn_sched_barrier(0);
-#endif
-    }
-    // columns 32 i + l16 and those sixteen further
-    __device__ static __forceinline__ void columns(const char* tile, int i, int l16, int g4, Raw (&to)[2][4]) {
-        typedef __attribute__((address_space(3))) const char* lds_ptr;
-#if defined(__HIP_DEVICE_COMPILE__)
-        const unsigned base = static_cast<unsigned>(reinterpret_cast<unsigned long long>((lds_ptr)tile));
-        const unsigned p = base + column_at(32 * i, l16, g4), q = base + column_at(32 * i + 16, l16, g4);
-        asm volatile(
-            "ds_read_b64_tr_b16 %0, %8\n"
-            "ds_read_b64_tr_b16 %1, %8 offset:2048\n"
-            "ds_read_b64_tr_b16 %2, %8 offset:4096\n"
-            "ds_read_b64_tr_b16 %3, %8 offset:6144\n"
-            "ds_read_b64_tr_b16 %4, %9\n"
-            "ds_read_b64_tr_b16 %5, %9 offset:2048\n"
-            "ds_read_b64_tr_b16 %6, %9 offset:4096\n"
-            "ds_read_b64_tr_b16 %7, %9 offset:6144\n"
-            "s_waitcnt lgkmcnt(0)"
-            : "=&v"(to[0][0]), "=&v"(to[0][1]), "=&v"(to[0][2]), "=&v"(to[0][3]), "=&v"(to[1][0]), "=&v"(to[1][1]), "=&v"(to[1][2]),
-              "=&v"(to[1][3]) : "v"(p), "v"(q) : "memory");
-        __builtin_amdgcn_sched_barrier(0);
-#endif
+        const char* from = tile + at(row, col >> 3) + 8 * (col >> 2 & 1);      // (rows sixteen apart are permuted alike)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) to[b] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(from + 16 * b * kRow));
     }
     __device__ static __forceinline__ float4v floats(Raw r) {
         const uint2v u = __builtin_bit_cast(uint2v, r);
@@ -174,11 +143,6 @@ struct Elem<float> {
                 to[b][e] = *reinterpret_cast<const float*>(tile + at(row, col >> 2) + 4 * (col & 3));
             }
     }
-    template <int kBlocks>
-    __device__ static __forceinline__ void columns(const char* tile, int i, int l16, int g4, Raw (&to)[2][kBlocks]) {
-        column(tile, 32 * i, l16, g4, to[0]);
-        column(tile, 32 * i + 16, l16, g4, to[1]);
-    }
     __device__ static __forceinline__ float4v floats(Raw r) { return r; }
     template <int kTerms>
     __device__ static __forceinline__ float4v fine(float4v x) { return x; }
@@ -198,7 +162,7 @@ struct Elem<float> {
     }
 };
 
-constexpr int kWaves = 4, kThreads = 2 * 64 * kWaves;          // waves of either part
+constexpr int kWaves = 4, kMovers = 2, kThreads = 64 * (2 * kWaves + kMovers);      // consumers and producers; movers
 constexpr int kGPlaces = 8;            // places for a chunk's g, asked for a chunk earlier than the rows,
 constexpr int kDecayPlaces = 3;        // and for its decays: being formed, the producers', the consumers'
 constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
@@ -221,20 +185,21 @@ struct Layout {
     static constexpr int kTile = kC * Elem<T>::kRow;
     static constexpr int kTiles = kStates ? 2 : 3;               // k, v, q
     static constexpr int kStage = kTile * kTiles;
-    // places for a chunk's tiles: the consumers', the producers', and as many on their way as fit
-    static constexpr int kStages = kSums ? 4 : 5;
+    static constexpr int kStages = 4;                            // places for a chunk's tiles: the consumers', the producers', two on their way
     static constexpr int kBlocks = kC / 16;
     // terms of a bf16 operand that is no row.  What reaches fp32 results (states, gradients of decays, fp32 read-outs) keeps
     // all bits; for read-outs that are rounded to bf16, 2^-17 is far below that rounding
     static constexpr int kStateTerms = 3, kOutTerms = sizeof(Out) == 4 || kSums ? 3 : 2;
-    static constexpr int kInner = kStates ? 0 : kC * kHeadSize * 4;    // the producers' read-outs
+    static constexpr int kInner = kStates ? 0 : kC * kHeadSize * 4;    // a chunk's read-outs: being formed, completed, stored
     static constexpr int kOffG = kStages * kStage;
     static constexpr int kOffDecays = kOffG + kGPlaces * 256;
     static constexpr int kOffInner = kOffDecays + kDecayPlaces * static_cast<int>(sizeof(Decays<kC>));
-    static constexpr int kOffSums = kOffInner + 2 * kInner;      // [chunk parity][token][wave][g4]
-    static constexpr int kLds = kOffSums + (kSums ? 2 * kC * 64 : 0);
-    static constexpr int kLoads = kTile / 1024 / kWaves;         // of a producer, tile and chunk
+    static constexpr int kLds = kOffInner + 3 * kInner;
+    static constexpr int kLoads = kTile / 1024 / kMovers;        // of a mover, tile and chunk
     static constexpr int kAsked = kLoads * kTiles + 1;           // and g
+    // stores of read-outs: lanes a row, rows of a store, stores of a mover and chunk
+    static constexpr int kRowLanes = sizeof(Out) == 4 ? 16 : 8, kRowsAStore = 64 / kRowLanes, kStores = kC / kMovers / kRowsAStore;
+    static constexpr int kLeft = kStates ? 0 : kSums ? 2 * kStores : kStores;      // and of their sums
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
@@ -320,16 +285,16 @@ __device__ __forceinline__ float exp2_near(float x) {
     return __builtin_amdgcn_ldexpf(fmaf(q, f, 1.f), static_cast<int>(n));
 }
 
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {                 // (nought from lanes that are not there)
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
+}
 // Sum over the lanes of a row of sixteen up to this one
 __device__ __forceinline__ float prefix16(float v) {
-    auto shifted = [](float x, auto ctrl) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
-    };
-    v += shifted(v, std::integral_constant<int, 0x111>{});     // row_shr
-    v += shifted(v, std::integral_constant<int, 0x112>{});
-    v += shifted(v, std::integral_constant<int, 0x114>{});
-    v += shifted(v, std::integral_constant<int, 0x118>{});
-    return v;
+    v += dpp<0x111>(v);                                         // from one, two, four, eight lanes below
+    v += dpp<0x112>(v);
+    v += dpp<0x114>(v);
+    return v + dpp<0x118>(v);
 }
 
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
@@ -373,7 +338,7 @@ struct Walk {
         ask_tile(w.v, w.v_row, tokens, token, to + L::kTile);
         if constexpr (!kStates) ask_tile(w.q, w.q_row, tokens, token, to + 2 * L::kTile);
     }
-    // g by place (each producer's sixteen lanes of it, so that all have asked for as many loads).  In reverse a token's is that of
+    // g by place (each mover's half of it, so that both have asked for as many loads).  In reverse a token's is that of
     // the token behind it; places without one are cleared where they are read
     __device__ __forceinline__ void ask_g(int n) const {
         const int token = chunk_token(n < chunks ? n : chunks - 1);
@@ -381,12 +346,12 @@ struct Walk {
         int t = token + (w.reverse ? kC - lane : lane);
         t = t < 0 ? 0 : t < s.len ? t : s.len - 1;
         const float* from = a.g + (s.first + t) * a.g_row + s.h;
-        const bool mine = (lane >> 4) == wave;
-        if (mine)
+        if (lane >> 5 == wave)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                              (lds_ptr)(lds + L::kOffG + (n & (kGPlaces - 1)) * 256), 4, 0, 0);
     }
 
+    __device__ __forceinline__ char* inner_of(int n) const { return lds + L::kOffInner + n % 3 * L::kInner; }
     __device__ __forceinline__ char* rows_of(int n) const { return lds + n % L::kStages * L::kStage; }
     __device__ __forceinline__ Decays<kC>& decays(int n) const {
         return *reinterpret_cast<Decays<kC>*>(lds + L::kOffDecays + n % kDecayPlaces * static_cast<int>(sizeof(Decays<kC>)));
@@ -469,12 +434,12 @@ struct Walk {
 #pragma unroll
             for (int kb = 0; kb < kBlocks; kb += 2)
                 if (kb <= qb) acc[j] = E::mul(v[kb], v[kb + 1], p[kb], p[kb + 1], acc[j]);
-            *reinterpret_cast<float4v*>(lds + L::kOffInner + (n & 1) * L::kInner + (qb * 4 + j0 + j) * 1024 + lane * 16) = acc[j];
+            *reinterpret_cast<float4v*>(inner_of(n) + (qb * 4 + j0 + j) * 1024 + lane * 16) = acc[j];
         }
     }
 
-    // A consumer's read-outs of the chunk and the state behind it
-    __device__ __forceinline__ void advance(int n, float4v* out) {
+    // A consumer's part: the read-outs of the chunk and the state behind it
+    __device__ __forceinline__ void advance(int n) {
         const char* tile = rows_of(n);
         const Decays<kC>& d = decays(n);
         typename E::Raw v[kBlocks];
@@ -491,10 +456,8 @@ struct Walk {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
                     o = E::mul(st[2 * m], st[2 * m + 1], E::row_piece(q, query, 2 * m, g4), E::row_piece(q, query, 2 * m + 1, g4), o);
-                const float4v inner = *reinterpret_cast<const float4v*>(lds + L::kOffInner + (n & 1) * L::kInner + (b * 4 + wave) * 1024 + lane * 16);
-                const float f = d.in_chunk[query];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[b][e] = fmaf(o[e], f, inner[e]);
+                float4v& inner = *reinterpret_cast<float4v*>(inner_of(n) + (b * 4 + wave) * 1024 + lane * 16);
+                inner += o * d.in_chunk[query];
             }
         }
         typename E::template Fine<L::kStateTerms> vd[kBlocks];
@@ -504,43 +467,74 @@ struct Walk {
         const float less = d.less[0];
         if constexpr (kStates) total = fmaf(total, less, total);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            typename E::Raw k[2][kBlocks];
-            E::columns(tile, h, l16, g4, k);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float4v& st = state[2 * h + i];
+        for (int i = 0; i < 4; ++i) {
+                typename E::Raw k[kBlocks];
+                E::column(tile, 16 * i, l16, g4, k);
+                float4v& st = state[i];
                 st += st * less;
                 if constexpr (E::kSize == 4) {
                     // the chunk's own sum first: eight roundings of its size, and one of the state's, which is the larger with long memories
                     float4v sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int b = 0; b < kBlocks; b += 2) sum = E::mul(k[i][b], k[i][b + 1], vd[b], vd[b + 1], sum);
+                    for (int b = 0; b < kBlocks; b += 2) sum = E::mul(k[b], k[b + 1], vd[b], vd[b + 1], sum);
                     st += sum;
                 } else {
 #pragma unroll
-                    for (int b = 0; b < kBlocks; b += 2) st = E::mul(k[i][b], k[i][b + 1], vd[b], vd[b + 1], st);
+                    for (int b = 0; b < kBlocks; b += 2) st = E::mul(k[b], k[b + 1], vd[b], vd[b + 1], st);
                 }
-            }
         }
     }
 
-    __device__ __forceinline__ void store(int n, const float4v (&out)[kBlocks]) const {
+    // kSums: a mover's rows that the read-outs are multiplied with, laid out like its stores
+    typedef std::conditional_t<sizeof(Out) == 4, float4v, uint4v> With;
+    __device__ __forceinline__ void ask_with(int n, With (&to)[L::kStores]) const {
+        const int token = chunk_token(n), left = s.len - token, tokens = left < kC ? left : kC;
+        const char* rows = w.with + (s.first + token) * w.with_row + static_cast<long long>(s.h) * E::kRow + lane % L::kRowLanes * 16;
+#pragma unroll
+        for (int i = 0; i < L::kStores; ++i) {
+            const int r = (wave * L::kStores + i) * L::kRowsAStore + lane / L::kRowLanes;
+            int t = w.reverse ? kC - 1 - r : r;
+            t = t < tokens ? t : tokens - 1;
+            to[i] = *reinterpret_cast<const With*>(rows + t * w.with_row);
+        }
+    }
+
+    // A mover's half of the chunk's read-outs, in whole rows, and their sums.  Rows that are not there lie behind a descriptor's end: always
+    // the same number of stores.
+    __device__ __forceinline__ void store(int n, const With (&with)[L::kStores]) const {
         constexpr int kOutSize = sizeof(Out) == 4 ? 4 : 2;
         const int token = chunk_token(n);
         const int left = s.len - token, tokens = left < kC ? left : kC;
         const int row = static_cast<int>(w.out_row);
         const __amdgpu_buffer_rsrc_t rows = descriptor(w.out + (s.first + token) * w.out_row + static_cast<long long>(s.h) * (kHeadSize * kOutSize),
                                                        (tokens - 1) * row + kHeadSize * kOutSize);
+        const __amdgpu_buffer_rsrc_t sums = descriptor(reinterpret_cast<const char*>(w.sums + s.h * a.rows + s.first + token), kSums && w.with ? 4 * tokens : 0);
+        const int x = lane % L::kRowLanes;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const int r = 16 * b + l16, t = w.reverse ? kC - 1 - r : r;
-            // (a row that is not there lies behind the descriptor's end)
-            const int off = t < tokens ? t * row + (16 * wave + 4 * g4) * kOutSize : 0x7ffffff0;
+        for (int i = 0; i < L::kStores; ++i) {
+            const int r = (wave * L::kStores + i) * L::kRowsAStore + lane / L::kRowLanes, t = w.reverse ? kC - 1 - r : r;
+            const char* from = inner_of(n) + (r >> 4) * 4096 + (r & 15) * 16;         // (block of queries, of columns, four columns, query)
+            const int off = t < tokens ? t * row + 16 * x : 0x7ffffff0;
+            float sum;
             if constexpr (kOutSize == 4) {
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, out[b]), rows, off, 0, 0);
+                const float4v o = *reinterpret_cast<const float4v*>(from + x * 256);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, o), rows, off, 0, 0);
+                const float4v p = o * with[i];
+                sum = (p[0] + p[1]) + (p[2] + p[3]);
             } else {
-                __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uint2v, __builtin_convertvector(out[b], bf16x4)), rows, off, 0, 0);
+                const float4v o0 = *reinterpret_cast<const float4v*>(from + x * 512), o1 = *reinterpret_cast<const float4v*>(from + x * 512 + 256);
+                const bf16x8 o = __builtin_convertvector(__builtin_shufflevector(o0, o1, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, o), rows, off, 0, 0);
+                const float4v p = o0 * Elem<Bf16>::floats(__builtin_bit_cast(short4v, uint2v{with[i].x, with[i].y})) +
+                                  o1 * Elem<Bf16>::floats(__builtin_bit_cast(short4v, uint2v{with[i].z, with[i].w}));
+                sum = (p[0] + p[1]) + (p[2] + p[3]);
+            }
+            if constexpr (kSums) {
+                sum += dpp<0xB1>(sum);                          // over the row's lanes: neighbours, pairs, fours, eights
+                sum += dpp<0x4E>(sum);
+                sum += dpp<0x141>(sum);
+                if constexpr (L::kRowLanes == 16) sum += dpp<0x140>(sum);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, sum), sums, x == 0 && t < tokens ? 4 * t : 0x7ffffff0, 0, 0);
             }
         }
     }
@@ -580,40 +574,6 @@ struct Walk {
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i * 256] = state[i];
     }
-
-    // kSums: the rows that the read-outs are multiplied with, in their layout
-    typedef std::conditional_t<E::kSize == 4, uint4v, uint2v> WithPiece;
-    struct With {
-        WithPiece piece[kBlocks];
-    };
-    __device__ __forceinline__ void ask_with(int n, With& to) const {
-        if (!w.with) return;
-        const int token = chunk_token(n), left = s.len - token, tokens = left < kC ? left : kC;
-        const char* rows = w.with + (s.first + token) * w.with_row + static_cast<long long>(s.h) * E::kRow + (16 * wave + 4 * g4) * E::kSize;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const int r = 16 * b + l16;
-            int t = w.reverse ? kC - 1 - r : r;
-            t = t < tokens ? t : tokens - 1;
-            to.piece[b] = *reinterpret_cast<const WithPiece*>(rows + t * w.with_row);
-        }
-    }
-    __device__ __forceinline__ void part_sums(int n, const float4v (&out)[kBlocks], const With& with) const {
-        if (!w.with) return;
-        float* to = reinterpret_cast<float*>(lds + L::kOffSums + (n & 1) * (kC * 64));
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const float4v p = out[b] * E::floats(__builtin_bit_cast(typename E::Raw, with.piece[b]));
-            to[(16 * b + l16) * 16 + 4 * wave + g4] = (p[0] + p[1]) + (p[2] + p[3]);
-        }
-    }
-    __device__ __forceinline__ void fold_sums(int n) const {
-        if (!w.with || lane >= kC) return;
-        const float4v* part = reinterpret_cast<const float4v*>(lds + L::kOffSums + (n & 1) * (kC * 64) + lane * 64);
-        const float4v p = (part[0] + part[1]) + (part[2] + part[3]);
-        const int t = chunk_token(n) + (w.reverse ? kC - 1 - lane : lane);
-        if (t < s.len) w.sums[s.h * a.rows + s.first + t] = (p[0] + p[1]) + (p[2] + p[3]);
-    }
 };
 
 constexpr int kStateFloats = kHeadSize * kHeadSize;
@@ -643,36 +603,58 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
     // the segment that nothing follows on the walk hands nothing over
     if (kStates && (chunks == 0 || seg == (w.reverse ? 0 : s.segs - 1))) return;
 
-    constexpr int kAhead = L::kStages - 1;
-    if (part >= kWaves) {                                       // producers
+    if (part >= 2 * kWaves) {                                   // movers
         if (chunks == 0) return;
+        constexpr int kAhead = L::kStages - 1;
         for (int n = 0; n <= kAhead; ++n) walk.ask_g(n);
         for (int n = 0; n < kAhead && n < chunks; ++n) walk.ask_rows(n);
         wait_loads<0>();
         lds_barrier();
-        if (wave < 2 && wave < chunks) walk.form_decays(wave);
+        if (wave < chunks) walk.form_decays(wave);
         lds_barrier();
-        if constexpr (!kStates) walk.form_inner(0);
-        for (int n = 0; n < chunks; ++n) {
+        typename W::With with[2][L::kStores];
+        auto round = [&](int n, typename W::With(&asked)[L::kStores], typename W::With(&used)[L::kStores]) {
             // all rows of chunk n + 1 are there, chunk n - 1 is done with, and what the last round formed can be read
             lds_barrier();
+            if constexpr (kSums)
+                if (w.with) walk.ask_with(n, asked);
+            __builtin_amdgcn_sched_barrier(0);
             const bool more = n + kAhead < chunks;
             if (more) {
                 walk.ask_g(n + kAhead + 1);
                 walk.ask_rows(n + kAhead);
             }
-            if constexpr (kSums)
-                if (n > 0 && wave == 1) walk.fold_sums(n - 1);
-            if (n + 2 < chunks && wave == 0) walk.form_decays(n + 2);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (!kStates)
-                if (n + 1 < chunks) walk.form_inner(n + 1);
-            // rows of chunk n + 2; the younger ones stay on their way
-            if (more) wait_loads<L::kAsked * (L::kStages - 3)>();
-            else wait_loads<0>();
+                if (n > 0) walk.store(n - 1, used);
+            if (n + 2 < chunks && wave == 0) walk.form_decays(n + 2);
+            // rows of chunk n + 2, asked for a round ago: behind them that round's and this one's stores and this one's loads
+            if (!more) wait_loads<0>();
+            else if (n < 2) wait_loads<L::kAsked>();
+            else wait_loads<L::kAsked + 2 * L::kLeft>();
+        };
+        for (int n = 0; n < chunks; n += 2) {
+            round(n, with[0], with[1]);
+            if (n + 1 < chunks) round(n + 1, with[1], with[0]);
         }
-        if constexpr (kSums) {
+        if constexpr (!kStates) {
             lds_barrier();
-            if (wave == 1) walk.fold_sums(chunks - 1);
+            walk.store(chunks - 1, with[(chunks - 1) & 1]);
+        }
+        return;
+    }
+    if (part >= kWaves) {                                       // producers
+        if (kStates) {
+            for (int n = 0; n < chunks + 2; ++n) lds_barrier();
+        } else if (chunks > 0) {
+            lds_barrier();
+            lds_barrier();
+            walk.form_inner(0);
+            for (int n = 0; n < chunks; ++n) {
+                lds_barrier();
+                if (n + 1 < chunks) walk.form_inner(n + 1);
+            }
+            lds_barrier();
         }
         return;
     }
@@ -698,28 +680,13 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
     if (chunks > 0) {
         lds_barrier();
         lds_barrier();
-        typename W::With with;
-        if constexpr (kSums) walk.ask_with(0, with);
         for (int n = 0; n < chunks; ++n) {
             lds_barrier();
-            if constexpr (kStates) {
-                walk.advance(n, nullptr);
-            } else {
-                typename W::With next;
-                if constexpr (kSums)
-                    if (n + 1 < chunks) walk.ask_with(n + 1, next);
-                if (w.anchors && w.reverse) walk.keep_anchor(n);
-                float4v out[L::kBlocks];
-                walk.advance(n, out);
-                walk.store(n, out);
-                if constexpr (kSums) {
-                    walk.part_sums(n, out, with);
-                    with = next;
-                }
-                if (w.anchors && !w.reverse) walk.keep_anchor(n);
-            }
+            if (!kStates && w.anchors && w.reverse) walk.keep_anchor(n);
+            walk.advance(n);
+            if (!kStates && w.anchors && !w.reverse) walk.keep_anchor(n);
         }
-        if constexpr (kSums) lds_barrier();
+        if constexpr (!kStates) lds_barrier();
     }
     if constexpr (kStates) {
         walk.write_state(locals + seg * units * kStateFloats, w.locals_turned, 1.f);
