@@ -96,29 +96,23 @@ struct Elem<Bf16> {
     __device__ static __forceinline__ bf16x8 both(Raw a, Raw b) {
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+    template <int kTerms>
+    __device__ static __forceinline__ Raw term(const Fine<kTerms>& f, int i) { return f.term[i]; }
     // acc += A B over 32 contraction indices (two pieces)
-    template <int kTerms>
-    __device__ static __forceinline__ float4v mul(Raw a0, Raw a1, const Fine<kTerms>& b0, const Fine<kTerms>& b1, float4v acc) {
-#pragma unroll
-        for (int i = kTerms - 1; i >= 0; --i)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0.term[i], b1.term[i]), acc, 0, 0, 0);
-        return acc;
+    __device__ static __forceinline__ float4v mul(Raw a0, Raw a1, Raw b0, Raw b1, float4v acc) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0, a1), both(b0, b1), acc, 0, 0, 0);
     }
-    template <int kTerms>
-    __device__ static __forceinline__ float4v mul(const Fine<kTerms>& a0, const Fine<kTerms>& a1, Raw b0, Raw b1, float4v acc) {
+    // products of rows 16 i + l16 of one tile with a row of another
+    template <int kCount, int kSize>
+    __device__ static __forceinline__ void row_products(const char* ta, const char* tb, int row, int l16, int g4, float4v (&acc)[kSize]) {
 #pragma unroll
-        for (int i = kTerms - 1; i >= 0; --i)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both(a0.term[i], a1.term[i]), both(b0, b1), acc, 0, 0, 0);
-        return acc;
-    }
-    // rows a of one tile times rows b of another over all columns
-    __device__ static __forceinline__ float4v row_products(const char* ta, int ra, const char* tb, int rb, int g4) {
-        float4v acc = {0.f, 0.f, 0.f, 0.f};
+        for (int m = 0; m < 2; ++m) {
+            const bf16x8 b = *reinterpret_cast<const bf16x8*>(tb + at(row, 4 * m + g4));
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(ta + at(ra, 4 * m + g4)),
-                                                          *reinterpret_cast<const bf16x8*>(tb + at(rb, 4 * m + g4)), acc, 0, 0, 0);
-        return acc;
+            for (int i = 0; i < kCount; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(ta + at(16 * i + l16, 4 * m + g4)), b,
+                                                                 m == 0 ? float4v{0.f, 0.f, 0.f, 0.f} : acc[i], 0, 0, 0);
+        }
     }
 };
 
@@ -146,19 +140,24 @@ struct Elem<float> {
     __device__ static __forceinline__ float4v floats(Raw r) { return r; }
     template <int kTerms>
     __device__ static __forceinline__ float4v fine(float4v x) { return x; }
-    __device__ static __forceinline__ float4v mul(float4v a, float4v b, float4v acc) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], acc, 0, 0, 0);
-        return acc;
-    }
+    __device__ static __forceinline__ float4v term(float4v f, int) { return f; }
     __device__ static __forceinline__ float4v mul(float4v a0, float4v a1, float4v b0, float4v b1, float4v acc) {
-        return mul(a1, b1, mul(a0, b0, acc));
-    }
-    __device__ static __forceinline__ float4v row_products(const char* ta, int ra, const char* tb, int rb, int g4) {
-        float4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc = mul(row_piece(ta, ra, q, g4), row_piece(tb, rb, q, g4), acc);
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a0[e], b0[e], acc, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a1[e], b1[e], acc, 0, 0, 0);
         return acc;
+    }
+    template <int kCount, int kSize>
+    __device__ static __forceinline__ void row_products(const char* ta, const char* tb, int row, int l16, int g4, float4v (&acc)[kSize]) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) acc[i] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+            const float4v b0 = row_piece(tb, row, q, g4), b1 = row_piece(tb, row, q + 1, g4);
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) acc[i] = mul(row_piece(ta, 16 * i + l16, q, g4), row_piece(ta, 16 * i + l16, q + 1, g4), b0, b1, acc[i]);
+        }
     }
 };
 
@@ -189,7 +188,7 @@ struct Layout {
     static constexpr int kBlocks = kC / 16;
     // terms of a bf16 operand that is no row.  What reaches fp32 results (states, gradients of decays, fp32 read-outs) keeps
     // all bits; for read-outs that are rounded to bf16, 2^-17 is far below that rounding
-    static constexpr int kStateTerms = 3, kOutTerms = sizeof(Out) == 4 || kSums ? 3 : 2;
+    static constexpr int kStateTerms = Elem<T>::kSize == 4 ? 1 : 3, kOutTerms = Elem<T>::kSize == 4 ? 1 : sizeof(Out) == 4 || kSums ? 3 : 2;
     static constexpr int kInner = kStates ? 0 : kC * kHeadSize * 4;    // a chunk's read-outs: being formed, completed, stored
     static constexpr int kOffG = kStages * kStage;
     static constexpr int kOffDecays = kOffG + kGPlaces * 256;
@@ -203,11 +202,13 @@ struct Layout {
     static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
-__device__ __forceinline__ void lds_barrier() {                // all waves; loads and stores stay on their way
-    __builtin_amdgcn_sched_barrier(0);
+// All waves, and what they have written to LDS; loads and stores stay on their way (a fence would wait for loads into LDS).  The empty
+// statements keep the compiler from moving LDS accesses across, which the barrier alone does not.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);         // the wave's own LDS reads and writes
     __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
 }
 
 // A value that is the same in all lanes, in a scalar register: what depends on the kernel's argument or on memory through a computed
@@ -272,9 +273,8 @@ __device__ __forceinline__ float decay_factor(float g) {
 }
 
 // 2^x for x <= 0, half a unit in the last place off where v_exp_f32 is a whole one: a head's decays are often the same for all tokens, and
-// so would be their error.  2^f by its series, |f| <= 1/2 (first dropped term 5e-9)
-__device__ __forceinline__ float exp2_near(float x) {
-    const float n = __builtin_rintf(x), f = x - n;
+// so would be their error.  2^f - 1 by the series, |f| <= 1/2 (first dropped term 5e-9)
+__device__ __forceinline__ float exp2_less_1(float f) {
     float q = 1.5252734e-5f;
     q = fmaf(q, f, 1.5403530e-4f);
     q = fmaf(q, f, 1.3333558e-3f);
@@ -282,7 +282,11 @@ __device__ __forceinline__ float exp2_near(float x) {
     q = fmaf(q, f, 5.5504109e-2f);
     q = fmaf(q, f, 2.4022651e-1f);
     q = fmaf(q, f, 6.9314718e-1f);
-    return __builtin_amdgcn_ldexpf(fmaf(q, f, 1.f), static_cast<int>(n));
+    return q * f;
+}
+__device__ __forceinline__ float exp2_near(float x) {
+    const float n = __builtin_rintf(x);
+    return __builtin_amdgcn_ldexpf(1.f + exp2_less_1(x - n), static_cast<int>(n));
 }
 
 template <int kCtrl>
@@ -295,6 +299,16 @@ __device__ __forceinline__ float prefix16(float v) {
     v += dpp<0x112>(v);
     v += dpp<0x114>(v);
     return v + dpp<0x118>(v);
+}
+// and from it on
+__device__ __forceinline__ float suffix16(float v) {
+    v += dpp<0x101>(v);
+    v += dpp<0x102>(v);
+    v += dpp<0x104>(v);
+    return v + dpp<0x108>(v);
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
@@ -315,28 +329,49 @@ struct Walk {
     // token of the chunk's first place, by the chunk's number on the walk
     __device__ __forceinline__ int chunk_token(int n) const { return (first_chunk + (w.reverse ? chunks - 1 - n : n)) * kC; }
 
-    __device__ __forceinline__ void ask_tile(const char* base, long long row_bytes, int tokens, int token, int to) const {
-        // rows behind the sequence's last token are that token's again: their factors are nought
-        const long long first = s.first + token;
-        const int bytes = static_cast<int>((tokens - 1) * row_bytes) + E::kRow;
-        const __amdgpu_buffer_rsrc_t rows = descriptor(base + first * row_bytes + static_cast<long long>(s.h) * E::kRow, bytes);
-        typedef __attribute__((address_space(3))) char* lds_ptr;
+    // A mover's offsets in a chunk's rows: lanes take 16 bytes each, places permuted.  Rows behind the sequence's last token are
+    // that token's again: their factors are nought
+    __device__ __forceinline__ void offsets_in(int (&off)[L::kLoads], long long row_bytes, int tokens) const {
         constexpr int kRowsALoad = 1024 / E::kRow;
 #pragma unroll
         for (int i = 0; i < L::kLoads; ++i) {
             const int r = (wave * L::kLoads + i) * kRowsALoad + lane / E::kPlaces;
             int t = w.reverse ? kC - 1 - r : r;
             t = t < tokens ? t : tokens - 1;
-            const int off = t * static_cast<int>(row_bytes) + 16 * ((lane % E::kPlaces) ^ E::swizzle(r));
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(lds + to + (wave * L::kLoads + i) * 1024), 16, off, 0, 0, 0);
+            off[i] = t * static_cast<int>(row_bytes) + 16 * ((lane % E::kPlaces) ^ E::swizzle(r));
         }
     }
-    __device__ __forceinline__ void ask_rows(int n) const {
+    struct Offsets {                                            // of whole chunks
+        int k[L::kLoads], v[L::kLoads], q[L::kLoads];
+    };
+    __device__ __forceinline__ Offsets whole_offsets() const {
+        Offsets o;
+        offsets_in(o.k, w.k_row, kC);
+        offsets_in(o.v, w.v_row, kC);
+        if constexpr (!kStates) offsets_in(o.q, w.q_row, kC);
+        return o;
+    }
+    __device__ __forceinline__ void ask_tile(const char* base, long long row_bytes, int tokens, int token, int to, const int (&whole)[L::kLoads]) const {
+        const __amdgpu_buffer_rsrc_t rows = descriptor(base + (s.first + token) * row_bytes + static_cast<long long>(s.h) * E::kRow,
+                                                       static_cast<int>((tokens - 1) * row_bytes) + E::kRow);
+        typedef __attribute__((address_space(3))) char* lds_ptr;
+        char* dst = lds + to + wave * (L::kLoads * 1024);
+        if (tokens == kC) {
+#pragma unroll
+            for (int i = 0; i < L::kLoads; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(dst + 1024 * i), 16, whole[i], 0, 0, 0);
+        } else {
+            int off[L::kLoads];
+            offsets_in(off, row_bytes, tokens);
+#pragma unroll
+            for (int i = 0; i < L::kLoads; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_ptr)(dst + 1024 * i), 16, off[i], 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void ask_rows(int n, const Offsets& o) const {
         const int to = n % L::kStages * L::kStage;
         const int token = chunk_token(n), left = s.len - token, tokens = left < kC ? left : kC;
-        ask_tile(w.k, w.k_row, tokens, token, to);
-        ask_tile(w.v, w.v_row, tokens, token, to + L::kTile);
-        if constexpr (!kStates) ask_tile(w.q, w.q_row, tokens, token, to + 2 * L::kTile);
+        ask_tile(w.k, w.k_row, tokens, token, to, o.k);
+        ask_tile(w.v, w.v_row, tokens, token, to + L::kTile, o.v);
+        if constexpr (!kStates) ask_tile(w.q, w.q_row, tokens, token, to + 2 * L::kTile, o.q);
     }
     // g by place (each mover's half of it, so that both have asked for as many loads).  In reverse a token's is that of
     // the token behind it; places without one are cleared where they are read
@@ -368,19 +403,14 @@ struct Walk {
         const bool has = w.reverse ? t + 1 < s.len : there;
         g = g < kLowest ? kLowest : g;                          // (NaN stays)
         g = has ? g * kLog2e : 0.f;
-        const float pre = prefix16(g);
-        const float block = __shfl(pre, lane | 15);             // the block's sum
-        // behind this token: from the other end, so that nothing is subtracted
-        float behind = __shfl(g, (lane & 48) | (15 - (lane & 15)));
-        behind = prefix16(behind);
-        behind = __shfl(behind, (lane & 48) | ((14 - (lane & 15)) & 15));
-        behind = (lane & 15) == 15 ? 0.f : behind;
-        float before = 0.f, after = 0.f, all = 0.f;             // sums over the blocks in front of and behind this one
+        const float pre = prefix16(g), behind = dpp<0x101>(suffix16(g));        // (nothing is subtracted)
+        float block = 0.f, before = 0.f, after = 0.f, all = 0.f;               // sums over this block, those in front of it and behind it
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
-            const float sum = __shfl(block, 16 * i);
-            before += i < (lane >> 4) ? sum : 0.f;
-            after += i > (lane >> 4) ? sum : 0.f;
+            const float sum = lane_value(pre, 16 * i + 15);
+            block = i == lane >> 4 ? sum : block;
+            before += i < lane >> 4 ? sum : 0.f;
+            after += i > lane >> 4 ? sum : 0.f;
             all += sum;
         }
         if (lane < kC) {
@@ -393,49 +423,63 @@ struct Walk {
             if ((lane & 15) == 0) d.block[lane >> 4] = exp2_near(block);
             // S + (w - 1) S has one rounding of the size of S where w S has two: with a decay near one, and the same in every chunk, these
             // would add up over the chunks that the state remembers
-            if (lane == 0) d.less[0] = expm1f(all * 0.6931471805599453f);
+            if (lane == 0) d.less[0] = all > -0.5f ? exp2_less_1(all) : exp2_near(all) - 1.f;
         }
     }
 
-    // A producer's part of sum_{i <= t} P_ti v_i: 16 queries (with fewer blocks than producers, of a share of the columns)
+    // A producer's part of sum_{i <= t} P_ti v_i: 16 queries (with fewer blocks than producers, of a share of the columns).  Loops run over
+    // what does not depend on one another innermost, here and in advance: a product waits for the one before it in its sum
+    template <int kQ>
     __device__ __forceinline__ void form_inner(int n) const {
-        const int qb = wave % kBlocks, j0 = wave / kBlocks * kBlocks;        // blocks of 16
+        const int j0 = wave / kBlocks * kBlocks;                // block of columns
         const char* tile = rows_of(n);
         const Decays<kC>& d = decays(n);
-        const int query = 16 * qb + l16;
-        typename E::template Fine<L::kOutTerms> p[kBlocks];
-        float4v acc[kBlocks];
+        const int query = 16 * kQ + l16;
+        constexpr int kKeys = kQ + 1, kEven = (kKeys + 1) / 2 * 2;           // blocks of keys, in pairs
+        float4v sc[kEven];
+        E::template row_products<kKeys>(tile, tile + 2 * L::kTile, query, l16, g4, sc);
+        typename E::template Fine<L::kOutTerms> p[kEven];
+        float f = d.in_block[query];                            // from behind a block of keys to the query
 #pragma unroll
-        for (int j = 0; j < kBlocks; ++j) acc[j] = float4v{0.f, 0.f, 0.f, 0.f};
-        float f = d.in_block[query];                            // from behind block kb to the query
-#pragma unroll
-        for (int kb = kBlocks - 1; kb >= 0; --kb) {
-            if (kb > qb) {
-                p[kb] = {};
-                continue;
-            }
+        for (int kb = kQ; kb >= 0; --kb) {
             const int key = 16 * kb + 4 * g4;
-            float4v sc = E::row_products(tile, 16 * kb + l16, tile + 2 * L::kTile, query, g4);
-            if (kb == qb) {
+            if (kb == kQ) {
                 const float pre = d.pre[query];
                 const float4v pk = *reinterpret_cast<const float4v*>(&d.pre_key[key]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[e] = key + e <= query ? sc[e] * exp2_near(pre - pk[e]) : 0.f;
+                for (int e = 0; e < 4; ++e) sc[kb][e] = key + e <= query ? sc[kb][e] * exp2_near(pre - pk[e]) : 0.f;
             } else {
-                sc *= *reinterpret_cast<const float4v*>(&d.to_block[key]) * f;
+                sc[kb] *= *reinterpret_cast<const float4v*>(&d.to_block[key]) * f;
                 f *= d.block[kb];
             }
-            p[kb] = E::template fine<L::kOutTerms>(sc);
+            p[kb] = E::template fine<L::kOutTerms>(sc[kb]);
         }
+        if constexpr (kEven > kKeys) p[kKeys] = {};
+        typename E::Raw v[kBlocks][kEven];
+        float4v acc[kBlocks];
 #pragma unroll
         for (int j = 0; j < kBlocks; ++j) {
-            typename E::Raw v[kBlocks];
-            E::column(tile + L::kTile, 16 * (j0 + j), l16, g4, v);
-#pragma unroll
-            for (int kb = 0; kb < kBlocks; kb += 2)
-                if (kb <= qb) acc[j] = E::mul(v[kb], v[kb + 1], p[kb], p[kb + 1], acc[j]);
-            *reinterpret_cast<float4v*>(inner_of(n) + (qb * 4 + j0 + j) * 1024 + lane * 16) = acc[j];
+            E::column(tile + L::kTile, 16 * (j0 + j), l16, g4, v[j]);
+            acc[j] = float4v{0.f, 0.f, 0.f, 0.f};
         }
+#pragma unroll
+        for (int kb = 0; kb < kEven; kb += 2)
+#pragma unroll
+            for (int i = L::kOutTerms - 1; i >= 0; --i)
+#pragma unroll
+                for (int j = 0; j < kBlocks; ++j) acc[j] = E::mul(v[j][kb], v[j][kb + 1], E::term(p[kb], i), E::term(p[kb + 1], i), acc[j]);
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) *reinterpret_cast<float4v*>(inner_of(n) + (kQ * 4 + j0 + j) * 1024 + lane * 16) = acc[j];
+    }
+    template <int kQ>
+    __device__ __forceinline__ void produce() const {
+        lds_barrier();
+        lds_barrier();
+        for (int n = 0; n < chunks; ++n) {                      // in front of barrier n
+            form_inner<kQ>(n);
+            lds_barrier();
+        }
+        lds_barrier();
     }
 
     // A consumer's part: the read-outs of the chunk and the state behind it
@@ -445,19 +489,28 @@ struct Walk {
         typename E::Raw v[kBlocks];
         E::column(tile + L::kTile, 16 * wave, l16, g4, v);
         if constexpr (!kStates) {
+            const char* q = tile + 2 * L::kTile;
+            typename E::Raw row[kBlocks][4];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) row[b][m] = E::row_piece(q, 16 * b + l16, m, g4);
             typename E::template Fine<L::kOutTerms> st[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) st[i] = E::template fine<L::kOutTerms>(state[i]);
-            const char* q = tile + 2 * L::kTile;
+            float4v o[kBlocks];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) o[b] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int m = 0; m < 4; m += 2)
+#pragma unroll
+                for (int i = L::kOutTerms - 1; i >= 0; --i)
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) o[b] = E::mul(E::term(st[m], i), E::term(st[m + 1], i), row[b][m], row[b][m + 1], o[b]);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
-                const int query = 16 * b + l16;
-                float4v o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-                    o = E::mul(st[2 * m], st[2 * m + 1], E::row_piece(q, query, 2 * m, g4), E::row_piece(q, query, 2 * m + 1, g4), o);
                 float4v& inner = *reinterpret_cast<float4v*>(inner_of(n) + (b * 4 + wave) * 1024 + lane * 16);
-                inner += o * d.in_chunk[query];
+                inner += o[b] * d.in_chunk[16 * b + l16];
             }
         }
         typename E::template Fine<L::kStateTerms> vd[kBlocks];
@@ -466,22 +519,26 @@ struct Walk {
             vd[b] = E::template fine<L::kStateTerms>(E::floats(v[b]) * *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]));
         const float less = d.less[0];
         if constexpr (kStates) total = fmaf(total, less, total);
+        typename E::Raw k[4][kBlocks];
+        float4v sum[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-                typename E::Raw k[kBlocks];
-                E::column(tile, 16 * i, l16, g4, k);
-                float4v& st = state[i];
-                st += st * less;
-                if constexpr (E::kSize == 4) {
-                    // the chunk's own sum first: eight roundings of its size, and one of the state's, which is the larger with long memories
-                    float4v sum = {0.f, 0.f, 0.f, 0.f};
+            E::column(tile, 16 * i, l16, g4, k[i]);
+            state[i] += state[i] * less;
+            // fp32 rows: the chunk's own sum first, eight roundings of its size, and one of the state's, which is the larger with long memories
+            if constexpr (E::kSize == 4) sum[i] = float4v{0.f, 0.f, 0.f, 0.f};
+            else sum[i] = state[i];
+        }
 #pragma unroll
-                    for (int b = 0; b < kBlocks; b += 2) sum = E::mul(k[b], k[b + 1], vd[b], vd[b + 1], sum);
-                    st += sum;
-                } else {
+        for (int b = 0; b < kBlocks; b += 2)
 #pragma unroll
-                    for (int b = 0; b < kBlocks; b += 2) st = E::mul(k[b], k[b + 1], vd[b], vd[b + 1], st);
-                }
+            for (int t = L::kStateTerms - 1; t >= 0; --t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = E::mul(k[i][b], k[i][b + 1], E::term(vd[b], t), E::term(vd[b + 1], t), sum[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E::kSize == 4) state[i] += sum[i];
+            else state[i] = sum[i];
         }
     }
 
@@ -489,13 +546,14 @@ struct Walk {
     typedef std::conditional_t<sizeof(Out) == 4, float4v, uint4v> With;
     __device__ __forceinline__ void ask_with(int n, With (&to)[L::kStores]) const {
         const int token = chunk_token(n), left = s.len - token, tokens = left < kC ? left : kC;
-        const char* rows = w.with + (s.first + token) * w.with_row + static_cast<long long>(s.h) * E::kRow + lane % L::kRowLanes * 16;
+        const __amdgpu_buffer_rsrc_t rows = descriptor(w.with + (s.first + token) * w.with_row + static_cast<long long>(s.h) * E::kRow,
+                                                       static_cast<int>((tokens - 1) * w.with_row) + E::kRow);
 #pragma unroll
         for (int i = 0; i < L::kStores; ++i) {
             const int r = (wave * L::kStores + i) * L::kRowsAStore + lane / L::kRowLanes;
             int t = w.reverse ? kC - 1 - r : r;
             t = t < tokens ? t : tokens - 1;
-            to[i] = *reinterpret_cast<const With*>(rows + t * w.with_row);
+            to[i] = __builtin_bit_cast(With, __builtin_amdgcn_raw_buffer_load_b128(rows, t * static_cast<int>(w.with_row) + lane % L::kRowLanes * 16, 0, 0));
         }
     }
 
@@ -606,8 +664,9 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
     if (part >= 2 * kWaves) {                                   // movers
         if (chunks == 0) return;
         constexpr int kAhead = L::kStages - 1;
+        const typename W::Offsets offsets = walk.whole_offsets();
         for (int n = 0; n <= kAhead; ++n) walk.ask_g(n);
-        for (int n = 0; n < kAhead && n < chunks; ++n) walk.ask_rows(n);
+        for (int n = 0; n < kAhead && n < chunks; ++n) walk.ask_rows(n, offsets);
         wait_loads<0>();
         lds_barrier();
         if (wave < chunks) walk.form_decays(wave);
@@ -622,7 +681,7 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
             const bool more = n + kAhead < chunks;
             if (more) {
                 walk.ask_g(n + kAhead + 1);
-                walk.ask_rows(n + kAhead);
+                walk.ask_rows(n + kAhead, offsets);
             }
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (!kStates)
@@ -647,14 +706,13 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
         if (kStates) {
             for (int n = 0; n < chunks + 2; ++n) lds_barrier();
         } else if (chunks > 0) {
-            lds_barrier();
-            lds_barrier();
-            walk.form_inner(0);
-            for (int n = 0; n < chunks; ++n) {
-                lds_barrier();
-                if (n + 1 < chunks) walk.form_inner(n + 1);
+            const int q = wave % L::kBlocks;
+            if (q == 0) walk.template produce<0>();
+            else if (q == 1) walk.template produce<1>();
+            else if constexpr (L::kBlocks > 2) {
+                if (q == 2) walk.template produce<2>();
+                else walk.template produce<3>();
             }
-            lds_barrier();
         }
         return;
     }
