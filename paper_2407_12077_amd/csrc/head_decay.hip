@@ -14,10 +14,11 @@
 //     dr = mix(q = do, k = v, v = k; S_0 transposed)     dv = reversed mix(q = k, k = r, v = do)     dk = reversed mix(q = v, k = do, v = r)
 // and that of g_t is the sum of r.dr - k.dk from t to the end of any later block plus <dS, S> there: see decay_gradient_kernel.
 //
-// A workgroup takes one segment of one (sequence, head) and walks its chunks.  Its ten waves have three parts, so that one's matrix products
+// A workgroup takes one segment of one (sequence, head) and walks its chunks.  Its eleven waves have four parts, so that one's matrix products
 // run beside another's vector instructions and waits; they meet at one barrier a chunk:
-//   movers     (2) bring the rows straight from memory into LDS, kStages - 1 chunks ahead, form the decays two chunks ahead, and store the
-//              read-outs of the chunk before in whole rows
+//   movers     (2) bring the rows straight from memory into LDS, kStages - 1 chunks ahead, and store the read-outs of the chunk before in
+//              whole rows
+//   a timer    (1) forms the decays two chunks ahead
 //   producers  (4) form, one chunk ahead, the part of the read-outs that needs no state: a producer takes 16 queries, P^T (keys x queries)
 //              from the rows of k and q as they lie, whose accumulators are, lane by lane, the operand of v^T P^T (v through transposing
 //              reads); so P never leaves the registers
@@ -161,9 +162,8 @@ struct Elem<float> {
     }
 };
 
-constexpr int kWaves = 4, kMovers = 2, kThreads = 64 * (2 * kWaves + kMovers);      // consumers and producers; movers
-constexpr int kGPlaces = 8;            // places for a chunk's g, asked for a chunk earlier than the rows,
-constexpr int kDecayPlaces = 3;        // and for its decays: being formed, the producers', the consumers'
+constexpr int kWaves = 4, kMovers = 2, kThreads = 64 * (2 * kWaves + kMovers + 1);  // consumers, producers; movers; the timer
+constexpr int kDecayPlaces = 3;        // for a chunk's decays: being formed, the producers', the consumers'
 constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
 
 // A chunk's decays by token, in LDS.  In logarithms to base 2 (pre) or as factors (the others)
@@ -190,12 +190,11 @@ struct Layout {
     // all bits; for read-outs that are rounded to bf16, 2^-17 is far below that rounding
     static constexpr int kStateTerms = Elem<T>::kSize == 4 ? 1 : 3, kOutTerms = Elem<T>::kSize == 4 ? 1 : sizeof(Out) == 4 || kSums ? 3 : 2;
     static constexpr int kInner = kStates ? 0 : kC * kHeadSize * 4;    // a chunk's read-outs: being formed, completed, stored
-    static constexpr int kOffG = kStages * kStage;
-    static constexpr int kOffDecays = kOffG + kGPlaces * 256;
+    static constexpr int kOffDecays = kStages * kStage;
     static constexpr int kOffInner = kOffDecays + kDecayPlaces * static_cast<int>(sizeof(Decays<kC>));
     static constexpr int kLds = kOffInner + 3 * kInner;
-    static constexpr int kLoads = kTile / 1024 / kMovers;        // of a mover, tile and chunk
-    static constexpr int kAsked = kLoads * kTiles + 1;           // and g
+    static constexpr int kLoads = kTile / 1024 / kMovers;        // of a mover and tile,
+    static constexpr int kAsked = kLoads * kTiles;               // and chunk
     // stores of read-outs: lanes a row, rows of a store, stores of a mover and chunk
     static constexpr int kRowLanes = sizeof(Out) == 4 ? 16 : 8, kRowsAStore = 64 / kRowLanes, kStores = kC / kMovers / kRowsAStore;
     static constexpr int kLeft = kStates ? 0 : kSums ? 2 * kStores : kStores;      // and of their sums
@@ -373,17 +372,12 @@ struct Walk {
         ask_tile(w.v, w.v_row, tokens, token, to + L::kTile, o.v);
         if constexpr (!kStates) ask_tile(w.q, w.q_row, tokens, token, to + 2 * L::kTile, o.q);
     }
-    // g by place (each mover's half of it, so that both have asked for as many loads).  In reverse a token's is that of
-    // the token behind it; places without one are cleared where they are read
-    __device__ __forceinline__ void ask_g(int n) const {
+    // The timer's g, a lane a place.  In reverse a token's is that of the token behind it; places without one are cleared later
+    __device__ __forceinline__ float read_g(int n) const {
         const int token = chunk_token(n < chunks ? n : chunks - 1);
-        typedef __attribute__((address_space(3))) char* lds_ptr;
         int t = token + (w.reverse ? kC - lane : lane);
         t = t < 0 ? 0 : t < s.len ? t : s.len - 1;
-        const float* from = a.g + (s.first + t) * a.g_row + s.h;
-        if (lane >> 5 == wave)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                             (lds_ptr)(lds + L::kOffG + (n & (kGPlaces - 1)) * 256), 4, 0, 0);
+        return a.g[(s.first + t) * a.g_row + s.h];
     }
 
     __device__ __forceinline__ char* inner_of(int n) const { return lds + L::kOffInner + n % 3 * L::kInner; }
@@ -392,13 +386,10 @@ struct Walk {
         return *reinterpret_cast<Decays<kC>*>(lds + L::kOffDecays + n % kDecayPlaces * static_cast<int>(sizeof(Decays<kC>)));
     }
 
-    // the chunk's decays, by one wave, a lane a token
-    __device__ __forceinline__ void form_decays(int n) const {
+    // the chunk's decays from its g, a lane a token
+    __device__ __forceinline__ void form_decays(int n, float g) const {
         Decays<kC>& d = decays(n);
-        const int token = chunk_token(n);
-        const int at = lane < kC ? lane : 0;
-        const int t = token + (w.reverse ? kC - 1 - at : at);
-        float g = *reinterpret_cast<const float*>(lds + L::kOffG + (n & (kGPlaces - 1)) * 256 + 4 * at);
+        const int at = lane < kC ? lane : 0, t = chunk_token(n) + (w.reverse ? kC - 1 - at : at);
         const bool there = t < s.len;
         const bool has = w.reverse ? t + 1 < s.len : there;
         g = g < kLowest ? kLowest : g;                          // (NaN stays)
@@ -473,7 +464,6 @@ struct Walk {
     }
     template <int kQ>
     __device__ __forceinline__ void produce() const {
-        lds_barrier();
         lds_barrier();
         for (int n = 0; n < chunks; ++n) {                      // in front of barrier n
             form_inner<kQ>(n);
@@ -644,7 +634,7 @@ __device__ __forceinline__ int index_on_xcd() {
 
 // Index: unit outermost, then segment, then sweep.
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
-__global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))) void mix_kernel(const MixArgs a) {
     using L = Layout<T, Out, kC, kStates, kSums>;
     extern __shared__ __align__(16) char lds[];
     int at = index_on_xcd();
@@ -661,15 +651,28 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
     // the segment that nothing follows on the walk hands nothing over
     if (kStates && (chunks == 0 || seg == (w.reverse ? 0 : s.segs - 1))) return;
 
+    if (part == 2 * kWaves + kMovers) {                         // the timer
+        if (chunks == 0) return;
+        float g[4] = {walk.read_g(0), walk.read_g(1), walk.read_g(2), walk.read_g(3)};
+        walk.form_decays(0, g[0]);
+        if (chunks > 1) walk.form_decays(1, g[1]);
+        lds_barrier();
+        for (int n = 0; n < chunks; ++n) {
+            g[0] = g[2];
+            g[2] = g[3];
+            g[3] = walk.read_g(n + 4);
+            lds_barrier();
+            if (n + 2 < chunks) walk.form_decays(n + 2, g[0]);
+        }
+        if constexpr (!kStates) lds_barrier();
+        return;
+    }
     if (part >= 2 * kWaves) {                                   // movers
         if (chunks == 0) return;
         constexpr int kAhead = L::kStages - 1;
         const typename W::Offsets offsets = walk.whole_offsets();
-        for (int n = 0; n <= kAhead; ++n) walk.ask_g(n);
         for (int n = 0; n < kAhead && n < chunks; ++n) walk.ask_rows(n, offsets);
         wait_loads<0>();
-        lds_barrier();
-        if (wave < chunks) walk.form_decays(wave);
         lds_barrier();
         typename W::With with[2][L::kStores];
         auto round = [&](int n, typename W::With(&asked)[L::kStores], typename W::With(&used)[L::kStores]) {
@@ -679,14 +682,10 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
                 if (w.with) walk.ask_with(n, asked);
             __builtin_amdgcn_sched_barrier(0);
             const bool more = n + kAhead < chunks;
-            if (more) {
-                walk.ask_g(n + kAhead + 1);
-                walk.ask_rows(n + kAhead, offsets);
-            }
+            if (more) walk.ask_rows(n + kAhead, offsets);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (!kStates)
                 if (n > 0) walk.store(n - 1, used);
-            if (n + 2 < chunks && wave == 0) walk.form_decays(n + 2);
             // rows of chunk n + 2, asked for a round ago: behind them that round's and this one's stores and this one's loads
             if (!more) wait_loads<0>();
             else if (n < 2) wait_loads<L::kAsked>();
@@ -704,7 +703,7 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
     }
     if (part >= kWaves) {                                       // producers
         if (kStates) {
-            for (int n = 0; n < chunks + 2; ++n) lds_barrier();
+            for (int n = 0; n < chunks + 1; ++n) lds_barrier();
         } else if (chunks > 0) {
             const int q = wave % L::kBlocks;
             if (q == 0) walk.template produce<0>();
@@ -736,7 +735,6 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(const MixArgs a) {
         }
     }
     if (chunks > 0) {
-        lds_barrier();
         lds_barrier();
         for (int n = 0; n < chunks; ++n) {
             lds_barrier();

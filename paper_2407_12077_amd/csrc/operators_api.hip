@@ -49,7 +49,7 @@ bool space_of(int B, int T, int H, long long rows, bool backward, Space* s) {
     s->plan = wkv6::plan_mix(B, T, H, backward);
     const long long units = static_cast<long long>(B) * H;
     s->blocks = (T + s->plan.anchor_len - 1) / s->plan.anchor_len;
-    const long long most = 6710886;                            // workgroups of 640
+    const long long most = 6100805;                            // workgroups of 704
     if (units >= most || units * s->plan.segs * (backward ? 3 : 1) >= most || (backward && units * s->blocks >= most)) return false;
     if (s->plan.segs > 1) s->locals = s->plan.segs * units * (kStateFloats + 4);
     s->floats = s->locals;
