@@ -4,7 +4,7 @@
 //     dx = rstd (a - mean(a) - u mean(a u)),  a = gamma dy        dgamma = sum over rows of dy u        dbeta = sum over rows of dy
 //
 // Both are bound by memory: a row is read once, stays in registers between its sums and its results, and every value leaves once.  A
-// row's values lie eight to a lane over one wave (64 lanes, sums without LDS) or over a workgroup of four.
+// row's values lie eight to a lane over one wave (64 lanes, sums without LDS) or over a workgroup of four, or of eight.
 //
 // The sums over the rows: a workgroup takes every gridDim.x-th group of rows and a lane always the same columns, so its shares
 // of dgamma and dbeta stay in registers to the end; the waves' meet in LDS, the workgroups' in a second kernel that adds them in a
@@ -24,17 +24,29 @@ typedef unsigned uint4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float float8v __attribute__((ext_vector_type(8)));
 
-// eight values of a row
+// eight values of a row, as they lie in memory
+template <bool kF32>
+struct Raw8 {
+    std::conditional_t<kF32, float8v, uint4v> bits;
+    __device__ __forceinline__ void load(const void* p, long long item) {
+        if constexpr (kF32) {
+            const float4v* f = static_cast<const float4v*>(p) + 2 * item;
+            const float4v a = __builtin_nontemporal_load(f), b = __builtin_nontemporal_load(f + 1);
+            bits = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            bits = __builtin_nontemporal_load(static_cast<const uint4v*>(p) + item);
+        }
+    }
+    __device__ __forceinline__ float8v values() const {
+        if constexpr (kF32) return bits;
+        else return float8v{bf16_lo(bits.x), bf16_hi(bits.x), bf16_lo(bits.y), bf16_hi(bits.y), bf16_lo(bits.z), bf16_hi(bits.z), bf16_lo(bits.w), bf16_hi(bits.w)};
+    }
+};
 template <bool kF32>
 __device__ __forceinline__ float8v load8(const void* p, long long item) {
-    if constexpr (kF32) {
-        const float4v* f = static_cast<const float4v*>(p) + 2 * item;
-        const float4v a = __builtin_nontemporal_load(f), b = __builtin_nontemporal_load(f + 1);
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-        const uint4v u = __builtin_nontemporal_load(static_cast<const uint4v*>(p) + item);
-        return float8v{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y), bf16_lo(u.z), bf16_hi(u.z), bf16_lo(u.w), bf16_hi(u.w)};
-    }
+    Raw8<kF32> r;
+    r.load(p, item);
+    return r.values();
 }
 template <bool kF32>
 __device__ __forceinline__ void store8(void* p, long long item, float8v v) {
@@ -72,13 +84,17 @@ template <int kLanes, int kCount>
 __device__ __forceinline__ void row_sums(float (&v)[kCount], float (*place)[kCount]) {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) v[i] = wave_sum(v[i]);
-    if constexpr (kLanes == 256) {
+    if constexpr (kLanes > 64) {
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < kCount; ++i) place[threadIdx.x >> 6][i] = v[i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) v[i] = (place[0][i] + place[1][i]) + (place[2][i] + place[3][i]);
+        for (int i = 0; i < kCount; ++i) {
+            v[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kLanes / 64; w += 4) v[i] += (place[w][i] + place[w + 1][i]) + (place[w + 2][i] + place[w + 3][i]);
+        }
     }
 }
 
@@ -118,10 +134,10 @@ __global__ __launch_bounds__(256) void norm_kernel(long long M, int items, const
 }
 
 template <bool kXF32, bool kYF32, int kLanes, int kItems>
-__global__ __launch_bounds__(256) void norm_backward_kernel(long long M, int items, const void* x, const float2* stats, const float* gamma,
+__global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void norm_backward_kernel(long long M, int items, const void* x, const float2* stats, const float* gamma,
                                                             const void* dy, void* dx, float* partials) {
-    constexpr int kRows = 256 / kLanes;                        // of a workgroup at a time
-    __shared__ float place[2][4][2];
+    constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;     // of a workgroup at a time
+    __shared__ float place[2][kLanes < 256 ? 4 : kLanes / 64][2];
     __shared__ float8v meet[kRows > 1 ? 2 * 64 : 1];
     const int at = threadIdx.x % kLanes;
     float8v gm[kItems], dg[kItems], db[kItems];
@@ -132,19 +148,38 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(long long M, int ite
         dg[i] = db[i] = float8v{};
     }
     const float width = 1.f / static_cast<float>(8 * items);
-    int turn = 0;
-    for (long long row = static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / kLanes; row < M;
-         row += static_cast<long long>(gridDim.x) * kRows, turn ^= 1) {
+    // the next row of this lane's is on its way while one is worked on
+    Raw8<kXF32> x_raw[kItems] = {};
+    Raw8<kYF32> y_raw[kItems] = {};
+    float2 ms_next = make_float2(0.f, 0.f);
+    auto ask = [&](long long row) {
+        ms_next = stats[row];
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+            if (at + i * kLanes < items) {
+                x_raw[i].load(x, row * items + at + i * kLanes);
+                y_raw[i].load(dy, row * items + at + i * kLanes);
+            }
+    };
+    const long long step = static_cast<long long>(gridDim.x) * kRows;
+    long long row = static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / kLanes;
+    // (the widest fp32 rows leave no registers for it: 4096 x 16384 262 us with, 212 without; bf16 109 and 117)
+    constexpr bool kNext = kLanes < 512 || !kXF32 || !kYF32;
+    if (kNext && row < M) ask(row);
+    for (int turn = 0; row < M; row += step, turn ^= 1) {
+        if (!kNext) ask(row);
         const long long first = row * items;
-        const float2 ms = stats[row];
+        const float2 ms = ms_next;
         float8v u[kItems], a[kItems];
         float sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            const int item = at + i * kLanes;
-            const bool there = item < items;
-            u[i] = there ? (load8<kXF32>(x, first + item) - ms.x) * ms.y : float8v{};
-            a[i] = there ? load8<kYF32>(dy, first + item) : float8v{};
+            u[i] = (x_raw[i].values() - ms.x) * ms.y;
+            a[i] = y_raw[i].values();                          // (nought where there is nothing)
+        }
+        if (kNext && row + step < M) ask(row + step);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
             db[i] += a[i];
             dg[i] += a[i] * u[i];
             a[i] *= gm[i];
@@ -185,40 +220,52 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(long long M, int ite
     }
 }
 
-// 64 columns a workgroup; a thread adds every sixteenth row of four of them
+// Sixteen columns a workgroup: a thread adds every 64th row of four of them, eight asked for at a time.  (64 columns a workgroup and one row
+// at a time: 13 to 15 us, most of it waiting, where this takes 4.)
 __global__ __launch_bounds__(256) void norm_fold_kernel(int rows, int D, const float4v* partials, float4v* dgamma, float4v* dbeta) {
-    __shared__ float4v part[16][16];
-    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
-    const int column = blockIdx.x * 16 + lane, columns = D / 2;          // fours of dgamma, then of dbeta
+    __shared__ float4v part[64][4];
+    const int lane = threadIdx.x & 3, group = threadIdx.x >> 2;
+    const int column = blockIdx.x * 4 + lane, columns = D / 2;           // fours of dgamma, then of dbeta (D / 2 is a multiple of four)
     float4v sum = {0.f, 0.f, 0.f, 0.f};
-    if (column < columns)
-        for (int r = group; r < rows; r += 16) sum += partials[static_cast<long long>(r) * columns + column];
+    for (int r0 = group; r0 < rows; r0 += 512) {
+        float4v v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = r0 + 64 * i < rows ? partials[static_cast<long long>(r0 + 64 * i) * columns + column] : float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i];
+    }
     part[group][lane] = sum;
     __syncthreads();
-    if (group > 0 || column >= columns) return;
-#pragma unroll
-    for (int i = 1; i < 16; ++i) sum += part[i][lane];
-    if (column < D / 4) dgamma[column] = sum;
-    else dbeta[column - D / 4] = sum;
+    for (int half = 32; half > 0; half /= 2) {
+        if (group < half) part[group][lane] += part[group + half][lane];
+        __syncthreads();
+    }
+    if (group > 0) return;
+    if (column < D / 4) dgamma[column] = part[0][lane];
+    else dbeta[column - D / 4] = part[0][lane];
 }
 
-// Lanes of a row: one wave, or four where a wave would hold too much or would leave most of the card idle.
-bool wide_rows(long long M, int D, int most) { return D > most || (D >= 1024 && M <= 1024); }
-constexpr int kNormWave = 4096, kBackwardWave = 2048;          // widest rows of one wave
+// Lanes of a row of the forward pass: one wave, or four where a wave would hold too much or would leave most of the card idle.
+int norm_lanes(long long M, int D) { return D > 4096 || (D >= 1024 && M <= 1024) ? 256 : 64; }
+// Of the backward pass, which keeps a row, the next one, gamma and two sums for every column: 512 columns of bf16 rows a wave and more than that
+// several
+int norm_backward_lanes(long long M, int D, bool bf16) { return D > 8192 ? 512 : D > (bf16 ? 2048 : 1024) || (D >= 1024 && M <= 1024) ? 256 : 64; }
 
-// f(lanes, items of a lane) with the least that hold a row of up to kMost items a wave, or any in a workgroup
+// f(lanes, items of a lane), items of eight columns: the least of 1, 2, 4 and, up to kMost, 8 that hold a row
 template <int kMost, typename F>
-hipError_t with_width(bool wide, int items, F f) {
-    const int n = (items + (wide ? 255 : 63)) / (wide ? 256 : 64);
-    auto pick = [&](auto lanes) {
-        constexpr int kLanes = decltype(lanes)::value;
-        if (n <= 1) return f(lanes, std::integral_constant<int, 1>{});
-        if (n <= 2) return f(lanes, std::integral_constant<int, 2>{});
-        if constexpr (kLanes == 256 || kMost > 4)
-            if (n > 4) return f(lanes, std::integral_constant<int, 8>{});
-        return f(lanes, std::integral_constant<int, 4>{});
+hipError_t with_items(int lanes, int items, F f) {
+    const int n = (items + lanes - 1) / lanes;
+    auto pick = [&](auto l) {
+        if (n <= 1) return f(l, std::integral_constant<int, 1>{});
+        if (n <= 2) return f(l, std::integral_constant<int, 2>{});
+        if constexpr (kMost > 4)
+            if (n > 4) return f(l, std::integral_constant<int, 8>{});
+        return f(l, std::integral_constant<int, 4>{});
     };
-    return wide ? pick(std::integral_constant<int, 256>{}) : pick(std::integral_constant<int, 64>{});
+    if constexpr (kMost == 4)
+        if (lanes == 512) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
+    return lanes == 64 ? pick(std::integral_constant<int, 64>{}) : pick(std::integral_constant<int, 256>{});
 }
 // f(type of x, type of y)
 template <typename F>
@@ -231,10 +278,10 @@ hipError_t with_types(bool x_f32, bool y_f32, F f) {
 
 hipError_t launch_norm(long long M, int D, const void* x, const float* gamma, const float* beta, float eps, void* y, float* stats, bool x_f32,
                        bool y_f32, hipStream_t stream) {
-    const bool wide = wide_rows(M, D, kNormWave);
-    const unsigned grid = static_cast<unsigned>(wide ? M : (M + 3) / 4);
+    const int row_lanes = norm_lanes(M, D);
+    const unsigned grid = static_cast<unsigned>(row_lanes == 256 ? M : (M + 3) / 4);
     return with_types(x_f32, y_f32, [&](auto xf, auto yf) {
-        return with_width<kNormWave / 512>(wide, D / 8, [&](auto lanes, auto count) {
+        return with_items<8>(row_lanes, D / 8, [&](auto lanes, auto count) {
             hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_kernel<decltype(xf)::value, decltype(yf)::value, decltype(lanes)::value, decltype(count)::value>),
                                dim3(grid), dim3(256), 0, stream, M, D / 8, x, gamma, beta, eps, y, reinterpret_cast<float2*>(stats));
             return hipGetLastError();
@@ -242,21 +289,22 @@ hipError_t launch_norm(long long M, int D, const void* x, const float* gamma, co
     });
 }
 
-int norm_partials(long long M, int D) {
-    const int rows = wide_rows(M, D, kBackwardWave) ? 1 : 4;
+int norm_partials(long long M, int D, bool bf16) {
+    const int rows = norm_backward_lanes(M, D, bf16) == 64 ? 4 : 1;
     const long long most = (M + rows - 1) / rows;
     return static_cast<int>(most < 512 ? most : 512);
 }
 
 hipError_t launch_norm_backward(long long M, int D, const void* x, const float* stats, const float* gamma, const void* dy, void* dx,
                                 float* dgamma, float* dbeta, float* partials, bool x_f32, bool y_f32, hipStream_t stream) {
-    const bool wide = wide_rows(M, D, kBackwardWave);
-    const int grid = norm_partials(M, D);
+    const bool bf16 = !x_f32 && !y_f32;
+    const int row_lanes = norm_backward_lanes(M, D, bf16);
+    const int grid = norm_partials(M, D, bf16);
     if (grid > 0) {
         const hipError_t err = with_types(x_f32, y_f32, [&](auto xf, auto yf) {
-            return with_width<kBackwardWave / 512>(wide, D / 8, [&](auto lanes, auto count) {
+            return with_items<4>(row_lanes, D / 8, [&](auto lanes, auto count) {
                 hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_backward_kernel<decltype(xf)::value, decltype(yf)::value, decltype(lanes)::value, decltype(count)::value>),
-                                   dim3(grid), dim3(256), 0, stream, M, D / 8, x, reinterpret_cast<const float2*>(stats), gamma, dy, dx,
+                                   dim3(grid), dim3(row_lanes < 256 ? 256 : row_lanes), 0, stream, M, D / 8, x, reinterpret_cast<const float2*>(stats), gamma, dy, dx,
                                    dgamma ? partials : nullptr);
                 return hipGetLastError();
             });
@@ -264,7 +312,7 @@ hipError_t launch_norm_backward(long long M, int D, const void* x, const float* 
         if (err != hipSuccess) return err;
     }
     if (dgamma)
-        hipLaunchKernelGGL(norm_fold_kernel, dim3(static_cast<unsigned>((D / 2 + 15) / 16)), dim3(256), 0, stream, grid, D,
+        hipLaunchKernelGGL(norm_fold_kernel, dim3(static_cast<unsigned>(D / 8)), dim3(256), 0, stream, grid, D,
                            reinterpret_cast<const float4v*>(partials), reinterpret_cast<float4v*>(dgamma), reinterpret_cast<float4v*>(dbeta));
     return hipGetLastError();
 }

@@ -227,7 +227,8 @@ int wkv6_layernorm_forward(long long M, int D, const void* x, const float* gamma
 
 long long wkv6_layernorm_backward_workspace_bytes(long long M, int D) {
     if (D < 8 || D % 8 != 0 || D > wkv6::kNormMaxWidth || M < 0 || M >= 1ll << 24) return -1;
-    return 8ll * D * wkv6::norm_partials(M, D);
+    const int bf16 = wkv6::norm_partials(M, D, true), other = wkv6::norm_partials(M, D, false);
+    return 8ll * D * (bf16 > other ? bf16 : other);
 }
 
 int wkv6_layernorm_backward(long long M, int D, const void* x, const float* mean_rstd, const float* gamma, const void* dy, void* dx,
