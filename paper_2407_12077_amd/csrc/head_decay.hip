@@ -62,7 +62,8 @@ struct Elem<Bf16> {
     struct Fine {
         short4v term[kTerms];
     };
-    __device__ static __forceinline__ int swizzle(int row) { return row >> 1 & 7; }
+    // reads of a place of sixteen rows, and of 32 bytes of every other one of eight, take all banks
+    __device__ static __forceinline__ int swizzle(int row) { return (row & 6) | (row >> 3 & 1); }
     __device__ static __forceinline__ int at(int row, int place) { return row * kRow + 16 * (place ^ swizzle(row)); }
     // lanes are rows, contraction indices columns 16 q + 4 g4 ..
     __device__ static __forceinline__ Raw row_piece(const char* tile, int row, int q, int g4) {
@@ -382,6 +383,12 @@ struct Walk {
     }
 
     __device__ __forceinline__ char* inner_of(int n) const { return lds + L::kOffInner + n % 3 * L::kInner; }
+    // a lane's four of 16 queries x 16 columns: query l16, columns 4 g4 ..  The queries of a group of columns are permuted by the group, so that
+    // whole rows (a lane a group) take all banks too
+    __device__ __forceinline__ static int inner_place(int columns, int g, int query) { return columns * 1024 + g * 256 + ((query ^ (4 * columns + g)) & 15) * 16; }
+    __device__ __forceinline__ float4v* inner_at(int n, int queries, int columns) const {
+        return reinterpret_cast<float4v*>(inner_of(n) + queries * 4096 + inner_place(columns, g4, l16));
+    }
     __device__ __forceinline__ char* rows_of(int n) const { return lds + n % L::kStages * L::kStage; }
     __device__ __forceinline__ Decays<kC>& decays(int n) const {
         return *reinterpret_cast<Decays<kC>*>(lds + L::kOffDecays + n % kDecayPlaces * static_cast<int>(sizeof(Decays<kC>)));
@@ -461,7 +468,7 @@ struct Walk {
 #pragma unroll
                 for (int j = 0; j < kBlocks; ++j) acc[j] = E::mul(v[j][kb], v[j][kb + 1], E::term(p[kb], i), E::term(p[kb + 1], i), acc[j]);
 #pragma unroll
-        for (int j = 0; j < kBlocks; ++j) *reinterpret_cast<float4v*>(inner_of(n) + (kQ * 4 + j0 + j) * 1024 + lane * 16) = acc[j];
+        for (int j = 0; j < kBlocks; ++j) *inner_at(n, kQ, j0 + j) = acc[j];
     }
     template <int kQ>
     __device__ __forceinline__ void produce() const {
@@ -477,19 +484,27 @@ struct Walk {
     __device__ __forceinline__ void advance(int n) {
         const char* tile = rows_of(n);
         const Decays<kC>& d = decays(n);
-        typename E::Raw v[kBlocks];
-        E::column(tile + L::kTile, 16 * wave, l16, g4, v);
+        // everything is asked for well before it is waited for
+        typename E::Raw v[kBlocks], k[4][kBlocks];
+        float4v to_chunk[kBlocks], inner[kBlocks], o[kBlocks];
+        float in_chunk[kBlocks];
+        typename E::Raw row[kBlocks][4];
         if constexpr (!kStates) {
             const char* q = tile + 2 * L::kTile;
-            typename E::Raw row[kBlocks][4];
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int m = 0; m < 4; ++m) row[b][m] = E::row_piece(q, 16 * b + l16, m, g4);
+        }
+        E::column(tile + L::kTile, 16 * wave, l16, g4, v);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) to_chunk[b] = *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]);
+        const float less = d.less[0];
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kStates) {
             typename E::template Fine<L::kOutTerms> st[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) st[i] = E::template fine<L::kOutTerms>(state[i]);
-            float4v o[kBlocks];
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) o[b] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -500,21 +515,25 @@ struct Walk {
                     for (int b = 0; b < kBlocks; ++b) o[b] = E::mul(E::term(st[m], i), E::term(st[m + 1], i), row[b][m], row[b][m + 1], o[b]);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
-                float4v& inner = *reinterpret_cast<float4v*>(inner_of(n) + (b * 4 + wave) * 1024 + lane * 16);
-                inner += o[b] * d.in_chunk[16 * b + l16];
+                inner[b] = *inner_at(n, b, wave);
+                in_chunk[b] = d.in_chunk[16 * b + l16];
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) E::column(tile, 16 * i, l16, g4, k[i]);
+        __builtin_amdgcn_sched_barrier(0);
         typename E::template Fine<L::kStateTerms> vd[kBlocks];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-            vd[b] = E::template fine<L::kStateTerms>(E::floats(v[b]) * *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]));
-        const float less = d.less[0];
+        for (int b = 0; b < kBlocks; ++b) vd[b] = E::template fine<L::kStateTerms>(E::floats(v[b]) * to_chunk[b]);
         if constexpr (kStates) total = fmaf(total, less, total);
-        typename E::Raw k[4][kBlocks];
+        if constexpr (!kStates) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                *inner_at(n, b, wave) = inner[b] + o[b] * in_chunk[b];
+        }
         float4v sum[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            E::column(tile, 16 * i, l16, g4, k[i]);
             state[i] += state[i] * less;
             // fp32 rows: the chunk's own sum first, eight roundings of its size, and one of the state's, which is the larger with long memories
             if constexpr (E::kSize == 4) sum[i] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -562,16 +581,17 @@ struct Walk {
 #pragma unroll
         for (int i = 0; i < L::kStores; ++i) {
             const int r = (wave * L::kStores + i) * L::kRowsAStore + lane / L::kRowLanes, t = w.reverse ? kC - 1 - r : r;
-            const char* from = inner_of(n) + (r >> 4) * 4096 + (r & 15) * 16;         // (block of queries, of columns, four columns, query)
+            const char* from = inner_of(n) + (r >> 4) * 4096;
             const int off = t < tokens ? t * row + 16 * x : 0x7ffffff0;
             float sum;
             if constexpr (kOutSize == 4) {
-                const float4v o = *reinterpret_cast<const float4v*>(from + x * 256);
+                const float4v o = *reinterpret_cast<const float4v*>(from + inner_place(x >> 2, x & 3, r & 15));
                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, o), rows, off, 0, kStreamed);
                 const float4v p = o * with[i];
                 sum = (p[0] + p[1]) + (p[2] + p[3]);
             } else {
-                const float4v o0 = *reinterpret_cast<const float4v*>(from + x * 512), o1 = *reinterpret_cast<const float4v*>(from + x * 512 + 256);
+                const float4v o0 = *reinterpret_cast<const float4v*>(from + inner_place(x >> 1, x % 2 * 2, r & 15));
+                const float4v o1 = *reinterpret_cast<const float4v*>(from + inner_place(x >> 1, x % 2 * 2 + 1, r & 15));
                 const bf16x8 o = __builtin_convertvector(__builtin_shufflevector(o0, o1, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, o), rows, off, 0, kStreamed);
                 const float4v p = o0 * Elem<Bf16>::floats(__builtin_bit_cast(short4v, uint2v{with[i].x, with[i].y})) +
@@ -728,13 +748,21 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
         if (w.state_in) walk.read_state(w.state_in + unit * static_cast<long long>(kStateFloats), w.turned, walk.state);
         // and what the segments in front of this one hand over, in the walk's order
         const int count = w.reverse ? s.segs - 1 - seg : seg;
-        for (int x = 0; x < count; ++x) {
-            const int other = w.reverse ? s.segs - 1 - x : x;
-            float4v add[4];
-            walk.read_state(locals + other * units * kStateFloats, w.locals_turned, add);
-            const float decay = totals[other * units];
+        constexpr int kAtOnce = 4;                              // asked for together
+        for (int x0 = 0; x0 < count; x0 += kAtOnce) {
+            float4v add[kAtOnce][4];
+            float decay[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) walk.state[i] = walk.state[i] * decay + add[i];
+            for (int x = 0; x < kAtOnce; ++x) {
+                const int from = x0 + x < count ? x0 + x : count - 1, other = w.reverse ? s.segs - 1 - from : from;
+                walk.read_state(locals + other * units * kStateFloats, w.locals_turned, add[x]);
+                decay[x] = totals[other * units];
+            }
+#pragma unroll
+            for (int x = 0; x < kAtOnce; ++x)
+                if (x0 + x < count)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) walk.state[i] = walk.state[i] * decay[x] + add[x][i];
         }
     }
     if (chunks > 0) {
