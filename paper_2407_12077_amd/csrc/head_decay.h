@@ -7,6 +7,7 @@
 namespace wkv6 {
 
 constexpr int kMixBlock = 64;          // segments and anchors are whole multiples of this many tokens
+constexpr int kMixThreads = 704;       // of a workgroup
 
 // One product of the mix, o_t = sum_{i <= t} exp(g_{i+1} + .. + g_t) (q_t . k_i) v_i + exp(g_1 + .. + g_t) q_t S_0, with the state
 // S[key][value] behind it.  Rows have kHeadSize values a head; strides in bytes from token to token.
@@ -43,11 +44,11 @@ struct MixArgs {
     Sweep sweep[3];
 };
 
-// How the token axis is cut: segs segments of seg_len tokens, anchors every anchor_len (a divisor of seg_len).
+// How the token axis is cut: segs segments of seg_len tokens; anchors every anchor_len tokens.  Multiples of kMixBlock.
 struct MixPlan {
     int segs, seg_len, anchor_len;
 };
-MixPlan plan_mix(int B, int T, int H, bool backward);
+MixPlan plan_mix(int B, int T, int H, bool backward, bool f32_rows);
 
 hipError_t launch_mix(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t stream);
 

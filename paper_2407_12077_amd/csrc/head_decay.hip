@@ -31,6 +31,7 @@
 #include "wkv6_lds_loads.h"
 #include "wkv6_math.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace wkv6 {
@@ -164,6 +165,7 @@ struct Elem<float> {
 };
 
 constexpr int kWaves = 4, kMovers = 2, kThreads = 64 * (2 * kWaves + kMovers + 1);  // consumers, producers; movers; the timer
+static_assert(kThreads == kMixThreads, "the launch");
 constexpr int kDecayPlaces = 3;        // for a chunk's decays: being formed, the producers', the consumers'
 constexpr int kStreamed = 2;             // cache policy of the read-outs, non-temporal: prefill 8 x 4096 x 32 117.7 -> 115.6 us, its gradients 390 -> 384
 constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
@@ -261,7 +263,7 @@ __device__ __forceinline__ Span span_of(const MixArgs& a, int unit, int seg) {
         s.len = a.T;
     }
     s.seg = seg;
-    s.segs = s.len > 0 ? (s.len + a.seg_len - 1) / a.seg_len : 1;
+    s.segs = s.len > 0 ? (s.len - 1) / a.seg_len + 1 : 1;
     s.begin = seg * a.seg_len;
     s.end = s.begin + a.seg_len < s.len ? s.begin + a.seg_len : s.len;
     return s;
@@ -637,7 +639,7 @@ struct Walk {
     __device__ __forceinline__ void keep_anchor(int n) const {
         const int end = chunk_token(n) + kC;
         if (end % a.anchor_len != 0 && end < s.len) return;
-        const int blocks = (a.T + a.anchor_len - 1) / a.anchor_len;
+        const int blocks = (a.T - 1) / a.anchor_len + 1;
         float4v* to = reinterpret_cast<float4v*>(w.anchors) +
                       ((static_cast<long long>(s.b) * a.H + s.h) * blocks + (end - 1) / a.anchor_len) * (kHeadSize * kHeadSize / 4) + threadIdx.x;
 #pragma unroll
@@ -888,22 +890,39 @@ hipError_t launch(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t str
 
 }  // namespace
 
-MixPlan plan_mix(int B, int T, int H, bool backward) {
-    const long long units = static_cast<long long>(B) * H * (backward ? 3 : 1);
-    MixPlan p;
-    p.segs = 1;
-    if (units < 256) {
-        long long segs = 512 / units;
-        const long long most = T / 256;
-        if (segs > most) segs = most;
-        if (segs > 32) segs = 32;
-        if (segs > 1) p.segs = static_cast<int>(segs);
+namespace {
+
+// What a call takes in `segs` segments, in microseconds, from what a walk takes for 64 tokens and what memory takes: a compute unit holds one workgroup of
+// a walk with read-outs, two of one for the states alone.
+double modelled(double units, double tokens, int segs, bool backward, bool f32_rows) {
+    const double each = std::ceil(tokens / segs / kMixBlock), walks = units * (backward ? 3 : 1) * segs, load = walks < 256. ? walks / 256. : 1.;
+    const double per = f32_rows ? (backward ? 4.6 : 4.3) + 1.2 * load : (backward ? 1.6 : 1.4) + 0.6 * load;
+    const double stream = units * tokens * (f32_rows ? 256. : 128.) / 4.5e6;         // one read or write of all rows
+    const double whole = std::fmax(std::ceil(walks / 256.) * (5.5 + each * per), (backward ? 11. : 4.) * stream);
+    if (segs == 1) return whole;
+    const double states = std::ceil(units * (backward ? 2 : 1) * (segs - 1) / 512.) * each * (f32_rows ? 2. : 0.72);
+    return whole + 4. + 0.2 * segs + std::fmax(states, (backward ? 4. : 2.) * stream * (segs - 1) / segs);
+}
+
+}  // namespace
+
+MixPlan plan_mix(int B, int T, int H, bool backward, bool f32_rows) {
+    const double units = static_cast<double>(B) * H, tokens = T > 0 ? T : 1;
+    int segs = 1;
+    // pieces are for calls that would leave compute units idle; they read k and v (and r and dout) twice
+    if (units < 256.) {
+        double least = 0.93 * modelled(units, tokens, 1, backward, f32_rows);
+        for (int n = 2; n <= 32 && n * kMixBlock < T + kMixBlock; ++n) {
+            const double us = modelled(units, tokens, n, backward, f32_rows);
+            if (us < least) least = us, segs = n;
+        }
     }
-    const long long step = T > 1024LL * p.segs ? 1024 : kMixBlock;
-    const long long each = (static_cast<long long>(T > 0 ? T : 1) + p.segs - 1) / p.segs;
-    p.seg_len = static_cast<int>((each + step - 1) / step * step);
-    p.segs = T > 0 ? (T + p.seg_len - 1) / p.seg_len : 1;
-    p.anchor_len = p.seg_len > 1024 ? 1024 : p.seg_len;
+    MixPlan p;
+    const long long each = (static_cast<long long>(tokens) + segs - 1) / segs;
+    p.seg_len = static_cast<int>((each + kMixBlock - 1) / kMixBlock * kMixBlock);
+    p.segs = T > 0 ? (T - 1) / p.seg_len + 1 : 1;
+    const int longest = T > 0 ? (T - 1) / kMixBlock * kMixBlock + kMixBlock : kMixBlock;
+    p.anchor_len = longest < 1024 ? longest : 1024;
     return p;
 }
 
@@ -934,7 +953,7 @@ hipError_t launch_mix_locals(const MixArgs& a, int count, bool f32_rows, hipStre
 
 hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const float* k_sums, const float* behind, const float* front,
                                  float* head_sums, float* dg, hipStream_t stream) {
-    const int blocks = (a.T + a.anchor_len - 1) / a.anchor_len;
+    const int blocks = a.T > 0 ? (a.T - 1) / a.anchor_len + 1 : 0;
     const long long count = static_cast<long long>(a.B) * blocks;
     if (count > 0)
         hipLaunchKernelGGL(decay_gradient_kernel, dim3(static_cast<unsigned>(count * a.H)), dim3(256), 0, stream, a, blocks, r_sums, k_sums,

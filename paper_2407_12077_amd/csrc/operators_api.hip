@@ -39,18 +39,19 @@ int check_strides(int H, long long token_stride, long long g_stride, int dtype) 
     return token_stride % (dtype == WKV6_DTYPE_F32 ? 4 : 8) != 0 ? WKV6_ERR_ALIGN : WKV6_OK;
 }
 
-// Workspace in floats, every part a multiple of four; 0 where none is needed, -1 where the launches would not fit.
+// Workspace in floats, every part a multiple of four; false where the launches would not fit.
 struct Space {
     wkv6::MixPlan plan;
     long long blocks = 0, locals = 0, sums = 0, anchors = 0, head_sums = 0, floats = 0;
 };
 long long four(long long n) { return (n + 3) / 4 * 4; }
-bool space_of(int B, int T, int H, long long rows, bool backward, Space* s) {
-    s->plan = wkv6::plan_mix(B, T, H, backward);
+bool space_of(int B, int T, int H, long long rows, bool backward, bool f32_rows, Space* s) {
+    s->plan = wkv6::plan_mix(B, T, H, backward, f32_rows);
     const long long units = static_cast<long long>(B) * H;
-    s->blocks = (T + s->plan.anchor_len - 1) / s->plan.anchor_len;
-    const long long most = 6100805;                            // workgroups of 704
-    if (units >= most || units * s->plan.segs * (backward ? 3 : 1) >= most || (backward && units * s->blocks >= most)) return false;
+    s->blocks = T > 0 ? (T - 1) / s->plan.anchor_len + 1 : 0;
+    if (!wkv6::fits_a_launch(units, wkv6::kMixThreads) || !wkv6::fits_a_launch(units * s->plan.segs * (backward ? 3 : 1), wkv6::kMixThreads) ||
+        (backward && !wkv6::fits_a_launch(units * s->blocks, wkv6::kMixThreads)))
+        return false;
     if (s->plan.segs > 1) s->locals = s->plan.segs * units * (kStateFloats + 4);
     s->floats = s->locals;
     if (backward) {
@@ -60,6 +61,12 @@ bool space_of(int B, int T, int H, long long rows, bool backward, Space* s) {
         s->floats = 2 * s->locals + 2 * s->sums + 2 * s->anchors + s->head_sums;
     }
     return true;
+}
+// for rows of either type
+long long workspace_bytes_of(int B, int T, int H, long long rows, bool backward) {
+    Space bf16, f32;
+    if (!space_of(B, T, H, rows, backward, false, &bf16) || !space_of(B, T, H, rows, backward, true, &f32)) return -1;
+    return 4 * (bf16.floats > f32.floats ? bf16.floats : f32.floats);
 }
 
 wkv6::MixArgs mix_args(int B, int T, int H, long long rows, const float* g, long long g_stride, const int* offsets, const wkv6::MixPlan& p) {
@@ -76,17 +83,13 @@ wkv6::MixArgs mix_args(int B, int T, int H, long long rows, const float* g, long
 extern "C" {
 
 long long wkv6_head_decay_workspace_bytes(int B, int T, int H, int N) {
-    Space s;
     if (N != kHeadSize || B < 0 || T < 0 || H < 1 || H > kMaxHeads) return -1;
-    if (B == 0) return 0;
-    return space_of(B, T, H, 0, false, &s) ? 4 * s.floats : -1;
+    return B == 0 ? 0 : workspace_bytes_of(B, T, H, 0, false);
 }
 
 long long wkv6_head_decay_backward_workspace_bytes(int B, int T, int H, int N, long long rows) {
-    Space s;
     if (N != kHeadSize || B < 0 || T < 0 || H < 1 || H > kMaxHeads || rows < 0 || rows > 0x7fffffffLL) return -1;
-    if (B == 0) return 0;
-    return space_of(B, T, H, rows, true, &s) ? 4 * s.floats : -1;
+    return B == 0 ? 0 : workspace_bytes_of(B, T, H, rows, true);
 }
 
 int wkv6_head_decay_prefill(int B, int T, int H, int N, long long rows, const void* r, const void* k, const void* v,
@@ -103,7 +106,7 @@ int wkv6_head_decay_prefill(int B, int T, int H, int N, long long rows, const vo
     }
     if (any_misaligned(r, k, v, out, state_in, state_out) || misaligned4(g) || misaligned4(offsets)) return WKV6_ERR_ALIGN;
     Space s;
-    if (!space_of(B, T, H, rows, false, &s)) return WKV6_ERR_SHAPE;
+    if (!space_of(B, T, H, rows, false, dtype == WKV6_DTYPE_F32, &s)) return WKV6_ERR_SHAPE;
     if (s.floats > 0) {
         if (!workspace) return WKV6_ERR_NULL;
         if (misaligned(workspace)) return WKV6_ERR_ALIGN;
@@ -160,7 +163,7 @@ int wkv6_head_decay_backward(int B, int T, int H, int N, long long rows, const v
         misaligned4(dg) || misaligned4(offsets))
         return WKV6_ERR_ALIGN;
     Space s;
-    if (!space_of(B, T, H, rows, true, &s)) return WKV6_ERR_SHAPE;
+    if (!space_of(B, T, H, rows, true, dtype == WKV6_DTYPE_F32, &s)) return WKV6_ERR_SHAPE;
     if (s.floats > 0) {
         if (!workspace) return WKV6_ERR_NULL;
         if (misaligned(workspace)) return WKV6_ERR_ALIGN;
