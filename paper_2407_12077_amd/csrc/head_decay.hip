@@ -8,7 +8,7 @@
 //     S   = A_last S_0 + sum_i k_i^T (exp(g_{i+1} + .. + g_last) v_i)
 //
 // four products on the matrix cores.  Decays are only ever exponentials of sums of g inside a block of 16 tokens and products of
-// such, never a quotient, so nothing overflows and nothing but a difference inside a block is subtracted.
+// such, never a quotient, so nothing overflows and nothing is subtracted but sums inside a block, which two numbers hold to 2^-31.
 //
 // The gradients are products of the same form (o, S as above, do the gradient of o):
 //     dr = mix(q = do, k = v, v = k; S_0 transposed)     dv = reversed mix(q = k, k = r, v = do)     dk = reversed mix(q = v, k = do, v = r)
@@ -170,12 +170,12 @@ constexpr int kDecayPlaces = 3;        // for a chunk's decays: being formed, th
 constexpr int kStreamed = 2;             // cache policy of the read-outs, non-temporal: prefill 8 x 4096 x 32 117.7 -> 115.6 us, its gradients 390 -> 384
 constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
 
-// A chunk's decays by token, in LDS.  In logarithms to base 2 (pre) or as factors (the others)
+// A chunk's decays by token, in LDS.  In logarithms to base 2 (high, low) or as factors (the others)
 template <int kC>
 struct Decays {
-    float pre[kC];                     // sum of g from the block's first token to this
-    float pre_key[kC];                 // the same of tokens that are there, far above nought of others
-    float in_block[kC];                // exp2(pre)
+    float high[kC], low[kC];           // sum of g from the block's first token to this, in two parts: in multiples of 2^-10, which stay exact, and the rest
+    float high_key[kC];                // high of tokens that are there, far above nought of others
+    float in_block[kC];                // exp2(high + low)
     float to_block[kC];                // from behind this token to the block's end; nought for tokens that are not there
     float in_chunk[kC];                // from the chunk's first token to this
     float to_chunk[kC];                // from behind this token to the chunk's end; nought for tokens that are not there
@@ -404,7 +404,9 @@ struct Walk {
         const bool has = w.reverse ? t + 1 < s.len : there;
         g = g < kLowest ? kLowest : g;                          // (NaN stays)
         g = has ? g * kLog2e : 0.f;
-        const float pre = prefix16(g), behind = dpp<0x101>(suffix16(g));        // (nothing is subtracted)
+        // a token that forgets nearly all takes no bits from the differences of tokens behind it: 22 bits hold sixteen parts of up to 185
+        const float step = __builtin_rintf(g * 1024.f) * (1.f / 1024.f), high = prefix16(step), low = prefix16(g - step);
+        const float pre = high + low, behind = dpp<0x101>(suffix16(g));         // (the factors: nothing is subtracted)
         float block = 0.f, before = 0.f, after = 0.f, all = 0.f;               // sums over this block, those in front of it and behind it
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
@@ -415,8 +417,9 @@ struct Walk {
             all += sum;
         }
         if (lane < kC) {
-            d.pre[lane] = pre;
-            d.pre_key[lane] = there ? pre : 32768.f;             // 2^-32768 is nought
+            d.high[lane] = high;
+            d.low[lane] = low;
+            d.high_key[lane] = there ? high : 32768.f;           // 2^-32768 is nought
             d.in_block[lane] = exp2_near(pre);
             d.to_block[lane] = there ? exp2_near(behind) : 0.f;
             d.in_chunk[lane] = exp2_near(before + pre);
@@ -445,10 +448,10 @@ struct Walk {
         for (int kb = kQ; kb >= 0; --kb) {
             const int key = 16 * kb + 4 * g4;
             if (kb == kQ) {
-                const float pre = d.pre[query];
-                const float4v pk = *reinterpret_cast<const float4v*>(&d.pre_key[key]);
+                const float4v high = d.high[query] - *reinterpret_cast<const float4v*>(&d.high_key[key]);
+                const float4v low = d.low[query] - *reinterpret_cast<const float4v*>(&d.low[key]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[kb][e] = key + e <= query ? sc[kb][e] * exp2_near(pre - pk[e]) : 0.f;
+                for (int e = 0; e < 4; ++e) sc[kb][e] = key + e <= query ? sc[kb][e] * exp2_near(high[e] + low[e]) : 0.f;
             } else {
                 sc[kb] *= *reinterpret_cast<const float4v*>(&d.to_block[key]) * f;
                 f *= d.block[kb];

@@ -1,0 +1,310 @@
+"""The head-decay time mix and its gradients against the recurrence in 64 bits (oracle/head_decay_numpy.py), element by element
+within bounds that tests/operator_util.py derives: lengths around blocks of 16 and chunks of 32 and 64, single tokens, packed sequences with empty ones and
+rows of nobody, cuts of the token axis, decays of nought and infinity, both types of rows, strides, streams, graphs, shared workspaces."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_12077_amd as wkv
+from operator_util import CODE, N, Mix, check, np64, roundings
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = [(BF16, BF16), (BF16, F32), (F32, F32)]
+IDS = ["bf16", "bf16_f32out", "f32"]
+STEP = 2.0 ** -24
+
+
+def check_prefill(x, out, state, out_dtype):
+    want, last = x.exact()
+    m, m_last = x.magnitudes()
+    K = STEP * roundings(x.T) + (2.0 ** -17 if out_dtype == BF16 else 0)
+    check("out", out, want, K * m, x.covered, out_dtype)
+    if state is not None:
+        check("state", state, last, STEP * roundings(x.T) * m_last)
+
+
+def check_gradients(x, got):
+    want, bounds = x.exact_gradients(), x.gradient_bounds()
+    for name, a, w, b in zip(("dr", "dk", "dv"), got, want, bounds):
+        check(name, a, w, b, x.covered, x.dtype)
+    if x.decay == "head":
+        mask = x.covered.numpy()
+        check("dg", got[3], want[3][mask].sum(0), bounds[3][mask].sum(0) + STEP * abs(want[3][mask]).sum(0))
+    else:
+        check("dg", got[3], want[3], bounds[3], x.covered)
+    if got[4] is not None:
+        check("dstate_in", got[4], want[4], bounds[4])
+
+
+# ---------------------------------------------------------------------------------------------- prompts
+@pytest.mark.parametrize("dtype,out_dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 32, 33, 47, 63, 64, 65, 127, 128, 130, 193, 300])
+def test_prefill_lengths(gpu_device, T, dtype, out_dtype):
+    x = Mix(T, H=2, B=2, T=T, dtype=dtype, fused=T % 2 == 1, decay="head" if T % 3 == 0 else "token", state=T % 4 != 0)
+    out, state = x.prefill(out_dtype)
+    check_prefill(x, out, state, out_dtype)
+
+
+@pytest.mark.parametrize("dtype,out_dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("lengths,H", [([5, 0, 64, 1, 130, 0], 3), ([0, 0], 2), ([1] * 9, 1), ([257, 3, 64, 129], 2)])
+def test_prefill_packed(gpu_device, lengths, H, dtype, out_dtype):
+    x = Mix(len(lengths), H=H, lengths=lengths, front=3, tail=5, dtype=dtype, fused=True, longest=max(1, max(lengths)))
+    out, state = x.prefill(out_dtype)
+    check_prefill(x, out, state, out_dtype)
+    for b, n in enumerate(lengths):
+        if n == 0:
+            assert torch.equal(state[b], x.state_in[b])
+
+
+@pytest.mark.parametrize("dtype,out_dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("T,packed", [(1500, False), (2111, True)])
+def test_prefill_in_pieces(gpu_device, T, packed, dtype, out_dtype):
+    x = Mix(7, H=1, lengths=[T, 700, 64, 65, 0, 1], tail=2, dtype=dtype, longest=T) if packed else Mix(8, H=2, B=1, T=T, dtype=dtype)
+    assert wkv.wkv6_head_decay_workspace_bytes(x.B, x.T, x.H, N) > 0
+    out, state = x.prefill(out_dtype)
+    check_prefill(x, out, state, out_dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_prefill_decays_of_nought_and_one(gpu_device, dtype):
+    x = Mix(11, H=3, B=2, T=150, dtype=dtype)
+    x.g[::7] = 0.
+    x.g[5::31] = -float("inf")
+    x.g[40:44] = -1e30
+    x.g[100:120] = -90.                                        # a whole block far below one
+    x.g[:, 2] = -float("inf")                                  # a head that forgets everything
+    out, state = x.prefill()
+    check_prefill(x, out, state, F32)
+    alone = (x.r[:, 2].double() * x.k[:, 2].double()).sum(1)[:, None] * x.v[:, 2].double()
+    assert torch.allclose(out[:, 2].double(), alone, rtol=2e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("scale", [1e-12, 1e9])
+def test_prefill_bf16_rows_of_any_size(gpu_device, scale):
+    """No operand has to lie inside a smaller type's range."""
+    x = Mix(13, H=1, B=1, T=100, scale=scale, state=False)
+    out, state = x.prefill()
+    check_prefill(x, out, state, F32)
+
+
+def test_prefill_state_in_place_absent_and_unwritten(gpu_device):
+    x = Mix(14, H=2, B=3, T=70)
+    out, state = x.prefill()
+    keep = x.state_in.clone()
+    again, same = x.prefill(state_out=x.state_in)
+    assert same is x.state_in and torch.equal(same, state) and torch.equal(again, out)
+    x.state_in.copy_(keep)
+    assert torch.equal(x.prefill(state_out=None)[0], out)
+    x.state_in = None
+    out, state = x.prefill()
+    check_prefill(x, out, state, F32)
+
+
+def test_prefill_continued_and_token_by_token(gpu_device):
+    """A prompt, the rest of it, and single tokens behind: as one call."""
+    x = Mix(15, H=2, B=2, T=90, dtype=F32)
+    whole, last = x.prefill()
+    parts, state = [], x.state_in
+    view = lambda t, a, b: t.view(2, 90, *t.shape[1:])[:, a:b].contiguous()  # noqa: E731
+    for a, b in ((0, 40), (40, 41), (41, 86)):
+        y = Mix(15, H=2, B=2, T=b - a, dtype=F32)
+        y.r, y.k, y.v, y.g = (view(t, a, b).view((b - a) * 2, *t.shape[1:]) for t in (x.r, x.k, x.v, x.g))
+        y.state_in = state
+        out, state = y.prefill()
+        parts.append(out.view(2, b - a, 2, N))
+    for t in range(86, 90):
+        out = torch.empty((2, 2, N), device="cuda")
+        r, k, v, g = (view(a, t, t + 1) for a in (x.r, x.k, x.v, x.g))
+        wkv.wkv6_head_decay_decode(2, 2, N, r, k, v, 2 * N, g, 2, state, out, state, CODE[F32], CODE[F32])
+        parts.append(out[:, None])
+    m, m_last = x.magnitudes()
+    K = 2 * STEP * roundings(x.T)
+    check("out", torch.cat(parts, 1).view(180, 2, N), np64(whole), K * m)
+    check("state", state, np64(last), K * m_last)
+
+
+def test_offsets_outside_the_rows_are_cut(gpu_device):
+    """-5 is taken as 0, what lies behind the rows as their end, and a sequence ends after T tokens: here 50 rows, T = 30."""
+    x = Mix(16, H=2, lengths=[30, 5, 0], tail=15, longest=30)
+    x.offsets = torch.tensor([-5, 40, 1 << 30, 3], dtype=torch.int32, device="cuda")
+    x.spans = [(0, 30), (40, 50), (50, 50)]
+    x.covered[:] = True
+    x.covered[30:40] = False
+    out, state = x.prefill()
+    check_prefill(x, out, state, F32)
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_prefill_random(gpu_device, seed):
+    rng = np.random.default_rng(seed)
+    H = int(rng.integers(1, 5))
+    lengths = [int(n) for n in rng.integers(0, 260, int(rng.integers(1, 7)))]
+    dtype, out_dtype = TYPES[seed % 3]
+    x = Mix(seed, H=H, lengths=lengths, front=int(rng.integers(0, 4)), tail=int(rng.integers(0, 4)), dtype=dtype, fused=bool(seed & 1),
+            decay="head" if seed & 2 else "token", state=bool(seed & 4), longest=max(1, max(lengths)) + int(rng.integers(0, 500)))
+    out, state = x.prefill(out_dtype)
+    check_prefill(x, out, state, out_dtype)
+
+
+# ---------------------------------------------------------------------------------------------- single tokens
+@pytest.mark.parametrize("dtype,out_dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("B,H", [(1, 1), (3, 5), (40, 12), (300, 7)])
+def test_decode(gpu_device, B, H, dtype, out_dtype):
+    x = Mix(B, H=H, B=B, T=1, dtype=dtype, fused=B % 2 == 1, decay="head" if H == 5 else "token", state=B != 40)
+    if x.decay == "token":
+        x.g[0, 0] = -float("inf")
+    out = torch.full((B, H, N), float("nan"), dtype=out_dtype, device="cuda")
+    state = torch.full((B, H, N, N), float("nan"), device="cuda")
+    wkv.wkv6_head_decay_decode(B, H, N, x.r, x.k, x.v, x.stride, x.g, x.g_stride, x.state_in, out, state, CODE[dtype], CODE[out_dtype])
+    want, last = x.exact()
+    m, m_last = x.magnitudes()
+    # 64 additions and five factors, the decay one unit in the last place (two roundings), no chunks
+    check("out", out, want, STEP * 72 * m, None, out_dtype)
+    check("state", state, last, STEP * 6 * m_last)
+    if x.state_in is not None:
+        keep = x.state_in.clone()
+        again = torch.empty_like(out)
+        wkv.wkv6_head_decay_decode(B, H, N, x.r, x.k, x.v, x.stride, x.g, x.g_stride, keep, again, keep, CODE[dtype], CODE[out_dtype])
+        assert torch.equal(keep, state) and torch.equal(again, out)
+        wkv.wkv6_head_decay_decode(B, H, N, x.r, x.k, x.v, x.stride, x.g, x.g_stride, x.state_in, again, None, CODE[dtype], CODE[out_dtype])
+        assert torch.equal(again, out)
+
+
+# ---------------------------------------------------------------------------------------------- gradients
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 2, 16, 17, 31, 32, 33, 64, 65, 100, 128, 129, 200])
+def test_gradients_lengths(gpu_device, T, dtype):
+    x = Mix(T, H=2, B=2, T=T, dtype=dtype, fused=T % 2 == 0, decay="head" if T % 3 == 2 else "token", state=T % 4 != 0, gradients=True)
+    check_gradients(x, x.backward())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("decay", ["token", "head"])
+@pytest.mark.parametrize("lengths", [[70, 0, 1, 33, 64], [0], [1, 1, 1]])
+def test_gradients_packed(gpu_device, lengths, decay, dtype):
+    x = Mix(len(lengths), H=3, lengths=lengths, front=2, tail=4, dtype=dtype, decay=decay, fused=True, longest=max(1, max(lengths)), gradients=True)
+    got = x.backward()
+    check_gradients(x, got)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("state", [True, False], ids=["states", "no_states"])
+def test_gradients_in_pieces_over_several_blocks(gpu_device, dtype, state):
+    x = Mix(21, H=1, lengths=[2100, 1024, 1025, 5], tail=1, dtype=dtype, state=state, gradients=True)
+    check_gradients(x, x.backward())
+
+
+def test_gradients_with_decays_of_nought_and_one(gpu_device):
+    x = Mix(22, H=2, B=1, T=140, dtype=F32, gradients=True)
+    x.g[::6] = 0.
+    x.g[9::40] = -float("inf")
+    x.g[70:90] = -200.
+    check_gradients(x, x.backward())
+
+
+def test_gradients_without_the_state_s(gpu_device):
+    x = Mix(23, H=2, B=2, T=80, gradients=True)
+    a = x.backward()
+    into = [torch.empty_like(t) for t in a[:4]] + [None]
+    x.backward(into=into)
+    for p, q in zip(a[:4], into):
+        assert torch.equal(p, q)
+    x.dstate_out = None
+    check_gradients(x, x.backward())
+
+
+def test_gradients_of_no_tokens(gpu_device):
+    x = Mix(24, H=3, lengths=[0, 0], longest=1, decay="head", gradients=True)
+    got = x.backward()
+    assert bool((got[3] == 0).all()) and torch.equal(got[4], x.dstate_out)
+
+
+def test_gradients_against_differences(gpu_device):
+    """fp32 rows: a step along a direction changes the loss, computed in 64 bits, by the gradients' product with it."""
+    from oracle.head_decay_numpy import head_decay_numpy
+    x = Mix(25, H=2, lengths=[50, 20, 0, 3], dtype=F32, gradients=True)
+    got = [np64(a) for a in x.backward()]
+    rng = np.random.default_rng(1)
+    base = dict(r=np64(x.r), k=np64(x.k), v=np64(x.v), g=np64(x.g), state_in=np64(x.state_in))
+    dout, dS = np64(x.dout), np64(x.dstate_out)
+
+    def loss(y):
+        out, S = head_decay_numpy(y["r"], y["k"], y["v"], y["g"], x.spans, y["state_in"])
+        return np.nansum(out * dout) + (S * dS).sum()
+    bounds = x.gradient_bounds()
+    for name, grad, bound in zip(("r", "k", "v", "g", "state_in"), got, bounds):
+        step = rng.standard_normal(grad.shape)
+        diff = (loss({**base, name: base[name] + 1e-5 * step}) - loss({**base, name: base[name] - 1e-5 * step})) / 2e-5
+        # the gradient's own bound along the direction, and the differences' error of second order
+        assert abs((grad * step).sum() - diff) <= (bound * abs(step)).sum() + 1e-6 * abs(grad * step).sum(), name
+
+
+# ---------------------------------------------------------------------------------------------- how it is called
+def test_same_bits_from_call_to_call(gpu_device):
+    x = Mix(31, H=2, lengths=[900, 30, 64], gradients=True, decay="head")
+    a, b = x.prefill(), x.prefill()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    a, b = x.backward(), x.backward()
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_two_streams_at_once(gpu_device):
+    xs = [Mix(41 + i, H=2, B=2, T=700 + 33 * i, gradients=True) for i in range(2)]
+    want = [(x.prefill(), x.backward()) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    spaces = [(x.workspace(), x.workspace(True)) for x in xs]
+    torch.cuda.synchronize()
+    got = []
+    for x, s, (w0, w1) in zip(xs, streams, spaces):
+        with torch.cuda.stream(s):
+            got.append((x.prefill(workspace=w0), x.backward(workspace=w1)))
+    torch.cuda.synchronize()
+    for (f, g), (f2, g2) in zip(want, got):
+        assert all(torch.equal(p, q) for p, q in zip(f + tuple(g), f2 + tuple(g2)))
+
+
+def test_captured_calls_share_a_workspace(gpu_device):
+    """Prefill and gradients of two inputs in two graphs that use one workspace, replayed in turn with eager work between."""
+    xs = [Mix(51 + i, H=2, lengths=[1200, 65 + i], gradients=True, decay="head" if i else "token") for i in range(2)]
+    want = [(x.prefill(), x.backward()) for x in xs]
+    space = torch.full((max(x.workspace(True).numel() for x in xs),), float("nan"), device="cuda")
+    outs = [(x.prefill(workspace=space), x.backward(workspace=space)) for x in xs]
+    side = torch.cuda.Stream()
+    graphs = []
+    torch.cuda.synchronize()
+    for x, (f, g) in zip(xs, outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            x.prefill(out=f[0], state_out=f[1], workspace=space)
+            x.backward(into=g, workspace=space)
+        graphs.append(graph)
+    for replay in range(3):
+        for f, g in outs:
+            for t in (*f, *g):
+                t.fill_(7.0)
+        space.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (f, g), (f2, g2) in zip(want, outs):
+            assert all(torch.equal(p, q) for p, q in zip(f + tuple(g), f2 + tuple(g2))), replay
+
+
+def test_long_prompt_of_the_benchmark_s_heads(gpu_device):
+    """8192 tokens of 32 heads: every unit's last state, and its read-outs at the end, by a walk in 64 bits on the GPU."""
+    x = Mix(61, H=32, B=1, T=8192, decay="head")
+    out, state = x.prefill()
+    S = x.state_in[0].double()
+    A = x.state_in[0].double().abs()
+    w = torch.exp(x.g.double())[:, None, None]
+    r, k, v = (t.double() for t in (x.r, x.k, x.v))
+    for t in range(x.T):
+        S = w * S + k[t][:, :, None] * v[t][:, None, :]
+        A = w.sqrt() * A + k[t].abs()[:, :, None] * v[t].abs()[:, None, :]
+        if t >= x.T - 3:
+            o, m = (r[t][:, :, None] * S).sum(1), (r[t].abs()[:, :, None] * A).sum(1)
+            check("out", out[t], np64(o), STEP * roundings(x.T) * np64(m))
+    check("state", state[0], np64(S), STEP * roundings(x.T) * np64(A))
