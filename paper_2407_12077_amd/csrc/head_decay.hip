@@ -676,8 +676,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
     const int chunks = s.end > s.begin ? (s.end - s.begin + kC - 1) / kC : 0;
     using W = Walk<T, Out, kC, kStates, kSums>;
     W walk{a, w, s, lds, lane, wave, lane & 15, lane >> 4, s.begin / kC, chunks, {}};
-    // the segment that nothing follows on the walk hands nothing over
-    if (kStates && (chunks == 0 || seg == (w.reverse ? 0 : s.segs - 1))) return;
+    const long long units = static_cast<long long>(a.B) * a.H;
+    float* const locals = w.locals + unit * static_cast<long long>(kStateFloats);
+    // A call in place: its last segment overwrites what others may not have read yet.  They read a copy in the place of the one segment that hands
+    // nothing over, as nothing follows it on the walk.
+    const int last = w.reverse ? 0 : s.segs - 1;
+    const bool copied = a.segs > 1 && w.state_in && w.state_in == w.state_out;
+    float4v* const copy = reinterpret_cast<float4v*>(locals + last * units * kStateFloats);
+    if (kStates && (chunks == 0 || seg == last)) {
+        const float4v* from = reinterpret_cast<const float4v*>(w.state_in + unit * static_cast<long long>(kStateFloats));
+        if (copied && seg == last)
+            for (int i = threadIdx.x; i < kStateFloats / 4; i += kThreads) copy[i] = from[i];
+        return;
+    }
 
     if (part == 2 * kWaves + kMovers) {                         // the timer
         if (chunks == 0) return;
@@ -744,13 +755,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
         return;
     }
 
-    const long long units = static_cast<long long>(a.B) * a.H;
-    float* const locals = w.locals + unit * static_cast<long long>(kStateFloats);
     float* const totals = w.locals + a.segs * units * kStateFloats + unit;
 #pragma unroll
     for (int i = 0; i < 4; ++i) walk.state[i] = float4v{0.f, 0.f, 0.f, 0.f};
     if constexpr (!kStates) {
-        if (w.state_in) walk.read_state(w.state_in + unit * static_cast<long long>(kStateFloats), w.turned, walk.state);
+        if (w.state_in) walk.read_state(copied ? reinterpret_cast<const float*>(copy) : w.state_in + unit * static_cast<long long>(kStateFloats), w.turned, walk.state);
         // and what the segments in front of this one hand over, in the walk's order
         const int count = w.reverse ? s.segs - 1 - seg : seg;
         constexpr int kAtOnce = 4;                              // asked for together
@@ -783,7 +792,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
     if constexpr (kStates) {
         walk.write_state(locals + seg * units * kStateFloats, w.locals_turned, 1.f);
         if (threadIdx.x == 0) totals[seg * units] = walk.total;
-    } else if (w.state_out && seg == (w.reverse ? 0 : s.segs - 1)) {
+    } else if (w.state_out && seg == last) {
         float factor = 1.f;
         if (w.reverse && s.len > 0) factor = decay_factor(a.g[s.first * a.g_row + s.h]);
         walk.write_state(w.state_out + unit * static_cast<long long>(kStateFloats), w.turned, factor);

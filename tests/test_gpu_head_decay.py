@@ -101,6 +101,42 @@ def test_prefill_state_in_place_absent_and_unwritten(gpu_device):
     check_prefill(x, out, state, F32)
 
 
+@pytest.mark.parametrize("lengths,H", [([3000], 40), ([2500, 0, 300, 4000, 1], 11)])
+def test_prefill_in_pieces_in_place(gpu_device, lengths, H):
+    """More workgroups than the card takes at once: the last pieces write states that the first have read, or a copy of them."""
+    x = Mix(17, H=H, lengths=lengths)
+    assert x.workspace().numel() > 4
+    out, state = x.prefill()
+    again, same = x.prefill(state_out=x.state_in)
+    assert same is x.state_in and torch.equal(same, state) and torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_rows_far_apart(gpu_device, dtype):
+    """Rows and decays inside wider tensors: what lies between them is neither read (NaN) nor written."""
+    x = Mix(18, H=2, lengths=[70, 33], dtype=dtype, gradients=True)
+    (out, state), grads = x.prefill(), x.backward()
+    wide = torch.full((x.rows, 3 * 2 * N + 24), float("nan"), dtype=dtype, device="cuda")
+    part = lambda t, i: t[:, i * 2 * N + 8:(i + 1) * 2 * N + 8]  # noqa: E731
+    for i, t in enumerate((x.r, x.k, x.v)):
+        part(wide, i).copy_(t.reshape(x.rows, -1))
+    x.r, x.k, x.v = (part(wide, i) for i in range(3))
+    x.stride = wide.shape[1]
+    decays = torch.full((x.rows, 7), float("nan"), device="cuda")
+    decays[:, 3:5] = x.g
+    x.g, x.g_stride = decays[:, 3:5], 7
+    out2, state2 = x.prefill()
+    assert torch.equal(out, out2) and torch.equal(state, state2)
+    to = torch.full_like(wide, 5.0)
+    dg = torch.empty((x.rows, 2), device="cuda")
+    d0 = torch.empty_like(grads[4])
+    x.backward(into=[*(part(to, i) for i in range(3)), dg, d0])
+    for i in range(3):
+        assert torch.equal(part(to, i), grads[i].reshape(x.rows, -1))
+    assert bool((to[:, :8] == 5).all()) and bool((to[:, 3 * 2 * N + 8:] == 5).all())
+    assert torch.equal(dg, grads[3]) and torch.equal(d0, grads[4])
+
+
 def test_prefill_continued_and_token_by_token(gpu_device):
     """A prompt, the rest of it, and single tokens behind: as one call."""
     x = Mix(15, H=2, B=2, T=90, dtype=F32)
