@@ -77,7 +77,7 @@ typedef enum {
     WKV6_ERR_UNSUPPORTED = 3, /* N != 64, or an unknown dtype code */
     WKV6_ERR_LAUNCH = 4,      /* hipGetLastError() after the launch was not hipSuccess */
     WKV6_ERR_ALIGN = 5,       /* a tensor base or the batch stride is not 16-byte aligned */
-    WKV6_ERR_WORKSPACE = 6    /* the shape needs more scratch memory than the library's fixed buffer */
+    WKV6_ERR_WORKSPACE = 6    /* the shape needs more scratch memory than the library's fixed buffer, or than the workspace of the call */
 } wkv6_status;
 
 typedef enum {

@@ -10,7 +10,7 @@
  * decay is given as its logarithm.  A scale of the read-out goes into r.
  *
  * Layout (row-major, innermost index last):
- *   B, T, H, N    sequences, tokens of the longest one, heads (at most 65536), head size, which must be 64
+ *   B, T, H, N    sequences, tokens of the longest one (at most 2^30), heads (at most 65536), head size, which must be 64
  *   rows          rows of the tensors below
  *   offsets       [B + 1] int32, device: sequence b has the rows offsets[b] .. offsets[b+1] - 1, one sequence behind the other, none longer
  *                 than T.  Rows in front of offsets[0] and from offsets[B] on belong to nobody: they are not read, and what a

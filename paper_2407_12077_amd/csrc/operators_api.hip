@@ -23,13 +23,14 @@ int status_of(hipError_t err) { return err == hipSuccess ? WKV6_OK : WKV6_ERR_LA
 // 32-bit offsets inside a chunk of 64 tokens
 constexpr long long kMaxStride = 1ll << 22;
 constexpr int kMaxHeads = 65536;
+constexpr int kMaxTokens = 1 << 30;
 constexpr long long kStateFloats = kHeadSize * kHeadSize;
 
 // Sizes and types that every call of the mix has; the strides are looked at where there are rows.
 int check_mix(int B, int T, int H, int N, long long rows, bool packed, int dtype, int out_dtype) {
     if (N != kHeadSize || !known(dtype) || !known(out_dtype)) return WKV6_ERR_UNSUPPORTED;
     if (dtype == WKV6_DTYPE_F32 && out_dtype != WKV6_DTYPE_F32) return WKV6_ERR_UNSUPPORTED;
-    if (B < 0 || T < 0 || H < 1 || H > kMaxHeads || rows < 0 || rows > 0x7fffffffLL) return WKV6_ERR_SHAPE;
+    if (B < 0 || T < 0 || T > kMaxTokens || H < 1 || H > kMaxHeads || rows < 0 || rows > 0x7fffffffLL) return WKV6_ERR_SHAPE;
     if (!packed && rows != static_cast<long long>(B) * T) return WKV6_ERR_SHAPE;
     return WKV6_OK;
 }
@@ -83,12 +84,12 @@ wkv6::MixArgs mix_args(int B, int T, int H, long long rows, const float* g, long
 extern "C" {
 
 long long wkv6_head_decay_workspace_bytes(int B, int T, int H, int N) {
-    if (N != kHeadSize || B < 0 || T < 0 || H < 1 || H > kMaxHeads) return -1;
+    if (N != kHeadSize || B < 0 || T < 0 || T > kMaxTokens || H < 1 || H > kMaxHeads) return -1;
     return B == 0 ? 0 : workspace_bytes_of(B, T, H, 0, false);
 }
 
 long long wkv6_head_decay_backward_workspace_bytes(int B, int T, int H, int N, long long rows) {
-    if (N != kHeadSize || B < 0 || T < 0 || H < 1 || H > kMaxHeads || rows < 0 || rows > 0x7fffffffLL) return -1;
+    if (N != kHeadSize || B < 0 || T < 0 || T > kMaxTokens || H < 1 || H > kMaxHeads || rows < 0 || rows > 0x7fffffffLL) return -1;
     return B == 0 ? 0 : workspace_bytes_of(B, T, H, rows, true);
 }
 

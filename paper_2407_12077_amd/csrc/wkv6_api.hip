@@ -401,7 +401,7 @@ const char* wkv6_status_string(int status) {
         case WKV6_ERR_UNSUPPORTED: return "unsupported head size or dtype";
         case WKV6_ERR_LAUNCH: return "kernel launch failed";
         case WKV6_ERR_ALIGN: return "pointer or stride not 16-byte aligned";
-        case WKV6_ERR_WORKSPACE: return "shape needs more scratch than the library holds";
+        case WKV6_ERR_WORKSPACE: return "shape needs more scratch than the library, or the workspace of the call, holds";
         default: return "unknown status";
     }
 }

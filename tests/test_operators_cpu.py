@@ -106,6 +106,7 @@ def test_prefill_refuses():
     assert prefill(dtype=F32, out_dtype=BF16) == UNSUPPORTED and prefill(out_dtype=7) == UNSUPPORTED
     assert prefill(T=-1) == SHAPE and prefill(rows=15) == SHAPE and prefill(rows=-1, offsets=A) == SHAPE
     assert prefill(rows=1 << 31, offsets=A) == SHAPE
+    assert prefill(T=(1 << 30) + 1, offsets=A) == SHAPE and backward(T=(1 << 30) + 1, offsets=A) == SHAPE
     assert prefill(out=None) == NULL and prefill(out=P(0x1004)) == ALIGN and prefill(state_out=P(0x1004)) == ALIGN
     assert prefill(offsets=P(0x1001)) == ALIGN
     assert prefill(B=1 << 20, T=0, H=64, rows=0) == SHAPE      # more workgroups than a launch has
@@ -164,7 +165,7 @@ def test_workspace_sizes():
     mix, back, norm = wkv.wkv6_head_decay_workspace_bytes, wkv.wkv6_head_decay_backward_workspace_bytes, wkv.wkv6_layernorm_backward_workspace_bytes
     assert mix(8, 4096, 32, 64) == 0                           # 256 units fill the compute units: one walk each
     assert mix(0, 10, 4, 64) == 0 and mix(1, 0, 4, 64) == 0 and mix(1, 1, 1, 64) == 0
-    for bad in ((1, 8, 2, 32), (-1, 8, 2, 64), (1, -8, 2, 64), (1, 8, 0, 64), (1 << 20, 8, 64, 64)):
+    for bad in ((1, 8, 2, 32), (-1, 8, 2, 64), (1, -8, 2, 64), (1, 8, 0, 64), (1 << 20, 8, 64, 64), (1, (1 << 30) + 1, 2, 64)):
         assert mix(*bad) == -1 and back(*bad, 8) == -1
     assert back(1, 8, 2, 64, -1) == -1
     # anchors of both directions, two sums a row and head, partial sums of a head
