@@ -25,6 +25,12 @@
 //   consumers  (4) own 16 of the 64 value columns each: the state's [64][16] columns stay in registers for the whole walk, and as accumulators
 //              of k^T (decayed v) they lie as S^T q^T wants them.  They add that to the producers' part, in its place in LDS
 //
+// What bounds it.  8 x 4096 tokens x 32 heads, bf16: 537 MB in 117 us, 4.6 TB/s, where a large copy reaches 5.1; a round (64 tokens of every
+// workgroup) takes 1.8 us, of which the consumers and the last producer work 1.25, so memory and the barrier share the rest.  One prompt of 131072 tokens: 230
+// us for the states and 460 for the read-outs, 3.2 GB at 4.8 TB/s (k and v are read twice).  Gradients of 8 x 4096 x 32: 396 us for 1.49 GB
+// (counted: dv and dk find the rows that they share in an XCD's L2, dr runs the other way), 3.8 TB/s: three rounds of workgroups of 2.05 us a chunk.  fp32
+// rows: 4.3 us for 64 tokens, fp32 matrix instructions in series with their LDS reads.
+//
 // bf16 rows: products of rows are exact in fp32; the computed operands (P, S, decayed v) enter as sums of three bf16, which hold an
 // fp32 value whole over its whole range, one product for each; two where only bf16 read-outs come of them.  fp32 rows: fp32 matrix instructions.
 #include "head_decay.h"
@@ -803,7 +809,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
 //     dg_t = sum_{t <= s <= a} (r_s . dr_s - k_s . dk_s) + w_{a+1} <dS_{a+1}, S_a>
 // for any a >= t; dS_{a+1} is the gradient of the state behind token a + 1, and behind the last token that of state_out.  The sums nearly
 // cancel, so a is the end of t's block of anchor_len tokens and not of the sequence, and they are taken in 64 bits.
-// A workgroup per unit and block.
+// A workgroup per unit and block.  14 us of the 8 x 4096 x 32 gradients' 400: 24 MB, and 256 tokens at a time in series.
 __global__ __launch_bounds__(256) void decay_gradient_kernel(const MixArgs a, int blocks, const float* r_sums, const float* k_sums,
                                                              const float* behind, const float* front, float* head_sums, float* dg) {
     __shared__ double part[4];
@@ -871,7 +877,7 @@ __global__ __launch_bounds__(256) void decay_gradient_kernel(const MixArgs a, in
     }
 }
 
-// dg of one decay a head: the partial sums of a head, always in the same order.  A wave a head.
+// dg of one decay a head: the partial sums of a head, always in the same order.  A wave a head: 4 us, a launch.
 __global__ __launch_bounds__(64) void head_sums_kernel(long long count, int H, const float* head_sums, float* dg) {
     double v = 0.;
     for (long long i = threadIdx.x; i < count; i += 64) v += static_cast<double>(head_sums[i * H + blockIdx.x]);
@@ -921,7 +927,11 @@ double modelled(double units, double tokens, int segs, bool backward, bool f32_r
 MixPlan plan_mix(int B, int T, int H, bool backward, bool f32_rows) {
     const double units = static_cast<double>(B) * H, tokens = T > 0 ? T : 1;
     int segs = 1;
-    // pieces are for calls that would leave compute units idle; they read k and v (and r and dout) twice
+    // Pieces are for calls that would leave compute units idle; they read k and v (and r and dout) twice.  Measured, whole / in the planned number of
+    // pieces / the best of 1 to 32, us: bf16 1 x 4096 x 32 heads 94.7 / 32.6 (8) / 32.6, 1 x 30000 x 12 659 / 84 (21) / 84 (24), 4 x 2048 x 32 53.2 / 51.0
+    // (2) / 51.0; 5 x 4096 x 32 stays whole, 100, where the best cut takes 132 (6).  Gradients: 1 x 4096 x 32 114 / 89.5 (5) / 87.4 (8), 1 x 30000 x 12
+    // 754 / 219 (14) / 213 (6); 4 x 2048 x 32 stays whole, 130, against 144 (2).  A modelled gain of under 7 % is left: of 52 sizes and types five are
+    // more than 8 % off the best, the furthest 20 %
     if (units < 256.) {
         double least = 0.93 * modelled(units, tokens, 1, backward, f32_rows);
         for (int n = 2; n <= 32 && n * kMixBlock < T + kMixBlock; ++n) {

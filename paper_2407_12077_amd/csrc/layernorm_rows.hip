@@ -3,8 +3,10 @@
 //     u = (x - mean) rstd        y = u gamma + beta
 //     dx = rstd (a - mean(a) - u mean(a u)),  a = gamma dy        dgamma = sum over rows of dy u        dbeta = sum over rows of dy
 //
-// Both are bound by memory: a row is read once, stays in registers between its sums and its results, and every value leaves once.  A
-// row's values lie eight to a lane over one wave (64 lanes, sums without LDS) or over a workgroup of four, or of eight.
+// Both are bound by memory: a row is read once, stays in registers between its sums and its results, and every value leaves once, past
+// the caches.  32768 x 2048 bf16 rows: forward 53 us, 5.1 TB/s, a large copy's rate; gradients 74.5 us, 5.4 TB/s, of which the fold is 4.5.
+// Few rows wait on their latency: 24 x 4096 4.0 us, gradients of 1531 x 768 10.3 (6 and 4 in two launches).
+// A row's values lie eight to a lane over one wave (64 lanes, sums without LDS) or over a workgroup of four, or of eight.
 //
 // The sums over the rows: a workgroup takes every gridDim.x-th group of rows and a lane always the same columns, so its shares
 // of dgamma and dbeta stay in registers to the end; the waves' meet in LDS, the workgroups' in a second kernel that adds them in a
@@ -246,26 +248,34 @@ __global__ __launch_bounds__(256) void norm_fold_kernel(int rows, int D, const f
     else dbeta[column - D / 4] = part[0][lane];
 }
 
-// Lanes of a row of the forward pass: one wave, or four where a wave would hold too much or would leave most of the card idle.
-int norm_lanes(long long M, int D) { return D > 4096 || (D >= 1024 && M <= 1024) ? 256 : 64; }
-// Of the backward pass, which keeps a row, the next one, gamma and two sums for every column: 512 columns of bf16 rows a wave and more than that
-// several
-int norm_backward_lanes(long long M, int D, bool bf16) { return D > 8192 ? 512 : D > (bf16 ? 2048 : 1024) || (D >= 1024 && M <= 1024) ? 256 : 64; }
+// Lanes of a row: a wave, which needs no LDS and no barrier, up to 1024 columns; four waves where one would hold too much, or would be too few to
+// keep memory busy.  Measured, a wave against four, us:
+//                      bf16 x 1024   x 2048       fp32 x 1024    x 2048       gradients, bf16 x 1024   x 2048      fp32 x 1024   x 2048
+//     1500 rows         4.4   4.6     5.8  4.5     4.5   4.5      7.7   6.0    9.7  10.4                12.9  12.2   11.8  11.8    20.3  15.7
+//     4096 rows         4.8   6.3     7.9  9.1     8.1   9.1     16.3  16.0   12.8  14.6                18.0  18.3   17.9  18.7    33.0  27.6
+//     32768 rows       25.6  35.4    53.0 55.2    58.4  58.3    122.8 109.5   40.6  60.2                74.5  78.6   84.2  95.5   161.1 161.2
+// (one type of either: as fp32.)  4096 columns, 32768 rows: bf16 119.5 against 110.6.
+int norm_lanes(long long M, int D, bool bf16) { return D > 2048 || (D > 1024 && (!bf16 || M < 4096)) ? 256 : 64; }
+// The gradients keep a row, the next one, gamma and two sums for every column, which four waves with eight items a lane barely hold: eight waves beyond
+// 8192 columns.  Eight against four at 4096 x 10240: bf16 71 and 89 us, fp32 134 and 164 (fp32 rows with bf16 dy 136 and 127); at 4096 x 8192
+// 60 and 54, 107 and 96.
+int norm_backward_lanes(long long M, int D, bool bf16) { return D > 8192 ? 512 : norm_lanes(M, D, bf16); }
 
-// f(lanes, items of a lane), items of eight columns: the least of 1, 2, 4 and, up to kMost, 8 that hold a row
-template <int kMost, typename F>
+// f(lanes, items of a lane), items of eight columns: the least of 1, 2, 4 and, in the forward pass, 8 that hold a row
+template <bool kForward, typename F>
 hipError_t with_items(int lanes, int items, F f) {
+    constexpr std::integral_constant<int, 64> wave;
+    constexpr std::integral_constant<int, 256> four;
+    constexpr std::integral_constant<int, 1> one;
+    constexpr std::integral_constant<int, 2> two;
+    constexpr std::integral_constant<int, 4> most;
     const int n = (items + lanes - 1) / lanes;
-    auto pick = [&](auto l) {
-        if (n <= 1) return f(l, std::integral_constant<int, 1>{});
-        if (n <= 2) return f(l, std::integral_constant<int, 2>{});
-        if constexpr (kMost > 4)
-            if (n > 4) return f(l, std::integral_constant<int, 8>{});
-        return f(l, std::integral_constant<int, 4>{});
-    };
-    if constexpr (kMost == 4)
-        if (lanes == 512) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
-    return lanes == 64 ? pick(std::integral_constant<int, 64>{}) : pick(std::integral_constant<int, 256>{});
+    if (lanes == 64) return n <= 1 ? f(wave, one) : n <= 2 ? f(wave, two) : f(wave, most);
+    if constexpr (!kForward)
+        if (lanes == 512) return f(std::integral_constant<int, 512>{}, most);
+    if constexpr (kForward)
+        if (n > 4) return f(four, std::integral_constant<int, 8>{});
+    return n <= 1 ? f(four, one) : n <= 2 ? f(four, two) : f(four, most);
 }
 // f(type of x, type of y)
 template <typename F>
@@ -278,10 +288,10 @@ hipError_t with_types(bool x_f32, bool y_f32, F f) {
 
 hipError_t launch_norm(long long M, int D, const void* x, const float* gamma, const float* beta, float eps, void* y, float* stats, bool x_f32,
                        bool y_f32, hipStream_t stream) {
-    const int row_lanes = norm_lanes(M, D);
+    const int row_lanes = norm_lanes(M, D, !x_f32 && !y_f32);
     const unsigned grid = static_cast<unsigned>(row_lanes == 256 ? M : (M + 3) / 4);
     return with_types(x_f32, y_f32, [&](auto xf, auto yf) {
-        return with_items<8>(row_lanes, D / 8, [&](auto lanes, auto count) {
+        return with_items<true>(row_lanes, D / 8, [&](auto lanes, auto count) {
             hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_kernel<decltype(xf)::value, decltype(yf)::value, decltype(lanes)::value, decltype(count)::value>),
                                dim3(grid), dim3(256), 0, stream, M, D / 8, x, gamma, beta, eps, y, reinterpret_cast<float2*>(stats));
             return hipGetLastError();
@@ -302,7 +312,7 @@ hipError_t launch_norm_backward(long long M, int D, const void* x, const float* 
     const int grid = norm_partials(M, D, bf16);
     if (grid > 0) {
         const hipError_t err = with_types(x_f32, y_f32, [&](auto xf, auto yf) {
-            return with_items<4>(row_lanes, D / 8, [&](auto lanes, auto count) {
+            return with_items<false>(row_lanes, D / 8, [&](auto lanes, auto count) {
                 hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_backward_kernel<decltype(xf)::value, decltype(yf)::value, decltype(lanes)::value, decltype(count)::value>),
                                    dim3(grid), dim3(row_lanes < 256 ? 256 : row_lanes), 0, stream, M, D / 8, x, reinterpret_cast<const float2*>(stats), gamma, dy, dx,
                                    dgamma ? partials : nullptr);

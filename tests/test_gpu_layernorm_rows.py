@@ -84,8 +84,8 @@ def check_gradients(x, stats, gamma, dy, dx, dg, db):
 @pytest.mark.parametrize("x_dtype,y_dtype", PAIRS, ids=IDS)
 @pytest.mark.parametrize("D", WIDTHS)
 def test_widths(gpu_device, D, x_dtype, y_dtype):
-    """Seven rows (a workgroup a row from 1024 columns on), and enough for a wave a row."""
-    for M in (7, 1030 if D <= 4096 else 600):
+    """Seven rows, and so many that bf16 rows of up to 2048 columns are a wave's each."""
+    for M in (7, 4099 if D in (1000, 2048) else 1030 if D <= 4096 else 600):
         x, gamma, beta, dy = inputs(D, M, D, x_dtype, y_dtype)
         y, stats = forward(x, gamma, beta, y_dtype)
         check_forward(x, gamma, beta, y, stats)
