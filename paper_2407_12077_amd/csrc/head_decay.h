@@ -48,7 +48,11 @@ struct MixArgs {
 struct MixPlan {
     int segs, seg_len, anchor_len;
 };
-MixPlan plan_mix(int B, int T, int H, bool backward, bool f32_rows);
+// packed_rows: of a call with offsets, else -1; such a call is cut into at most kMixPackedSegments, or as many as
+// the same call of sequences that are all T long.
+constexpr int kMixPackedSegments = 8;
+constexpr int kMixFewUnits = 256;      // calls of as many or more stay whole
+MixPlan plan_mix(int B, int T, int H, long long packed_rows, bool backward, bool f32_rows);
 
 hipError_t launch_mix(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t stream);
 

@@ -664,7 +664,7 @@ __device__ __forceinline__ int index_on_xcd() {
     return x * each + (x < rest ? x : rest) + (blockIdx.x >> 3);
 }
 
-// Index: unit outermost, then segment, then sweep.
+// Index: unit outermost, then segment, then sweep; of packed sequences segment outermost.
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))) void mix_kernel(const MixArgs a) {
     using L = Layout<T, Out, kC, kStates, kSums>;
@@ -674,7 +674,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
     int at = a.offsets ? static_cast<int>(blockIdx.x) : index_on_xcd();
     const int sweep = uniform(at % a.sweeps);
     at /= a.sweeps;
-    const int unit = uniform(at / a.segs), seg = uniform(at - unit * a.segs);
+    const int all_units = a.B * a.H;
+    // (and the segments of a packed call one behind the other: with the units outermost the first ones, which the short sequences have too,
+    // would share few XCDs: 20 x 8000 x 8 in eight 108 -> 98, in sixteen 121 -> 117)
+    const int unit = uniform(a.offsets ? at % all_units : at / a.segs), seg = uniform(a.offsets ? at / all_units : at % a.segs);
     const Sweep w = uniform_sweep(a.sweep[sweep]);
     const Span s = span_of(a, unit, seg);
     if (seg >= s.segs) return;
@@ -911,40 +914,57 @@ hipError_t launch(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t str
 namespace {
 
 // What a call takes in `segs` segments, in microseconds, from what a walk takes for 64 tokens and what memory takes: a compute unit holds one workgroup of
-// a walk with read-outs, two of one for the states alone.
-double modelled(double units, double tokens, int segs, bool backward, bool f32_rows) {
-    const double each = std::ceil(tokens / segs / kMixBlock), walks = units * (backward ? 3 : 1) * segs, load = walks < 256. ? walks / 256. : 1.;
+// a walk with read-outs, two of one for the states alone.  full: sequences that the rows would be if all were `tokens` long, times heads.
+// Packed sequences differ in length, so that short ones run beside the longest; segments that a short one does not have cost
+// their workgroups.
+double modelled(double units, double full, double tokens, int segs, bool packed, bool backward, bool f32_rows) {
+    const double sweeps = backward ? 3 : 1, each = std::ceil(tokens / segs / kMixBlock), walks = full * sweeps * segs, load = walks < 256. ? walks / 256. : 1.;
     const double per = f32_rows ? (backward ? 4.6 : 4.3) + 1.2 * load : (backward ? 1.6 : 1.4) + 0.6 * load;
-    const double stream = units * tokens * (f32_rows ? 256. : 128.) / 4.5e6;         // one read or write of all rows
-    const double whole = std::fmax(std::ceil(walks / 256.) * (5.5 + each * per), (backward ? 11. : 4.) * stream);
+    const double stream = full * tokens * (f32_rows ? 256. : 128.) / 4.5e6;          // one read or write of all rows
+    double whole = std::ceil(walks / 256.) * (5.5 + each * per);
+    double empty = 0.;
+    if (packed) {
+        const double shares = full * sweeps * tokens / kMixBlock / 256.;
+        whole = std::ceil(walks / 256.) * 5.5 + per * (each + std::fmax(0., shares - 0.5 * each)) + 1.6 * std::fmax(0., units * sweeps * segs / 256. - 1.);
+        empty = 0.8 * std::fmax(0., units * (backward ? 2 : 1) * segs / 512. - 1.);
+    }
+    whole = std::fmax(whole, (backward ? 11. : 4.) * stream);
     if (segs == 1) return whole;
-    const double states = std::ceil(units * (backward ? 2 : 1) * (segs - 1) / 512.) * each * (f32_rows ? 2. : 0.72);
+    const double states = std::ceil(full * (backward ? 2 : 1) * (segs - 1) / 512.) * each * (f32_rows ? 2. : 0.72) + empty;
     return whole + 4. + 0.2 * segs + std::fmax(states, (backward ? 4. : 2.) * stream * (segs - 1) / segs);
 }
 
 }  // namespace
 
-MixPlan plan_mix(int B, int T, int H, bool backward, bool f32_rows) {
-    const double units = static_cast<double>(B) * H, tokens = T > 0 ? T : 1;
+MixPlan plan_mix(int B, int T, int H, long long packed_rows, bool backward, bool f32_rows) {
+    const bool packed = packed_rows >= 0;
+    const int longest = packed && packed_rows < T ? static_cast<int>(packed_rows) : T;
+    const double units = static_cast<double>(B) * H, tokens = longest > 0 ? longest : 1;
+    const double full = packed ? std::fmin(units, static_cast<double>(packed_rows) * H / tokens) : units;
     int segs = 1;
     // Pieces are for calls that would leave compute units idle; they read k and v (and r and dout) twice.  Measured, whole / in the planned number of
     // pieces / the best of 1 to 32, us: bf16 1 x 4096 x 32 heads 94.7 / 32.6 (8) / 32.6, 1 x 30000 x 12 659 / 84 (21) / 84 (24), 4 x 2048 x 32 53.2 / 51.0
     // (2) / 51.0; 5 x 4096 x 32 stays whole, 100, where the best cut takes 132 (6).  Gradients: 1 x 4096 x 32 114 / 89.5 (5) / 87.4 (8), 1 x 30000 x 12
     // 754 / 219 (14) / 213 (6); 4 x 2048 x 32 stays whole, 130, against 144 (2).  A modelled gain of under 7 % is left: of 52 sizes and types five are
     // more than 8 % off the best, the furthest 20 %
-    if (units < 256.) {
-        double least = 0.93 * modelled(units, tokens, 1, backward, f32_rows);
-        for (int n = 2; n <= 32 && n * kMixBlock < T + kMixBlock; ++n) {
-            const double us = modelled(units, tokens, n, backward, f32_rows);
+    // Packed, 20 sequences of up to 8000 tokens x 8 heads 173 / 98 (8) / 93 (4), fp32 rows 564 / 244 (8) / 235 (4); 9 x 1531 x 12 37.6 / 29.3 (6) / 28.4 (4),
+    // gradients 51.9 whole against 58 (4), of fp32 rows 128 / 99 (4) / 99; of 40 such sizes and types most are within 8 % of the best, the
+    // furthest 16 %.  With 256 units and more (37 x 2011 x 12 51.6 whole, 67 in two) whole
+    if (units < kMixFewUnits) {
+        const int whole_ones = packed ? plan_mix(B, T, H, -1, backward, f32_rows).segs : 32;
+        const int most = whole_ones > kMixPackedSegments ? whole_ones : kMixPackedSegments;
+        double least = 0.93 * modelled(units, full, tokens, 1, packed, backward, f32_rows);
+        for (int n = 2; n <= most && n * kMixBlock < longest + kMixBlock; ++n) {
+            const double us = modelled(units, full, tokens, n, packed, backward, f32_rows);
             if (us < least) least = us, segs = n;
         }
     }
     MixPlan p;
     const long long each = (static_cast<long long>(tokens) + segs - 1) / segs;
     p.seg_len = static_cast<int>((each + kMixBlock - 1) / kMixBlock * kMixBlock);
-    p.segs = T > 0 ? (T - 1) / p.seg_len + 1 : 1;
-    const int longest = T > 0 ? (T - 1) / kMixBlock * kMixBlock + kMixBlock : kMixBlock;
-    p.anchor_len = longest < 1024 ? longest : 1024;
+    p.segs = longest > 0 ? (longest - 1) / p.seg_len + 1 : 1;
+    const int blocks = T > 0 ? (T - 1) / kMixBlock * kMixBlock + kMixBlock : kMixBlock;
+    p.anchor_len = blocks < 1024 ? blocks : 1024;
     return p;
 }
 

@@ -46,8 +46,8 @@ struct Space {
     long long blocks = 0, locals = 0, sums = 0, anchors = 0, head_sums = 0, floats = 0;
 };
 long long four(long long n) { return (n + 3) / 4 * 4; }
-bool space_of(int B, int T, int H, long long rows, bool backward, bool f32_rows, Space* s) {
-    s->plan = wkv6::plan_mix(B, T, H, backward, f32_rows);
+bool space_of(int B, int T, int H, long long rows, bool packed, bool backward, bool f32_rows, Space* s) {
+    s->plan = wkv6::plan_mix(B, T, H, packed ? rows : -1, backward, f32_rows);
     const long long units = static_cast<long long>(B) * H;
     s->blocks = T > 0 ? (T - 1) / s->plan.anchor_len + 1 : 0;
     if (!wkv6::fits_a_launch(units, wkv6::kMixThreads) || !wkv6::fits_a_launch(units * s->plan.segs * (backward ? 3 : 1), wkv6::kMixThreads) ||
@@ -63,11 +63,20 @@ bool space_of(int B, int T, int H, long long rows, bool backward, bool f32_rows,
     }
     return true;
 }
-// for rows of either type
+// for rows of either type, packed or not.  rows < 0: not known, for packed sequences of as many as may be
 long long workspace_bytes_of(int B, int T, int H, long long rows, bool backward) {
-    Space bf16, f32;
-    if (!space_of(B, T, H, rows, backward, false, &bf16) || !space_of(B, T, H, rows, backward, true, &f32)) return -1;
-    return 4 * (bf16.floats > f32.floats ? bf16.floats : f32.floats);
+    long long most = 0;
+    for (int i = 0; i < 4; ++i) {
+        Space s;
+        if (!space_of(B, T, H, rows < 0 ? 0 : rows, i & 1 && rows >= 0, backward, i & 2, &s)) return -1;
+        if (s.floats > most) most = s.floats;
+    }
+    const long long units = static_cast<long long>(B) * H, pieces = T > 0 ? (T - 1) / wkv6::kMixBlock + 1 : 1;
+    if (rows < 0 && units < wkv6::kMixFewUnits && pieces > 1) {
+        const long long cut = (pieces < wkv6::kMixPackedSegments ? pieces : wkv6::kMixPackedSegments) * units * (kStateFloats + 4);
+        if (cut > most) most = cut;
+    }
+    return 4 * most;
 }
 
 wkv6::MixArgs mix_args(int B, int T, int H, long long rows, const float* g, long long g_stride, const int* offsets, const wkv6::MixPlan& p) {
@@ -85,7 +94,7 @@ extern "C" {
 
 long long wkv6_head_decay_workspace_bytes(int B, int T, int H, int N) {
     if (N != kHeadSize || B < 0 || T < 0 || T > kMaxTokens || H < 1 || H > kMaxHeads) return -1;
-    return B == 0 ? 0 : workspace_bytes_of(B, T, H, 0, false);
+    return B == 0 ? 0 : workspace_bytes_of(B, T, H, -1, false);
 }
 
 long long wkv6_head_decay_backward_workspace_bytes(int B, int T, int H, int N, long long rows) {
@@ -107,7 +116,7 @@ int wkv6_head_decay_prefill(int B, int T, int H, int N, long long rows, const vo
     }
     if (any_misaligned(r, k, v, out, state_in, state_out) || misaligned4(g) || misaligned4(offsets)) return WKV6_ERR_ALIGN;
     Space s;
-    if (!space_of(B, T, H, rows, false, dtype == WKV6_DTYPE_F32, &s)) return WKV6_ERR_SHAPE;
+    if (!space_of(B, T, H, rows, offsets != nullptr, false, dtype == WKV6_DTYPE_F32, &s)) return WKV6_ERR_SHAPE;
     if (s.floats > 0) {
         if (!workspace) return WKV6_ERR_NULL;
         if (misaligned(workspace)) return WKV6_ERR_ALIGN;
@@ -164,7 +173,7 @@ int wkv6_head_decay_backward(int B, int T, int H, int N, long long rows, const v
         misaligned4(dg) || misaligned4(offsets))
         return WKV6_ERR_ALIGN;
     Space s;
-    if (!space_of(B, T, H, rows, true, dtype == WKV6_DTYPE_F32, &s)) return WKV6_ERR_SHAPE;
+    if (!space_of(B, T, H, rows, offsets != nullptr, true, dtype == WKV6_DTYPE_F32, &s)) return WKV6_ERR_SHAPE;
     if (s.floats > 0) {
         if (!workspace) return WKV6_ERR_NULL;
         if (misaligned(workspace)) return WKV6_ERR_ALIGN;

@@ -203,6 +203,24 @@ def test_launches_of_the_mix(fake):
     assert got[5][0].grid[0] == 3 * 256 and all(e.bytes <= 160 * 1024 for ev in got for e in ev)
 
 
+def test_workspace_holds_whatever_the_lengths_are(fake):
+    """A packed call is cut by its rows too, which the prefill's workspace function does not know."""
+    rng = np.random.default_rng(5)
+    calls = []
+    for _ in range(60):
+        B, H, T = int(rng.integers(1, 40)), int(rng.integers(1, 20)), int(2 ** rng.uniform(0, 14))
+        rows, dtype = int(rng.integers(0, B * T + 100)), int(rng.integers(0, 2))
+        for n in (rows, T):
+            name, args = mix_call(B, T, H, dtype, dtype, packed=True)
+            args[4], args[-2] = n, wkv.wkv6_head_decay_workspace_bytes(B, T, H, 64)
+            calls.append((name, args))
+            name, args = back_call(B, T, H, dtype)
+            args[4], args[11], args[-2] = n, lu.at(13), wkv.wkv6_head_decay_backward_workspace_bytes(B, T, H, 64, n)
+            calls.append((name, args))
+    for ev in lu.events(fake, calls):
+        assert [e for e in ev if e.kind == "launch"]
+
+
 def test_first_call_raises_every_limit(fake):
     for first in (mix_call(1, 5, 1), back_call(1, 5, 1, F32)):
         calls = [first, mix_call(8, 300, 32), mix_call(1, 4096, 32, BF16, F32), mix_call(1, 4096, 32, F32, F32), back_call(1, 4096, 32), back_call(1, 4096, 32, F32)]
