@@ -481,6 +481,8 @@ struct Walk {
 #pragma unroll
         for (int j = 0; j < kBlocks; ++j) *inner_at(n, kQ, j0 + j) = acc[j];
     }
+    // One call of form_inner: with a second one (the first chunk ahead of the loop) the compiler merged the two copies' last LDS writes at the loop's
+    // head, and there read a matrix product's accumulators before it had ended
     template <int kQ>
     __device__ __forceinline__ void produce() const {
         lds_barrier();
