@@ -285,6 +285,28 @@ def test_same_bits_from_call_to_call(gpu_device):
     assert all(torch.equal(p, q) for p, q in zip(a, b))
 
 
+def test_rows_past_four_gigabytes(gpu_device):
+    """A hundred tokens at the end of 4.9 GB of projection rows, and their gradients: as those tokens alone."""
+    x = Mix(32, H=32, lengths=[100], fused=True, gradients=True)
+    (out, state), grads = x.prefill(BF16), x.backward()
+    far = Mix(32, H=32, lengths=[100], fused=True, gradients=True)
+    far.rows, at = 400_000, 399_900
+    far.rkv = torch.empty((far.rows, 3, 32, N), dtype=BF16, device="cuda")
+    far.rkv[at:] = x.rkv
+    far.r, far.k, far.v = far.rkv.unbind(1)
+    for name in ("g", "dout"):
+        t = torch.empty((far.rows, *getattr(x, name).shape[1:]), dtype=getattr(x, name).dtype, device="cuda")
+        t[at:] = getattr(x, name)
+        setattr(far, name, t)
+    far.offsets += at
+    out2, state2 = far.prefill(BF16)
+    assert torch.equal(out2[at:], out) and torch.equal(state2, state) and bool((out2[at - 64:at] == 7).all())
+    grads2 = far.backward()
+    for a, b in zip(grads2[:4], grads):
+        assert torch.equal(a[at:], b) and bool((a[at - 64:at] == 7).all())
+    assert torch.equal(grads2[4], grads[4])
+
+
 def test_two_streams_at_once(gpu_device):
     xs = [Mix(41 + i, H=2, B=2, T=700 + 33 * i, gradients=True) for i in range(2)]
     want = [(x.prefill(), x.backward()) for x in xs]

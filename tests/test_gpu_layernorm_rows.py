@@ -135,6 +135,25 @@ def test_no_rows(gpu_device):
     assert bool((dg == 0).all()) and bool((db == 0).all())
 
 
+def test_rows_past_four_gigabytes(gpu_device):
+    M, D = 300_000, 8192
+    x = torch.zeros((M, D), dtype=BF16, device="cuda")
+    few, gamma, beta, dy = inputs(9, 600, D, BF16, BF16)
+    x[-600:] = few
+    y, stats = forward(x, gamma, beta, BF16)
+    want, want_stats = forward(few, gamma, beta, BF16)
+    assert torch.equal(y[-600:], want) and torch.equal(stats[-600:], want_stats)
+    y.zero_()
+    y[-600:] = dy                                              # a gradient of nought for the rows before
+    got = gradients(x, stats, gamma, y)
+    want = gradients(few, want_stats, gamma, dy)
+    assert torch.equal(got[0][-600:], want[0]) and not bool(got[0][:-600].any())
+    # other shares of the columns' sums: 24 roundings of each term more
+    u = (few.float() - want_stats[:, :1]) * want_stats[:, 1:]
+    assert bool(((got[1] - want[1]).abs() <= 64 * STEP * (dy.float() * u).abs().sum(0)).all())
+    assert bool(((got[2] - want[2]).abs() <= 64 * STEP * dy.float().abs().sum(0)).all())
+
+
 def test_gradients_against_differences(gpu_device):
     x, gamma, beta, dy = inputs(7, 9, 200, F32, F32)
     _, stats = forward(x, gamma, beta, F32)
