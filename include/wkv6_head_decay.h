@@ -21,7 +21,8 @@
  *   r, k, v       [rows][H][N], rows token_stride ELEMENTS apart (at least H N, at most 2^22; rows a multiple of 16 bytes): they may be
  *                 parts of one tensor [rows][3][H][N], as one projection leaves them.  dr, dk, dv likewise, with the same stride
  *   g             [rows][H] fp32, rows g_stride elements apart (at least H), or one decay a head for all tokens: [H] with g_stride = 0.
- *                 Meant for g <= 0; -inf (forget everything) is taken as -128, whose exponential is nothing in fp32.
+ *                 Meant for g <= 0, but a finite g above nought (states grow) is taken as it is, as far as states stay inside fp32's range;
+ *                 -inf (forget everything) is taken as -128, whose exponential is nothing in fp32.
  *   state_in      [B][H][N][N] fp32, NULL means zero.  state_out the same, NULL means "do not write"; it may equal state_in
  *   out, dout     [rows][H][N]
  * Device pointers, 16-byte aligned but for g, dg and offsets (4); `out` and the gradients must not alias any input.

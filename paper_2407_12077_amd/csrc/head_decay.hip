@@ -433,7 +433,8 @@ struct Walk {
             if ((lane & 15) == 0) d.block[lane >> 4] = exp2_near(block);
             // S + (w - 1) S has one rounding of the size of S where w S has two: with a decay near one, and the same in every chunk, these
             // would add up over the chunks that the state remembers
-            if (lane == 0) d.less[0] = all > -0.5f ? exp2_less_1(all) : exp2_near(all) - 1.f;
+            // (the series holds up to a half, on both sides: sums of g above nought are larger too)
+            if (lane == 0) d.less[0] = fabsf(all) < 0.5f ? exp2_less_1(all) : exp2_near(all) - 1.f;
         }
     }
 
