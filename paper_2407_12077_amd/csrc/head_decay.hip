@@ -186,7 +186,7 @@ struct Decays {
     float in_chunk[kC];                // from the chunk's first token to this
     float to_chunk[kC];                // from behind this token to the chunk's end; nought for tokens that are not there
     float block[kC / 16];              // of whole blocks
-    float less[4];                     // of the whole chunk, less one (one value)
+    float whole[4];                    // of the whole chunk, as keep + rest (two values): see form_decays
 };
 
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
@@ -432,9 +432,12 @@ struct Walk {
             d.to_chunk[lane] = there ? exp2_near(behind + after) : 0.f;
             if ((lane & 15) == 0) d.block[lane >> 4] = exp2_near(block);
             // S + (w - 1) S has one rounding of the size of S where w S has two: with a decay near one, and the same in every chunk, these
-            // would add up over the chunks that the state remembers
-            // (the series holds up to a half, on both sides: sums of g above nought are larger too)
-            if (lane == 0) d.less[0] = fabsf(all) < 0.5f ? exp2_less_1(all) : exp2_near(all) - 1.f;
+            // would add up over the chunks that the state remembers.  A w far from one is taken as it is: w - 1 would keep only what it has above 2^-25
+            if (lane == 0) {
+                const bool near_one = fabsf(all) < 0.5f;
+                d.whole[0] = near_one ? 1.f : 0.f;
+                d.whole[1] = near_one ? exp2_less_1(all) : exp2_near(all);
+            }
         }
     }
 
@@ -513,7 +516,7 @@ struct Walk {
         E::column(tile + L::kTile, 16 * wave, l16, g4, v);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) to_chunk[b] = *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]);
-        const float less = d.less[0];
+        const float keep = d.whole[0], rest = d.whole[1];
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (!kStates) {
             typename E::template Fine<L::kOutTerms> st[4];
@@ -539,7 +542,7 @@ struct Walk {
         typename E::template Fine<L::kStateTerms> vd[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) vd[b] = E::template fine<L::kStateTerms>(E::floats(v[b]) * to_chunk[b]);
-        if constexpr (kStates) total = fmaf(total, less, total);
+        if constexpr (kStates) total = fmaf(total, rest, total * keep);
         if constexpr (!kStates) {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -548,7 +551,8 @@ struct Walk {
         float4v sum[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            state[i] += state[i] * less;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) state[i][e] = fmaf(state[i][e], rest, state[i][e] * keep);      // (times one or nought: exact)
             // fp32 rows: the chunk's own sum first, eight roundings of its size, and one of the state's, which is the larger with long memories
             if constexpr (E::kSize == 4) sum[i] = float4v{0.f, 0.f, 0.f, 0.f};
             else sum[i] = state[i];
