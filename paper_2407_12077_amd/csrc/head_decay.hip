@@ -548,15 +548,10 @@ struct Walk {
             for (int b = 0; b < kBlocks; ++b)
                 *inner_at(n, b, wave) = inner[b] + o[b] * in_chunk[b];
         }
+        // what the chunk changes of the state first, whose roundings are of its size, and one of the state's, which is the larger with long memories
         float4v sum[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) state[i][e] = fmaf(state[i][e], rest, state[i][e] * keep);      // (times one or nought: exact)
-            // fp32 rows: the chunk's own sum first, eight roundings of its size, and one of the state's, which is the larger with long memories
-            if constexpr (E::kSize == 4) sum[i] = float4v{0.f, 0.f, 0.f, 0.f};
-            else sum[i] = state[i];
-        }
+        for (int i = 0; i < 4; ++i) sum[i] = state[i] * rest;
 #pragma unroll
         for (int b = 0; b < kBlocks; b += 2)
 #pragma unroll
@@ -564,10 +559,9 @@ struct Walk {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] = E::mul(k[i][b], k[i][b + 1], E::term(vd[b], t), E::term(vd[b + 1], t), sum[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (E::kSize == 4) state[i] += sum[i];
-            else state[i] = sum[i];
-        }
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) state[i][e] = fmaf(state[i][e], keep, sum[i][e]);      // times one or nought
     }
 
     // kSums: a mover's rows that the read-outs are multiplied with, laid out like its stores

@@ -1,0 +1,48 @@
+"""How many bits the head-decay time mix keeps: root mean squares of errors against 64 bits, beside those of the results.
+
+The bounds of tests/operator_util.py hold for every element and assume that all roundings fall the same way; these take them as they fall.  A rounding
+is at most half a step, 2^-24, evenly spread: 2^-24 / sqrt(3) at most as a root mean square.  A state with a decay w a token is rounded once a
+chunk of C = 64 tokens (32 of fp32 rows) and remembers M = 1 / (1 - w^(2 C)) of these in quadrature: sqrt(M / 3) steps.  Three steps more: the factor
+log2 e of a decay that is the same for all tokens and the decay's own factor, which fall the same way in every chunk, and a chunk's own sum, whose
+roundings are of its size."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_12077_amd as wkv
+from operator_util import N, Mix
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+STEP = 2.0 ** -24
+
+
+def rms(t):
+    return float(t.double().square().mean().sqrt())
+
+
+def walk(x, last=0):
+    """The state behind a whole call's tokens, and the read-outs of the last ones, in 64 bits on the GPU."""
+    r, k, v = (t.view(x.B, x.T, x.H, N) for t in (x.r, x.k, x.v))
+    w = torch.exp(x.g.double())
+    w = w.expand(x.B, x.T, x.H) if x.decay == "head" else w.view(x.B, x.T, x.H)
+    S = torch.zeros((x.B, x.H, N, N), dtype=torch.float64, device="cuda") if x.state_in is None else x.state_in.double()
+    out = []
+    for t in range(x.T):
+        S = w[:, t, :, None, None] * S + k[:, t].double()[..., None] * v[:, t].double()[:, :, None]
+        if t >= x.T - last:
+            out.append((r[:, t].double()[..., None] * S).sum(2))
+    return S, torch.stack(out, 1) if out else None
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B,T", [(64, 4096)], ids=["whole"])
+def test_states_with_long_memories(gpu_device, B, T, dtype):
+    x = Mix(3, H=4, B=B, T=T, dtype=dtype, decay="head", state=False)
+    x.g.copy_(torch.log1p(-torch.exp2(-torch.tensor([9., 10., 11., 12.], device="cuda", dtype=torch.float64))).float())
+    _, state = x.prefill()
+    want, _ = walk(x)
+    for h in range(4):
+        M = 1 / (1 - math.exp(2 * (64 if dtype == BF16 else 32) * float(x.g[h])))
+        assert rms(state[:, h].double() - want[:, h]) <= STEP * (math.sqrt(M / 3) + 3) * rms(want[:, h]), h
