@@ -24,7 +24,7 @@ struct Sweep {
     const float* state_in = nullptr;   // [B][H][64][64]; null: zeros
     float* state_out = nullptr;        // null: not written
     float* locals = nullptr;           // states of the segments from zero, [segment][unit][64][64], and behind them
-                                       // their total decays [segment][unit]
+                                       // their total decays [segment][unit], two floats each
     float* anchors = nullptr;          // [unit][block][4096] the states at blocks of anchor_len tokens: behind the block's last token,
                                        // in reverse in front of it; a private order
     bool reverse = false;

@@ -176,6 +176,23 @@ constexpr int kDecayPlaces = 3;        // for a chunk's decays: being formed, th
 constexpr int kStreamed = 2;             // cache policy of the read-outs, non-temporal: prefill 8 x 4096 x 32 117.7 -> 115.6 us, its gradients 390 -> 384
 constexpr float kLowest = -128.f;      // exp(-128) is nothing beside the smallest fp32 value: -inf is taken as this
 
+// A decay of many tokens, keep + rest, keep one or nought.  S + (w - 1) S has one rounding of the size of S where w S has two, w's and its own: with a
+// decay near one, and the same every time, these would add up over what the state remembers.  A w far from one is taken as it is: w - 1 would keep
+// only what it has above 2^-25
+struct Factor {
+    float keep, rest;
+    __device__ __forceinline__ float4v times(float4v s, float4v add) const {       // w s + add, the change first
+        const float4v change = s * rest + add;
+        return s * keep + change;
+    }
+    __device__ __forceinline__ Factor then(Factor f) const {
+        const float less = fmaf(rest, f.rest, rest) + f.rest;                       // of the product less one, if both are near it
+        const bool both = keep * f.keep != 0.f, near_one = both && fabsf(less) < 0.5f;
+        const float far = both ? 1.f + less : (keep + rest) * (f.keep + f.rest);
+        return {near_one ? 1.f : 0.f, near_one ? less : far};
+    }
+};
+
 // A chunk's decays by token, in LDS.  In logarithms to base 2 (high, low) or as factors (the others)
 template <int kC>
 struct Decays {
@@ -186,7 +203,7 @@ struct Decays {
     float in_chunk[kC];                // from the chunk's first token to this
     float to_chunk[kC];                // from behind this token to the chunk's end; nought for tokens that are not there
     float block[kC / 16];              // of whole blocks
-    float whole[4];                    // of the whole chunk, as keep + rest (two values): see form_decays
+    float whole[4];                    // of the whole chunk: a Factor (two values)
 };
 
 template <typename T, typename Out, int kC, bool kStates, bool kSums>
@@ -333,7 +350,7 @@ struct Walk {
     const int lane, wave, l16, g4;                              // wave of its part
     const int first_chunk, chunks;                              // of the segment
     float4v state[4];                                           // consumers: S[16 i + 4 g4 + e][16 wave + l16]
-    float total = 1.f;                                          // kStates: decay of all chunks so far
+    Factor total = {1.f, 0.f};                                  // kStates: decay of all chunks so far
 
     // token of the chunk's first place, by the chunk's number on the walk
     __device__ __forceinline__ int chunk_token(int n) const { return (first_chunk + (w.reverse ? chunks - 1 - n : n)) * kC; }
@@ -431,8 +448,6 @@ struct Walk {
             d.in_chunk[lane] = exp2_near(before + pre);
             d.to_chunk[lane] = there ? exp2_near(behind + after) : 0.f;
             if ((lane & 15) == 0) d.block[lane >> 4] = exp2_near(block);
-            // S + (w - 1) S has one rounding of the size of S where w S has two: with a decay near one, and the same in every chunk, these
-            // would add up over the chunks that the state remembers.  A w far from one is taken as it is: w - 1 would keep only what it has above 2^-25
             if (lane == 0) {
                 const bool near_one = fabsf(all) < 0.5f;
                 d.whole[0] = near_one ? 1.f : 0.f;
@@ -516,7 +531,7 @@ struct Walk {
         E::column(tile + L::kTile, 16 * wave, l16, g4, v);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) to_chunk[b] = *reinterpret_cast<const float4v*>(&d.to_chunk[16 * b + 4 * g4]);
-        const float keep = d.whole[0], rest = d.whole[1];
+        const Factor whole = {d.whole[0], d.whole[1]};
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (!kStates) {
             typename E::template Fine<L::kOutTerms> st[4];
@@ -542,7 +557,7 @@ struct Walk {
         typename E::template Fine<L::kStateTerms> vd[kBlocks];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) vd[b] = E::template fine<L::kStateTerms>(E::floats(v[b]) * to_chunk[b]);
-        if constexpr (kStates) total = fmaf(total, rest, total * keep);
+        if constexpr (kStates) total = total.then(whole);
         if constexpr (!kStates) {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -551,7 +566,7 @@ struct Walk {
         // what the chunk changes of the state first, whose roundings are of its size, and one of the state's, which is the larger with long memories
         float4v sum[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = state[i] * rest;
+        for (int i = 0; i < 4; ++i) sum[i] = state[i] * whole.rest;
 #pragma unroll
         for (int b = 0; b < kBlocks; b += 2)
 #pragma unroll
@@ -561,7 +576,7 @@ struct Walk {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) state[i][e] = fmaf(state[i][e], keep, sum[i][e]);      // times one or nought
+            for (int e = 0; e < 4; ++e) state[i][e] = fmaf(state[i][e], whole.keep, sum[i][e]);
     }
 
     // kSums: a mover's rows that the read-outs are multiplied with, laid out like its stores
@@ -765,7 +780,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
         return;
     }
 
-    float* const totals = w.locals + a.segs * units * kStateFloats + unit;
+    Factor* const totals = reinterpret_cast<Factor*>(w.locals + a.segs * units * kStateFloats) + unit;
 #pragma unroll
     for (int i = 0; i < 4; ++i) walk.state[i] = float4v{0.f, 0.f, 0.f, 0.f};
     if constexpr (!kStates) {
@@ -775,7 +790,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
         constexpr int kAtOnce = 4;                              // asked for together
         for (int x0 = 0; x0 < count; x0 += kAtOnce) {
             float4v add[kAtOnce][4];
-            float decay[kAtOnce];
+            Factor decay[kAtOnce];
 #pragma unroll
             for (int x = 0; x < kAtOnce; ++x) {
                 const int from = x0 + x < count ? x0 + x : count - 1, other = w.reverse ? s.segs - 1 - from : from;
@@ -786,7 +801,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
             for (int x = 0; x < kAtOnce; ++x)
                 if (x0 + x < count)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) walk.state[i] = walk.state[i] * decay[x] + add[x][i];
+                    for (int i = 0; i < 4; ++i) walk.state[i] = decay[x].times(walk.state[i], add[x][i]);
         }
     }
     if (chunks > 0) {

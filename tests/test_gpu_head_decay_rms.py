@@ -37,7 +37,7 @@ def walk(x, last=0):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-@pytest.mark.parametrize("B,T", [(64, 4096)], ids=["whole"])
+@pytest.mark.parametrize("B,T", [(64, 4096), (1, 6000)], ids=["whole", "pieces"])
 def test_states_with_long_memories(gpu_device, B, T, dtype):
     x = Mix(3, H=4, B=B, T=T, dtype=dtype, decay="head", state=False)
     x.g.copy_(torch.log1p(-torch.exp2(-torch.tensor([9., 10., 11., 12.], device="cuda", dtype=torch.float64))).float())
