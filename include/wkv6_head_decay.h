@@ -69,7 +69,7 @@ int wkv6_head_decay_decode(int B, int H, int N,
  * State and read-outs are formed again from the inputs; nothing has to be kept from the forward call.
  *   dg   [rows][H] fp32, or [H] with g_stride = 0: then summed over all tokens
  *        A g that stands for -inf (below -128) gets the gradient of the value that it is taken as: nought but for rounding.
- * Results are the same bits from call to call.  With T = 0 or rows = 0, dg of g_stride = 0 is nought.
+ * Results are the same bits from call to call.  With B = 0, T = 0 or rows = 0, dg of g_stride = 0 is nought.
  */
 int wkv6_head_decay_backward(int B, int T, int H, int N, long long rows,
                              const void *r, const void *k, const void *v, long long token_stride,

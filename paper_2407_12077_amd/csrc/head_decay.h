@@ -64,6 +64,9 @@ hipError_t launch_mix_locals(const MixArgs& a, int count, bool f32_rows, hipStre
 hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const float* k_sums, const float* behind, const float* front,
                                  float* head_sums, float* dg, hipStream_t stream);
 
+// dg [H] of one decay a head from `count` rows of partial sums [H]; none: nought.
+hipError_t launch_head_sums(long long count, int H, const float* head_sums, float* dg, hipStream_t stream);
+
 // Raises the dynamic LDS limits of all of these, without launching.
 hipError_t raise_mix_limits();
 

@@ -1017,8 +1017,11 @@ hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const fl
         hipLaunchKernelGGL(decay_gradient_kernel, dim3(static_cast<unsigned>(count * a.H)), dim3(256), 0, stream, a, blocks, r_sums, k_sums,
                            behind, front, head_sums, dg);
     const hipError_t err = hipGetLastError();
-    if (err != hipSuccess || !head_sums) return err;
-    hipLaunchKernelGGL(head_sums_kernel, dim3(static_cast<unsigned>(a.H)), dim3(64), 0, stream, count, a.H, head_sums, dg);
+    return err != hipSuccess || !head_sums ? err : launch_head_sums(count, a.H, head_sums, dg, stream);
+}
+
+hipError_t launch_head_sums(long long count, int H, const float* head_sums, float* dg, hipStream_t stream) {
+    hipLaunchKernelGGL(head_sums_kernel, dim3(static_cast<unsigned>(H)), dim3(64), 0, stream, count, H, head_sums, dg);
     return hipGetLastError();
 }
 

@@ -163,7 +163,10 @@ int wkv6_head_decay_backward(int B, int T, int H, int N, long long rows, const v
                              int dtype, void* workspace, long long workspace_bytes, void* stream) {
     int status = check_mix(B, T, H, N, rows, offsets != nullptr, dtype, dtype);
     if (status != WKV6_OK) return status;
-    if (B == 0) return WKV6_OK;
+    if (B == 0) {                                              // no sequence: but the sum over no tokens is nought
+        if (!dg || g_stride != 0) return WKV6_OK;
+        return misaligned4(dg) ? WKV6_ERR_ALIGN : status_of(wkv6::launch_head_sums(0, H, nullptr, dg, static_cast<hipStream_t>(stream)));
+    }
     if (rows > 0 && T > 0) {
         if (any_null(r, k, v, g, dout, dr, dk, dv, dg)) return WKV6_ERR_NULL;
         status = check_strides(H, token_stride, g_stride, dtype);

@@ -1,0 +1,40 @@
+"""Calls of the head-decay time mix at the edges of what its header allows, without a GPU: what they launch (tests/launch_util.py) and what they refuse."""
+import ctypes
+
+import pytest
+
+import launch_util as lu
+from paper_2407_12077_amd import binding
+
+OK, NULL, SHAPE, UNSUPPORTED, LAUNCH, ALIGN, WORKSPACE = range(7)
+BF16, F32 = 0, 1
+BIG = 1 << 50
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    return lu.build_fake(tmp_path_factory.mktemp("fake_hip"))
+
+
+def launches(fake, calls):
+    return [[e for e in ev if e.kind == "launch"] for ev in lu.events(fake, calls)]
+
+
+def backward(B, T, H, rows, g_stride=None, packed=False, dtype=BF16, dg=lu.at(10), workspace_bytes=BIG):
+    return ("wkv6_head_decay_backward", [B, T, H, 64, rows, lu.at(0), lu.at(1), lu.at(2), H * 64, lu.at(3), H if g_stride is None else g_stride,
+                                         lu.at(13) if packed else None, lu.at(4), lu.at(5), lu.at(6), lu.at(7), lu.at(8), lu.at(9), dg, lu.at(11), dtype,
+                                         lu.at(12), workspace_bytes, None])
+
+
+def status(call):
+    name, args = call
+    return getattr(binding.load(), name)(*[ctypes.c_void_p(a) if isinstance(a, int) and a >= 1 << 36 and a != BIG else a for a in args])
+
+
+def test_gradient_of_a_head_s_decay_with_no_sequence_is_written(fake):
+    """dg [H] is a sum over no tokens: nought, not what was there before."""
+    got = launches(fake, [backward(0, 0, 3, 0, g_stride=0), backward(0, 8, 3, 0, g_stride=0), backward(0, 8, 3, 5, g_stride=0, packed=True),
+                          backward(0, 8, 3, 0), backward(0, 8, 3, 0, g_stride=0, dg=None)])
+    assert [[e.base for e in ev] for ev in got] == [["head_sums_kernel"]] * 3 + [[], []]
+    assert got[0][0].grid[0] == 3
+    assert status(backward(0, 0, 3, 0, g_stride=0, dg=lu.at(10, 2))) == ALIGN
