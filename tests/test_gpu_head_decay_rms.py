@@ -46,3 +46,18 @@ def test_states_with_long_memories(gpu_device, B, T, dtype):
     for h in range(4):
         M = 1 / (1 - math.exp(2 * (64 if dtype == BF16 else 32) * float(x.g[h])))
         assert rms(state[:, h].double() - want[:, h]) <= STEP * (math.sqrt(M / 3) + 3) * rms(want[:, h]), h
+
+
+@pytest.mark.parametrize("g", [-0.02, -0.3])
+def test_the_factor_of_the_first_token(gpu_device, g):
+    """With queries and read-outs' gradients of nought dstate_in is exp(g) dstate_out: four logarithms near g.  The factor: half a step of its exponent, X = g log2 e,
+    which is X ln 2 steps of its value and falls as it does; its own, evenly spread; and the series' 2^-25 at the most.  The product: a rounding."""
+    x = Mix(6, H=4, B=512, T=1, dtype=F32, gradients=True)
+    x.g.copy_(g * (1 + torch.rand((512, 4), device="cuda", generator=torch.Generator("cuda").manual_seed(1)) / 4))
+    x.r.zero_()
+    x.dout.zero_()
+    got = x.backward()[4].double()
+    want = torch.exp(x.g.double())[:, :, None, None] * x.dstate_out.double()
+    error = (got - want) / want
+    assert rms(error) <= STEP * math.sqrt(((1.25 * g) ** 2 + 2) / 3 + 0.25)
+    assert float(error.abs().max()) <= STEP * (1.25 * abs(g) + 2.5)
