@@ -237,15 +237,6 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// Accumulators on their way into LDS: twelve wait states between the matrix products and whatever reads them behind this, more than the longest product
-// here needs (eight passes, ten states).  The compiler puts such states in as well, but counts them along its own final order of blocks.
-template <int kCount>
-__device__ __forceinline__ void settle(float4v (&acc)[kCount]) {
-    static_assert(kCount == 2 || kCount == 4, "blocks of tokens in a chunk");
-    if constexpr (kCount == 2) asm volatile("s_nop 11" : "+v"(acc[0]), "+v"(acc[1]));
-    else asm volatile("s_nop 11" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
-}
-
 // A value that is the same in all lanes, in a scalar register: what depends on the kernel's argument or on memory through a computed
 // index is not known to be, and a descriptor of such would be read lane by lane.
 template <typename V>
@@ -506,12 +497,9 @@ struct Walk {
             for (int i = L::kOutTerms - 1; i >= 0; --i)
 #pragma unroll
                 for (int j = 0; j < kBlocks; ++j) acc[j] = E::mul(v[j][kb], v[j][kb + 1], E::term(p[kb], i), E::term(p[kb + 1], i), acc[j]);
-        settle(acc);
 #pragma unroll
         for (int j = 0; j < kBlocks; ++j) *inner_at(n, kQ, j0 + j) = acc[j];
     }
-    // One call of form_inner: with a second one (the first chunk ahead of the loop) a compiler has merged the two copies' last LDS writes at the
-    // loop's head, too near behind the products; settle() holds wherever they go
     template <int kQ>
     __device__ __forceinline__ void produce() const {
         lds_barrier();

@@ -29,16 +29,16 @@ def functions(listing):
 
 
 def early_lds_writes(program, labels, states):
-    """[(line of a product, line of the LDS write, states between)] with fewer than `states` between them."""
+    """[(line of a product, line of the LDS write, states between)] with fewer than states[product] between them."""
     early = []
     for i, (line, text) in enumerate(program):
         if not text.startswith("v_mfma"):
             continue
-        result = registers(text.split(",")[0])
+        result, needed = registers(text.split(",")[0]), states[text.split()[0]]
         paths, seen = [(i + 1, 0, result)], set()
         while paths:
             at, waited, live = paths.pop()
-            while at < len(program) and waited < states and live and (at, waited) not in seen:
+            while at < len(program) and waited < needed and live and (at, waited) not in seen:
                 seen.add((at, waited))
                 number, now = program[at]
                 op, _, rest = now.partition(" ")
