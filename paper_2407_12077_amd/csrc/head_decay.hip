@@ -243,7 +243,14 @@ template <typename V>
 __device__ __forceinline__ V uniform(V v) {
     if constexpr (sizeof(V) == 8) {
         const uint2v u = __builtin_bit_cast(uint2v, v);
-        return __builtin_bit_cast(V, uint2v{static_cast<unsigned>(__builtin_amdgcn_readfirstlane(u.x)), static_cast<unsigned>(__builtin_amdgcn_readfirstlane(u.y))});
+        const uint2v same = {static_cast<unsigned>(__builtin_amdgcn_readfirstlane(u.x)), static_cast<unsigned>(__builtin_amdgcn_readfirstlane(u.y))};
+        if constexpr (std::is_pointer_v<V>) {
+            // device memory, which the compiler no longer sees: behind flat accesses it waits for all of a wave's LDS reads where it needs one
+            typedef __attribute__((address_space(1))) std::remove_pointer_t<V>* Global;
+            return (V)__builtin_bit_cast(Global, same);
+        } else {
+            return __builtin_bit_cast(V, same);
+        }
     } else {
         return static_cast<V>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
     }
