@@ -25,7 +25,7 @@ struct Sweep {
     float* state_out = nullptr;        // null: not written
     float* locals = nullptr;           // states of the segments from zero, [segment][unit][64][64], and behind them
                                        // their total decays [segment][unit], two floats each
-    float* anchors = nullptr;          // [unit][block][4096] the states at blocks of anchor_len tokens: behind the block's last token,
+    float* anchors = nullptr;          // [place][head][4096] the states at blocks of anchor_len tokens: behind the block's last token,
                                        // in reverse in front of it; a private order
     bool reverse = false;
     bool turned = false;               // state_in and state_out hold S[value][key],
@@ -39,15 +39,22 @@ struct MixArgs {
     long long g_row;                   // floats from token to token, 0: one decay a head
     const int* offsets;                // [B + 1] or null: B sequences of T rows
     int segs, seg_len;                 // a sequence's segments; seg_len is a multiple of kMixBlock
-    int anchor_len;
+    int anchor_len, blocks;            // blocks: of the longest sequence
+    int whole_places;                  // anchors' places by rows: see MixPlan; -1: by sequence and block
     int sweeps;
     Sweep sweep[3];
 };
 
-// How the token axis is cut: segs segments of seg_len tokens; anchors every anchor_len tokens.  Multiples of kMixBlock.
+// How the token axis is cut: segs segments of seg_len tokens; anchors every anchor_len tokens, at most `blocks` in a sequence.  Multiples of kMixBlock.
+// The anchors of a head have `places` places.  A packed call whose sequences differ in length would leave most of B x blocks empty.  There a
+// sequence's last block has a place of its own, whole_places + the sequence, and a block in front of it the place first row / anchor_len, below
+// whole_places = rows / anchor_len: such blocks are anchor_len rows long, so no two of them that share no row start between the same multiples.
 struct MixPlan {
-    int segs, seg_len, anchor_len;
+    int segs, seg_len, anchor_len, blocks;
+    int whole_places;
+    long long places;
 };
+constexpr int kDecayGradientThreads = 256;
 // packed_rows: of a call with offsets, else -1; such a call is cut into at most kMixPackedSegments, or as many as
 // the same call of sequences that are all T long.
 constexpr int kMixPackedSegments = 8;

@@ -299,6 +299,19 @@ __device__ __forceinline__ Span span_of(const MixArgs& a, int unit, int seg) {
     return s;
 }
 
+// The places of a sequence's anchors
+struct Anchors {
+    int last, last_place, first_place;                          // its last block, its place, and that of the first block if it is another one
+    __device__ __forceinline__ Anchors(const MixArgs& a, const Span& s)
+        : last((s.len - 1) / a.anchor_len),
+          last_place(a.whole_places < 0 ? s.b * a.blocks + last : a.whole_places + s.b),
+          first_place(a.whole_places < 0 ? s.b * a.blocks : static_cast<int>(s.first) / a.anchor_len) {}
+    __device__ __forceinline__ float4v* of(const float* anchors, int block, const MixArgs& a, const Span& s) const {
+        const long long place = block == last ? last_place : first_place + block;
+        return reinterpret_cast<float4v*>(const_cast<float*>(anchors)) + (place * a.H + s.h) * (kHeadSize * kHeadSize / 4);
+    }
+};
+
 // exp of a log-decay from memory
 __device__ __forceinline__ float decay_factor(float g) {
     g = g < kLowest ? kLowest : g;                              // (NaN stays)
@@ -669,9 +682,7 @@ struct Walk {
     __device__ __forceinline__ void keep_anchor(int n) const {
         const int end = chunk_token(n) + kC;
         if (end % a.anchor_len != 0 && end < s.len) return;
-        const int blocks = (a.T - 1) / a.anchor_len + 1;
-        float4v* to = reinterpret_cast<float4v*>(w.anchors) +
-                      ((static_cast<long long>(s.b) * a.H + s.h) * blocks + (end - 1) / a.anchor_len) * (kHeadSize * kHeadSize / 4) + threadIdx.x;
+        float4v* to = Anchors(a, s).of(w.anchors, (end - 1) / a.anchor_len, a, s) + threadIdx.x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i * 256] = state[i];
     }
@@ -834,13 +845,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
 // for any a >= t; dS_{a+1} is the gradient of the state behind token a + 1, and behind the last token that of state_out.  The sums nearly
 // cancel, so a is the end of t's block of anchor_len tokens and not of the sequence, and they are taken in 64 bits.
 // A workgroup per unit and block.  14 us of the 8 x 4096 x 32 gradients' 400: 24 MB, and 256 tokens at a time in series.
-__global__ __launch_bounds__(256) void decay_gradient_kernel(const MixArgs a, int blocks, const float* r_sums, const float* k_sums,
+__global__ __launch_bounds__(kDecayGradientThreads) void decay_gradient_kernel(const MixArgs a, const float* r_sums, const float* k_sums,
                                                              const float* behind, const float* front, float* head_sums, float* dg) {
     __shared__ double part[4];
     int at = index_on_xcd();
     const int h = at % a.H;
     at /= a.H;
-    const int b = at / blocks, block = at - b * blocks;
+    const int blocks = a.blocks, b = at / blocks, block = at - b * blocks;
     const int unit = b * a.H + h;
     const Span s = span_of(a, unit, 0);
     const int t0 = block * a.anchor_len, t1 = t0 + a.anchor_len < s.len ? t0 + a.anchor_len : s.len;
@@ -849,9 +860,8 @@ __global__ __launch_bounds__(256) void decay_gradient_kernel(const MixArgs a, in
         if (head_sums && threadIdx.x == 0) head_sums[(static_cast<long long>(b) * blocks + block) * a.H + h] = 0.f;
         return;
     }
-    const long long place = (static_cast<long long>(unit) * blocks + block) * (kStateFloats / 4);
-    const float4v* x = reinterpret_cast<const float4v*>(behind) + place;
-    const float4v* y = reinterpret_cast<const float4v*>(front) + place;
+    const Anchors anchors(a, s);
+    const float4v *x = anchors.of(behind, block, a, s), *y = anchors.of(front, block, a, s);
     double dot = 0.;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -984,8 +994,15 @@ MixPlan plan_mix(int B, int T, int H, long long packed_rows, bool backward, bool
     const long long each = (static_cast<long long>(tokens) + segs - 1) / segs;
     p.seg_len = static_cast<int>((each + kMixBlock - 1) / kMixBlock * kMixBlock);
     p.segs = longest > 0 ? (longest - 1) / p.seg_len + 1 : 1;
-    const int blocks = T > 0 ? (T - 1) / kMixBlock * kMixBlock + kMixBlock : kMixBlock;
-    p.anchor_len = blocks < 1024 ? blocks : 1024;
+    const int padded = longest > 0 ? (longest - 1) / kMixBlock * kMixBlock + kMixBlock : kMixBlock;
+    p.anchor_len = padded < 1024 ? padded : 1024;
+    p.blocks = longest > 0 ? (longest - 1) / p.anchor_len + 1 : 0;
+    p.places = static_cast<long long>(B) * p.blocks;
+    p.whole_places = -1;
+    if (packed && p.blocks > 0 && packed_rows / p.anchor_len + B < p.places) {
+        p.whole_places = static_cast<int>(packed_rows / p.anchor_len);
+        p.places = static_cast<long long>(p.whole_places) + B;
+    }
     return p;
 }
 
@@ -1016,11 +1033,10 @@ hipError_t launch_mix_locals(const MixArgs& a, int count, bool f32_rows, hipStre
 
 hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const float* k_sums, const float* behind, const float* front,
                                  float* head_sums, float* dg, hipStream_t stream) {
-    const int blocks = a.T > 0 ? (a.T - 1) / a.anchor_len + 1 : 0;
-    const long long count = static_cast<long long>(a.B) * blocks;
+    const long long count = static_cast<long long>(a.B) * a.blocks;
     if (count > 0)
-        hipLaunchKernelGGL(decay_gradient_kernel, dim3(static_cast<unsigned>(count * a.H)), dim3(256), 0, stream, a, blocks, r_sums, k_sums,
-                           behind, front, head_sums, dg);
+        hipLaunchKernelGGL(decay_gradient_kernel, dim3(static_cast<unsigned>(count * a.H)), dim3(kDecayGradientThreads), 0, stream, a, r_sums,
+                           k_sums, behind, front, head_sums, dg);
     const hipError_t err = hipGetLastError();
     return err != hipSuccess || !head_sums ? err : launch_head_sums(count, a.H, head_sums, dg, stream);
 }

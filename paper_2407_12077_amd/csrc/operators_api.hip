@@ -43,32 +43,33 @@ int check_strides(int H, long long token_stride, long long g_stride, int dtype) 
 // Workspace in floats, every part a multiple of four; false where the launches would not fit.
 struct Space {
     wkv6::MixPlan plan;
-    long long blocks = 0, locals = 0, sums = 0, anchors = 0, head_sums = 0, floats = 0;
+    long long locals = 0, sums = 0, anchors = 0, head_sums = 0, floats = 0;
 };
 long long four(long long n) { return (n + 3) / 4 * 4; }
 bool space_of(int B, int T, int H, long long rows, bool packed, bool backward, bool f32_rows, Space* s) {
     s->plan = wkv6::plan_mix(B, T, H, packed ? rows : -1, backward, f32_rows);
     const long long units = static_cast<long long>(B) * H;
-    s->blocks = T > 0 ? (T - 1) / s->plan.anchor_len + 1 : 0;
     if (!wkv6::fits_a_launch(units, wkv6::kMixThreads) || !wkv6::fits_a_launch(units * s->plan.segs * (backward ? 3 : 1), wkv6::kMixThreads) ||
-        (backward && !wkv6::fits_a_launch(units * s->blocks, wkv6::kMixThreads)))
+        (backward && !wkv6::fits_a_launch(units * s->plan.blocks, wkv6::kDecayGradientThreads)))
         return false;
     if (s->plan.segs > 1) s->locals = s->plan.segs * units * (kStateFloats + 4);
     s->floats = s->locals;
     if (backward) {
         s->sums = four(H * rows);
-        s->anchors = units * s->blocks * kStateFloats;
-        s->head_sums = four(B * s->blocks * H);
+        s->anchors = s->plan.places * H * kStateFloats;
+        s->head_sums = four(units * s->plan.blocks);
         s->floats = 2 * s->locals + 2 * s->sums + 2 * s->anchors + s->head_sums;
     }
     return true;
 }
-// for rows of either type, packed or not.  rows < 0: not known, for packed sequences of as many as may be
+// for rows of either type, packed or, if there are B T, not.  rows < 0: not known, for packed sequences of as many as may be
 long long workspace_bytes_of(int B, int T, int H, long long rows, bool backward) {
     long long most = 0;
     for (int i = 0; i < 4; ++i) {
+        const bool packed = i & 1 && rows >= 0;
+        if (!packed && rows >= 0 && rows != static_cast<long long>(B) * T) continue;
         Space s;
-        if (!space_of(B, T, H, rows < 0 ? 0 : rows, i & 1 && rows >= 0, backward, i & 2, &s)) return -1;
+        if (!space_of(B, T, H, rows < 0 ? 0 : rows, packed, backward, i & 2, &s)) return -1;
         if (s.floats > most) most = s.floats;
     }
     const long long units = static_cast<long long>(B) * H, pieces = T > 0 ? (T - 1) / wkv6::kMixBlock + 1 : 1;
@@ -83,7 +84,7 @@ wkv6::MixArgs mix_args(int B, int T, int H, long long rows, const float* g, long
     wkv6::MixArgs a;
     a.B = B; a.T = T; a.H = H; a.rows = rows;
     a.g = g; a.g_row = g_stride; a.offsets = offsets;
-    a.segs = p.segs; a.seg_len = p.seg_len; a.anchor_len = p.anchor_len;
+    a.segs = p.segs; a.seg_len = p.seg_len; a.anchor_len = p.anchor_len; a.blocks = p.blocks; a.whole_places = p.whole_places;
     a.sweeps = 1;
     return a;
 }

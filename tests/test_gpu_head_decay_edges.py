@@ -3,7 +3,8 @@ import pytest
 import torch
 
 import paper_2407_12077_amd as wkv
-from operator_util import CODE, N
+from operator_bits import head_off, off, parts_of
+from operator_util import CODE, N, Mix, check, np64
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -20,3 +21,26 @@ def test_gradient_of_a_head_s_decay_without_tokens(gpu_device, B, T, rows, packe
     offsets = torch.zeros(B + 1, dtype=torch.int32, device="cuda") if packed else None
     wkv.wkv6_head_decay_backward(B, T, H, N, rows, t, t, t, H * N, g, 0, offsets, None, t, None, dr, dk, dv, dg, None, CODE[BF16], ws, n)
     assert bool((dg[:H] == 0).all()) and float(dg[H]) == 7 and all(bool((a == 7).all()) for a in (dr, dk, dv))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("decay", ["token", "head"])
+@pytest.mark.parametrize("offsets,longest", [([0, 2100, 3124, 4149, 4149, 4154], 1 << 30), ([3, 1030, 2054, 2100, 2101, 5000], 70000), ([2000, 3500, 3500, 0, 1500], 9000),
+                                             ([500, 1524, 2548, 3573], 3100), ([700, 1400, 2100, 2800, 3500], 4000)])
+def test_gradients_of_packed_sequences_whose_longest_may_be_longer(gpu_device, offsets, longest, decay, dtype):
+    """T is a bound only: anchors lie by rows.  Offsets that fall leave a sequence without tokens and start again anywhere."""
+    B, rows = len(offsets) - 1, max(offsets) + 7
+    x = Mix(B, H=2, lengths=[0] * B, tail=rows, dtype=dtype, decay=decay, longest=longest, gradients=True)
+    x.offsets.copy_(torch.tensor(offsets, dtype=torch.int32))
+    x.spans = [(a, max(a, b)) for a, b in zip(offsets[:-1], offsets[1:])]
+    for a, b in x.spans:
+        x.covered[a:b] = True
+    got, parts = x.backward(), parts_of(x)
+    want, bounds = x.exact_gradients(), x.gradient_bounds()
+    for name, a, w, b in zip(("dr", "dk", "dv"), got, want, bounds):
+        check(name, a, w, b, x.covered, dtype)
+    check("dstate_in", got[4], want[4], bounds[4])
+    if decay == "head":
+        assert head_off(np64(got[3]), parts, x.spans).max() < 1
+    else:
+        assert off(np64(got[3]), parts).max() < 1 and bool((got[3][~x.covered] == 7).all())

@@ -38,3 +38,26 @@ def test_gradient_of_a_head_s_decay_with_no_sequence_is_written(fake):
     assert [[e.base for e in ev] for ev in got] == [["head_sums_kernel"]] * 3 + [[], []]
     assert got[0][0].grid[0] == 3
     assert status(backward(0, 0, 3, 0, g_stride=0, dg=lu.at(10, 2))) == ALIGN
+
+
+def packed_need(B, T, H, rows):
+    """Bytes of a packed gradient call with 256 units or more, which stay whole: anchors of both directions, two sums a row and head, a partial sum a block and head.  A head
+    has an anchor a block of 1024 tokens of every sequence, at most rows / 1024 blocks that are not a sequence's last and B that are."""
+    longest = min(T, rows)
+    block = min(1024, (longest + 63) // 64 * 64)
+    blocks = -(-longest // block)
+    four = lambda n: (n + 3) // 4 * 4  # noqa: E731
+    return 4 * (2 * min(B * blocks, rows // block + B) * H * 4096 + 2 * four(H * rows) + four(B * blocks * H))
+
+
+@pytest.mark.parametrize("B,T,H,rows", [(64, 131072, 32, 131072), (64, 131072, 32, 5000), (300, 1 << 30, 4, 9000), (2048, 131072, 32, 131072), (16, 4096, 16, 65536),
+                                        (16, 4096, 16, 65535), (256, 100, 1, 300)])
+def test_packed_gradients_take_what_their_rows_need(fake, B, T, H, rows):
+    """64 documents in 131072 rows took 8.7 GB of anchors where 0.2 hold them; T may be an upper bound, and 2048 x 32 units of 128 blocks fit a launch."""
+    need = binding.load().wkv6_head_decay_backward_workspace_bytes(B, T, H, 64, rows)
+    assert need == packed_need(B, T, H, rows)
+    ev, = launches(fake, [backward(B, T, H, rows, packed=True, workspace_bytes=need)])
+    assert [e.base for e in ev] == ["mix_kernel", "decay_gradient_kernel"]
+    longest = min(T, rows)
+    assert ev[1].grid[0] == B * -(-longest // min(1024, (longest + 63) // 64 * 64)) * H
+    assert status(backward(B, T, H, rows, packed=True, workspace_bytes=need - 1)) == WORKSPACE
