@@ -66,8 +66,8 @@ hipError_t launch_mix(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t
 // The segments' own states, `count` sweeps of a; before launch_mix when a.segs > 1.
 hipError_t launch_mix_locals(const MixArgs& a, int count, bool f32_rows, hipStream_t stream);
 
-// dg from the sums (r . dr in r_sums, k . dk in k_sums) and the anchors of both directions.  head_sums: [blocks][H] partial sums
-// when the decays are one a head, folded into dg [H]; otherwise dg is [rows][H].
+// dg from the sums (r . dr in r_sums, k . dk in k_sums) and the anchors of both directions.  When the decays are one a head (g_row = 0) partial sums
+// [blocks][H] in head_sums are folded into dg [H], which is written without any too; otherwise dg is [rows][H].
 hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const float* k_sums, const float* behind, const float* front,
                                  float* head_sums, float* dg, hipStream_t stream);
 

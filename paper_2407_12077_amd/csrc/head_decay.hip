@@ -1036,9 +1036,9 @@ hipError_t launch_decay_gradient(const MixArgs& a, const float* r_sums, const fl
     const long long count = static_cast<long long>(a.B) * a.blocks;
     if (count > 0)
         hipLaunchKernelGGL(decay_gradient_kernel, dim3(static_cast<unsigned>(count * a.H)), dim3(kDecayGradientThreads), 0, stream, a, r_sums,
-                           k_sums, behind, front, head_sums, dg);
+                           k_sums, behind, front, a.g_row == 0 ? head_sums : nullptr, dg);
     const hipError_t err = hipGetLastError();
-    return err != hipSuccess || !head_sums ? err : launch_head_sums(count, a.H, head_sums, dg, stream);
+    return err != hipSuccess || a.g_row != 0 ? err : launch_head_sums(count, a.H, head_sums, dg, stream);
 }
 
 hipError_t launch_head_sums(long long count, int H, const float* head_sums, float* dg, hipStream_t stream) {

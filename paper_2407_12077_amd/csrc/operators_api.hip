@@ -227,7 +227,7 @@ int wkv6_head_decay_backward(int B, int T, int H, int N, long long rows, const v
     hipError_t err = wkv6::raise_mix_limits();
     if (err == hipSuccess && a.segs > 1) err = wkv6::launch_mix_locals(a, 2, f32, st);
     if (err == hipSuccess) err = wkv6::launch_mix(a, f32, f32, st);
-    if (err == hipSuccess && dg) err = wkv6::launch_decay_gradient(a, r_sums, k_sums, behind, front, g_stride == 0 ? head_sums : nullptr, dg, st);
+    if (err == hipSuccess && dg) err = wkv6::launch_decay_gradient(a, r_sums, k_sums, behind, front, head_sums, dg, st);
     return status_of(err);
 }
 

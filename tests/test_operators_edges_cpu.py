@@ -40,6 +40,14 @@ def test_gradient_of_a_head_s_decay_with_no_sequence_is_written(fake):
     assert status(backward(0, 0, 3, 0, g_stride=0, dg=lu.at(10, 2))) == ALIGN
 
 
+def test_gradient_of_a_head_s_decay_without_a_workspace_is_written(fake):
+    """Without tokens no workspace is needed, and none may be given."""
+    calls = [backward(2, 0, 3, 0, g_stride=0, workspace_bytes=0), backward(2, 9, 3, 0, g_stride=0, packed=True, workspace_bytes=0)]
+    for _, args in calls:
+        args[-3] = None
+    assert [[e.base for e in ev][-1:] for ev in launches(fake, calls)] == [["head_sums_kernel"]] * 2
+
+
 def packed_need(B, T, H, rows):
     """Bytes of a packed gradient call with 256 units or more, which stay whole: anchors of both directions, two sums a row and head, a partial sum a block and head.  A head
     has an anchor a block of 1024 tokens of every sequence, at most rows / 1024 blocks that are not a sequence's last and B that are."""
