@@ -7,11 +7,13 @@ log2 e of a decay that is the same for all tokens and the decay's own factor, wh
 roundings are of its size."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2407_12077_amd as wkv
-from operator_util import N, Mix
+from operator_bits import STEPS, head_off, off, parts_of
+from operator_util import N, Mix, np64
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -61,3 +63,50 @@ def test_the_factor_of_the_first_token(gpu_device, g):
     error = (got - want) / want
     assert rms(error) <= STEP * math.sqrt(((1.25 * g) ** 2 + 2) / 3 + 0.25)
     assert float(error.abs().max()) <= STEP * (1.25 * abs(g) + 2.5)
+
+
+# Sums and factors that no long memory is in: chains of up to forty additions (an fp32 score has sixteen of four products, a read-out eight over keys and sixteen
+# over the state), whose partial sums have half the result's square on average, sqrt(40 / 2 / 3) < 2.6 steps, ten more roundings, sqrt(10 / 3) < 1.9; and the three
+# steps of above.  Two bf16 terms of a state or a score, in the place of three, are 41 steps of it off (tests/test_operator_bits_cpu.py)
+SUMS = 2.6 + 1.9 + 3
+
+
+def memory(x, h):
+    g = x.g[h] if x.decay == "head" else x.g[:, h].mean()
+    return 1 / (1 - math.exp(2 * (64 if x.dtype == BF16 else 32) * float(g)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("decay", ["token", "head"])
+@pytest.mark.parametrize("case", [dict(B=65, T=200, H=4), dict(B=300, T=70, H=1), dict(B=1, T=1500, H=2), dict(lengths=[900, 0, 33, 130, 64], H=3)], ids=str)
+def test_results_in_fp32(gpu_device, case, decay, dtype):
+    """Among them more units than the card has compute units, whole: a second round of workgroups."""
+    x = Mix(7, dtype=dtype, decay=decay, gradients=True, **case)
+    out, state = x.prefill(F32)
+    want, last = x.exact()
+    results = [("out", out, want), ("state", state, last)]
+    exact, got = x.exact_gradients(), x.backward()
+    if dtype == F32:
+        results += [(n, got[i], exact[i]) for i, n in enumerate(("dr", "dk", "dv"))]
+    results.append(("dstate_in", got[4], exact[4]))
+    for name, a, b in results:
+        b = torch.from_numpy(b).cuda()
+        for h in range(x.H):
+            u, v = a[:, h].double(), b[:, h]
+            if name in ("out", "dr", "dk", "dv"):
+                u, v = u[x.covered], v[x.covered]
+            assert rms(u - v) <= STEP * (math.sqrt(memory(x, h) / 3) + SUMS) * rms(v), (name, h)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("decay", ["token", "head"])
+@pytest.mark.parametrize("case", [dict(B=2, T=2100, H=2), dict(B=65, T=200, H=4), dict(lengths=[2100, 0, 1024, 1025, 5, 300], H=2, tail=3)], ids=str)
+def test_gradients_of_decays(gpu_device, case, decay, dtype):
+    """Over several blocks, and from short and empty sequences, per token and summed a head; the bounds are a small part of what they bound."""
+    x = Mix(8, dtype=dtype, decay=decay, gradients=True, **case)
+    got, parts = np64(x.backward()[3]), parts_of(x)
+    if decay == "head":
+        assert head_off(got, parts, x.spans).max() < 1
+    else:
+        assert off(got, parts).max() < 1
+    assert np.median(parts.spread[x.covered.numpy()] * STEPS / abs(parts.dg[x.covered.numpy()])) < 0.01

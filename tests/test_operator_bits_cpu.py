@@ -2,6 +2,7 @@
 what is carried from 256 tokens to the next; and they take the right one with every product rounded to fp32."""
 import numpy as np
 import pytest
+import torch
 
 from operator_bits import Parts, head_off, off
 from operator_util import N
@@ -48,3 +49,15 @@ def test_wrong_sums_over_all_tokens_are_refused(parts):
         left = parts.dg.copy()
         left[a:b] = 0
         assert (head_off(left.sum(0), parts, SPANS) > 1).all() or b - a < 8
+
+
+def test_two_bf16_terms_are_refused():
+    """What a state or a score in two bf16 terms, in the place of three, is off: beyond every bound of tests/test_gpu_head_decay_rms.py."""
+    x = torch.from_numpy(np.random.default_rng(9).standard_normal(1 << 16))
+
+    def error(terms):
+        left = x
+        for _ in range(terms):
+            left = left - left.bfloat16().double()
+        return float((left.square().mean() / x.square().mean()).sqrt()) * 2 ** 24
+    assert 40 < error(2) < 42 and error(3) < 0.2

@@ -69,3 +69,36 @@ def test_packed_gradients_take_what_their_rows_need(fake, B, T, H, rows):
     longest = min(T, rows)
     assert ev[1].grid[0] == B * -(-longest // min(1024, (longest + 63) // 64 * 64)) * H
     assert status(backward(B, T, H, rows, packed=True, workspace_bytes=need - 1)) == WORKSPACE
+
+
+def prefill(B, T, H, rows, packed, dtype, workspace_bytes):
+    return ("wkv6_head_decay_prefill", [B, T, H, 64, rows, lu.at(0), lu.at(1), lu.at(2), H * 64, lu.at(3), H, lu.at(13) if packed else None, lu.at(4),
+                                        lu.at(5), lu.at(6), dtype, dtype, lu.at(12), workspace_bytes, None])
+
+
+@pytest.mark.parametrize("B,T,H,rows", [(1, 4096, 32, None), (1, 1500, 2, None), (4, 700, 8, None), (2, 512, 16, None), (20, 8000, 8, 60000), (6, 2111, 1, 3000),
+                                        (3, 130, 5, 200), (9, 1531, 12, 7000)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_a_call_takes_exactly_the_workspace_of_its_pieces(fake, B, T, H, rows, dtype):
+    """Counted from what is launched: a state and four floats a piece and unit, of gradients for two states, and what packed_need counts."""
+    packed, rows = rows is not None, B * T if rows is None else rows
+    units = B * H
+    ev, back = launches(fake, [prefill(B, T, H, rows, packed, dtype, BIG), backward(B, T, H, rows, packed=packed, dtype=dtype)])
+    pieces = ev[0].grid[0] // units if len(ev) == 2 else 0
+    assert [e.grid[0] for e in ev] == [pieces * units] * 2 if pieces else [units]
+    need = 4 * pieces * units * 4100
+    assert need <= binding.load().wkv6_head_decay_workspace_bytes(B, T, H, 64)
+    launches(fake, [prefill(B, T, H, rows, packed, dtype, need)])
+    if need:
+        assert status(prefill(B, T, H, rows, packed, dtype, need - 1)) == WORKSPACE
+    pieces = back[0].grid[0] // (2 * units) if len(back) == 3 else 0
+    assert back[-2].grid[0] == 3 * units * max(1, pieces)
+    longest = min(T, rows)
+    block = min(1024, (longest + 63) // 64 * 64)
+    blocks = -(-longest // block)
+    four = lambda n: (n + 3) // 4 * 4  # noqa: E731
+    places = min(B * blocks, rows // block + B) if packed else B * blocks
+    need = 4 * (2 * pieces * units * 4100 + 2 * places * H * 4096 + 2 * four(H * rows) + four(units * blocks))
+    assert need <= binding.load().wkv6_head_decay_backward_workspace_bytes(B, T, H, 64, rows)
+    launches(fake, [backward(B, T, H, rows, packed=packed, dtype=dtype, workspace_bytes=need)])
+    assert status(backward(B, T, H, rows, packed=packed, dtype=dtype, workspace_bytes=need - 1)) == WORKSPACE
