@@ -58,7 +58,7 @@ constexpr int kDecayGradientThreads = 256;
 // packed_rows: of a call with offsets, else -1; such a call is cut into at most kMixPackedSegments, or as many as
 // the same call of sequences that are all T long.
 constexpr int kMixPackedSegments = 8;
-constexpr int kMixFewUnits = 256;      // calls of as many or more stay whole
+constexpr int kMixFewUnits = 256;      // calls of as many or more stay whole: see plan_mix
 MixPlan plan_mix(int B, int T, int H, long long packed_rows, bool backward, bool f32_rows);
 
 hipError_t launch_mix(const MixArgs& a, bool f32_rows, bool f32_out, hipStream_t stream);

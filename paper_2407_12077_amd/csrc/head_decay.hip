@@ -25,11 +25,11 @@
 //   consumers  (4) own 16 of the 64 value columns each: the state's [64][16] columns stay in registers for the whole walk, and as accumulators
 //              of k^T (decayed v) they lie as S^T q^T wants them.  They add that to the producers' part, in its place in LDS
 //
-// What bounds it.  8 x 4096 tokens x 32 heads, bf16: 537 MB in 117 us, 4.6 TB/s, where a large copy reaches 5.1; a round (64 tokens of every
-// workgroup) takes 1.8 us, of which the consumers and the last producer work 1.25, so memory and the barrier share the rest.  One prompt of 131072 tokens: 230
-// us for the states and 460 for the read-outs, 3.2 GB at 4.8 TB/s (k and v are read twice).  Gradients of 8 x 4096 x 32: 396 us for 1.49 GB
+// What bounds it.  8 x 4096 tokens x 32 heads, bf16: 537 MB in 119 us, 4.5 TB/s, where a large copy reaches 5.1; a round (64 tokens of every
+// workgroup) takes 1.85 us, of which the consumers and the last producer work 1.3, so memory and the barrier share the rest.  One prompt of 131072 tokens: 226
+// us for the states and 446 to 514 for the read-outs, 3.2 GB at 4.7 TB/s (k and v are read twice).  Gradients of 8 x 4096 x 32: 394 us for 1.49 GB
 // (counted: dv and dk find the rows that they share in an XCD's L2, dr runs the other way), 3.8 TB/s: three rounds of workgroups of 2.05 us a chunk.  fp32
-// rows: 4.3 us for 64 tokens, fp32 matrix instructions in series with their LDS reads.
+// rows: 5.0 us for 64 tokens of every compute unit (8 x 2048 x 32 160 us), fp32 matrix instructions in series with their LDS reads.
 //
 // bf16 rows: products of rows are exact in fp32; the computed operands (P, S, decayed v) enter as sums of three bf16, which hold an
 // fp32 value whole over its whole range, one product for each; two where only bf16 read-outs come of them.  fp32 rows: fp32 matrix instructions.
@@ -702,7 +702,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
     using L = Layout<T, Out, kC, kStates, kSums>;
     extern __shared__ __align__(16) char lds[];
     // Runs of units on one XCD, which read whole lines of neighbouring heads' rows: 8 x 4096 x 32 126 -> 118 us, 131072 x 32 784 -> 680.  Packed
-    // sequences differ in length, and an XCD that has the long ones would work alone: in turn (37 x 12 of up to 2011 tokens 74 -> 60)
+    // sequences differ in length, and an XCD that has the long ones would work alone: in turn (37 x 12 of up to 2011 tokens,
+    // fp32 read-outs, the kernel alone, 74 -> 60; 59 now)
     int at = a.offsets ? static_cast<int>(blockIdx.x) : index_on_xcd();
     const int sweep = uniform(at % a.sweeps);
     at /= a.sweeps;
@@ -843,8 +844,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 3))
 // dg.  exp(G_t - G_i) with G the running sum of g makes dL/dG_t = r_t . dr_t - k_t . dk_t, plus <dS, S> for a state handed on, so
 //     dg_t = sum_{t <= s <= a} (r_s . dr_s - k_s . dk_s) + w_{a+1} <dS_{a+1}, S_a>
 // for any a >= t; dS_{a+1} is the gradient of the state behind token a + 1, and behind the last token that of state_out.  The sums nearly
-// cancel, so a is the end of t's block of anchor_len tokens and not of the sequence, and they are taken in 64 bits.
-// A workgroup per unit and block.  14 us of the 8 x 4096 x 32 gradients' 400: 24 MB, and 256 tokens at a time in series.
+// cancel, so a is the end of t's block of anchor_len tokens and not of the sequence.  r_s . dr_s and k_s . dk_s are fp32 sums of 64 fp32 products, formed
+// beside the read-outs: exact products added in 64 bits there made the gradients of 8 x 4096 x 32 416 us where they took 398, packed ones of 20 x 3000 x 12
+// 96 and 90.  From there on all is in 64 bits but a block's partial sum of one decay a head, which is rounded to fp32 once.  Errors of dg are
+// 1.3e-7 to 2.2e-6 of its root mean square, where chunks in 32 bits with these products in 64 are 3e-7 to 4.2e-6 off.
+// A workgroup per unit and block.  15 us of the 8 x 4096 x 32 gradients' 408: 24 MB, and 256 tokens at a time in series.
 __global__ __launch_bounds__(kDecayGradientThreads) void decay_gradient_kernel(const MixArgs a, const float* r_sums, const float* k_sums,
                                                              const float* behind, const float* front, float* head_sums, float* dg) {
     __shared__ double part[4];
@@ -980,7 +984,10 @@ MixPlan plan_mix(int B, int T, int H, long long packed_rows, bool backward, bool
     // more than 8 % off the best, the furthest 20 %
     // Packed, 20 sequences of up to 8000 tokens x 8 heads 173 / 98 (8) / 93 (4), fp32 rows 564 / 244 (8) / 235 (4); 9 x 1531 x 12 37.6 / 29.3 (6) / 28.4 (4),
     // gradients 51.9 whole against 58 (4), of fp32 rows 128 / 99 (4) / 99; of 40 such sizes and types most are within 8 % of the best, the
-    // furthest 16 %.  With 256 units and more (37 x 2011 x 12 51.6 whole, 67 in two) whole
+    // furthest 16 %.  With 256 units and more whole: packed 37 x 2011 x 12 (bf16 read-outs) 51.6 whole, 67 in two; sequences of one length, whole and as
+    // cut by the model, bf16 9 x 4096 x 32 200 and 233, 10 x 199 and 246, 12 x 216 and 216, 9 x 8192 x 32 380 and 440, 300 x 4096 x 1 200 and 237, 33 x
+    // 32768 x 8 1520 and 1556; gradients 9 x 4096 x 32 504 and 508, fp32 1250 and 1256; fp32 9 x 4096 x 32 586 and 595, 12 x 590 and 664.  The only
+    // ones found that would gain are fp32 prompts of many more tokens, 33 x 8192 x 8 1158 and 1022, 33 x 32768 x 8 5200 and 3860
     if (units < kMixFewUnits) {
         const int whole_ones = packed ? plan_mix(B, T, H, -1, backward, f32_rows).segs : 32;
         const int most = whole_ones > kMixPackedSegments ? whole_ones : kMixPackedSegments;
