@@ -9,4 +9,7 @@ from .binding import (  # noqa: F401
     wkv6_prefill_bf16_strided, wkv6_prefill_f32, wkv6_split_segments, wkv6_split_workspace_bytes,
     wkv6_arena_layout, wkv6_version,
     wkv6_head_decay_backward, wkv6_head_decay_backward_workspace_bytes, wkv6_head_decay_decode, wkv6_head_decay_prefill,
-    wkv6_head_decay_workspace_bytes, wkv6_layernorm_backward, wkv6_layernorm_backward_workspace_bytes, wkv6_layernorm_forward)
+    wkv6_head_decay_workspace_bytes, wkv6_layernorm_backward, wkv6_layernorm_backward_workspace_bytes, wkv6_layernorm_forward,
+    wkv6_selective_scan_backward, wkv6_selective_scan_backward_workspace_bytes, wkv6_selective_scan_decode, wkv6_selective_scan_prefill,
+    wkv6_selective_scan_workspace_bytes, wkv6_short_conv_backward, wkv6_short_conv_backward_workspace_bytes, wkv6_short_conv_decode,
+    wkv6_short_conv_prefill)

@@ -1,7 +1,7 @@
 """Thin binding of ``libwkv6.so``: argument marshalling only.
 
-Every entry point has the name and argument order of ``include/wkv6.h``, ``include/wkv6_head_decay.h`` and
-``include/wkv6_layernorm.h``.  Tensors are
+Every entry point has the name and argument order of ``include/wkv6.h``, ``include/wkv6_head_decay.h``,
+``include/wkv6_layernorm.h``, ``include/wkv6_selective_scan.h`` and ``include/wkv6_short_conv.h``.  Tensors are
 PyTorch-ROCm tensors used purely as device memory (``data_ptr``) and the current HIP
 stream; nothing is computed here.  Calls that enqueue work go through the extension ``_call``
 (csrc/binding_call.cpp), the others through ctypes.  There is no fallback: if the library or the
@@ -33,6 +33,11 @@ EXPORTS = ("wkv6_prefill_bf16", "wkv6_prefill_bf16_f32out", "wkv6_prefill_bf16_s
 OPERATOR_EXPORTS = ("wkv6_head_decay_prefill", "wkv6_head_decay_workspace_bytes", "wkv6_head_decay_decode",
                     "wkv6_head_decay_backward", "wkv6_head_decay_backward_workspace_bytes", "wkv6_layernorm_forward",
                     "wkv6_layernorm_backward", "wkv6_layernorm_backward_workspace_bytes")
+
+# of include/wkv6_selective_scan.h and include/wkv6_short_conv.h
+SCAN_EXPORTS = ("wkv6_selective_scan_prefill", "wkv6_selective_scan_workspace_bytes", "wkv6_selective_scan_decode",
+                "wkv6_selective_scan_backward", "wkv6_selective_scan_backward_workspace_bytes", "wkv6_short_conv_prefill",
+                "wkv6_short_conv_decode", "wkv6_short_conv_backward", "wkv6_short_conv_backward_workspace_bytes")
 
 _lib = None
 _call = None               # the extension, bound to _lib
@@ -113,6 +118,25 @@ def load():
         lib.wkv6_layernorm_backward.argtypes = [ll, i] + [vp] * 7 + [i, i, vp, ll, vp]
         lib.wkv6_layernorm_backward_workspace_bytes.restype = ll
         lib.wkv6_layernorm_backward_workspace_bytes.argtypes = [ll, i]
+        scan = [vp, ll, vp, ll, vp, i, vp, vp, vp, ll, vp, vp, ll]            # x .. z_stride
+        lib.wkv6_selective_scan_prefill.restype = i
+        lib.wkv6_selective_scan_prefill.argtypes = [i, i, i, i, ll, *scan, vp, vp, vp, vp, i, i, vp, ll, vp]
+        lib.wkv6_selective_scan_decode.restype = i
+        lib.wkv6_selective_scan_decode.argtypes = [i, i, i, *scan, vp, vp, vp, i, i, vp]
+        lib.wkv6_selective_scan_backward.restype = i
+        lib.wkv6_selective_scan_backward.argtypes = [i, i, i, i, ll, *scan] + [vp] * 13 + [i, vp, ll, vp]
+        lib.wkv6_selective_scan_workspace_bytes.restype = ll
+        lib.wkv6_selective_scan_workspace_bytes.argtypes = [i, i, i, i]
+        lib.wkv6_selective_scan_backward_workspace_bytes.restype = ll
+        lib.wkv6_selective_scan_backward_workspace_bytes.argtypes = [i, i, i, i, ll]
+        lib.wkv6_short_conv_prefill.restype = i
+        lib.wkv6_short_conv_prefill.argtypes = [i, i, i, i, ll, vp, ll, vp, vp, i, vp, vp, vp, vp, i, vp]
+        lib.wkv6_short_conv_decode.restype = i
+        lib.wkv6_short_conv_decode.argtypes = [i, i, i, vp, ll, vp, vp, i, vp, vp, vp, i, vp]
+        lib.wkv6_short_conv_backward.restype = i
+        lib.wkv6_short_conv_backward.argtypes = [i, i, i, i, ll, vp, ll, vp, vp, i] + [vp] * 8 + [i, vp, ll, vp]
+        lib.wkv6_short_conv_backward_workspace_bytes.restype = ll
+        lib.wkv6_short_conv_backward_workspace_bytes.argtypes = [i, i, i, i, ll]
         lib.wkv6_arena_layout.restype = ctypes.c_longlong
         lib.wkv6_arena_layout.argtypes = [i, ctypes.POINTER(ctypes.c_longlong), ctypes.POINTER(ctypes.c_longlong)]
         lib.wkv6_status_string.restype = ctypes.c_char_p
@@ -315,6 +339,58 @@ def wkv6_layernorm_backward(M, D, x, mean_rstd, gamma, dy, dx, dgamma, dbeta, dt
 
 def wkv6_layernorm_backward_workspace_bytes(M, D):
     return load().wkv6_layernorm_backward_workspace_bytes(M, D)
+
+
+def wkv6_selective_scan_prefill(B, T, D, N, rows, x, x_stride, delta, delta_stride, delta_bias, softplus, a, b, c, bc_stride, skip,
+                                z, z_stride, offsets, state_in, out, state_out, dtype, out_dtype, workspace, workspace_bytes,
+                                stream=None):
+    (_call or _bound()).wkv6_selective_scan_prefill(B, T, D, N, rows, x, x_stride, delta, delta_stride, delta_bias, int(softplus), a, b,
+                                                    c, bc_stride, skip, z, z_stride, offsets, state_in, out, state_out, int(dtype),
+                                                    int(out_dtype), workspace, workspace_bytes, stream)
+
+
+def wkv6_selective_scan_workspace_bytes(B, T, D, N):
+    return load().wkv6_selective_scan_workspace_bytes(B, T, D, N)
+
+
+def wkv6_selective_scan_decode(B, D, N, x, x_stride, delta, delta_stride, delta_bias, softplus, a, b, c, bc_stride, skip, z, z_stride,
+                               state_in, out, state_out, dtype, out_dtype, stream=None):
+    (_call or _bound()).wkv6_selective_scan_decode(B, D, N, x, x_stride, delta, delta_stride, delta_bias, int(softplus), a, b, c,
+                                                   bc_stride, skip, z, z_stride, state_in, out, state_out, int(dtype),
+                                                   int(out_dtype), stream)
+
+
+def wkv6_selective_scan_backward(B, T, D, N, rows, x, x_stride, delta, delta_stride, delta_bias, softplus, a, b, c, bc_stride, skip,
+                                 z, z_stride, offsets, state_in, dout, dstate_out, dx, ddelta, db, dc, dz, da, dskip, ddelta_bias,
+                                 dstate_in, dtype, workspace, workspace_bytes, stream=None):
+    (_call or _bound()).wkv6_selective_scan_backward(B, T, D, N, rows, x, x_stride, delta, delta_stride, delta_bias, int(softplus), a,
+                                                     b, c, bc_stride, skip, z, z_stride, offsets, state_in, dout, dstate_out, dx,
+                                                     ddelta, db, dc, dz, da, dskip, ddelta_bias, dstate_in, int(dtype), workspace,
+                                                     workspace_bytes, stream)
+
+
+def wkv6_selective_scan_backward_workspace_bytes(B, T, D, N, rows):
+    return load().wkv6_selective_scan_backward_workspace_bytes(B, T, D, N, rows)
+
+
+def wkv6_short_conv_prefill(B, T, D, W, rows, x, x_stride, w, bias, silu, offsets, state_in, out, state_out, dtype, stream=None):
+    (_call or _bound()).wkv6_short_conv_prefill(B, T, D, W, rows, x, x_stride, w, bias, int(silu), offsets, state_in, out, state_out,
+                                                int(dtype), stream)
+
+
+def wkv6_short_conv_decode(B, D, W, x, x_stride, w, bias, silu, state_in, out, state_out, dtype, stream=None):
+    (_call or _bound()).wkv6_short_conv_decode(B, D, W, x, x_stride, w, bias, int(silu), state_in, out, state_out, int(dtype), stream)
+
+
+def wkv6_short_conv_backward(B, T, D, W, rows, x, x_stride, w, bias, silu, offsets, state_in, dout, dstate_out, dx, dw, dbias,
+                             dstate_in, dtype, workspace, workspace_bytes, stream=None):
+    (_call or _bound()).wkv6_short_conv_backward(B, T, D, W, rows, x, x_stride, w, bias, int(silu), offsets, state_in, dout,
+                                                 dstate_out, dx, dw, dbias, dstate_in, int(dtype), workspace, workspace_bytes,
+                                                 stream)
+
+
+def wkv6_short_conv_backward_workspace_bytes(B, T, D, W, rows):
+    return load().wkv6_short_conv_backward_workspace_bytes(B, T, D, W, rows)
 
 
 def wkv6_version():

@@ -8,7 +8,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libwkv6.so")
 SOURCES = ["wkv6_api.hip", "wkv6_recurrent.hip", "wkv6_chunked.hip", "wkv6_chunked_f32.hip", "wkv6_segments.hip", "wkv6_short.hip",
            "key_compress.hip", "layernorm_finalize.hip", "decay_input.hip", "head_decay.hip", "head_decay_step.hip", "layernorm_rows.hip",
-           "operators_api.hip"]
+           "operators_api.hip", "selective_scan.hip", "selective_scan_step.hip", "selective_scan_backward.hip", "short_conv.hip", "scan_api.hip"]
 CALL = os.path.join(PKG, "_call" + sysconfig.get_config_var("EXT_SUFFIX"))      # plain host code: no HIP in it
 # packed-fp32 VALU forms are switched off on purpose for the whole library
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -20,6 +20,8 @@
 #include "wkv6.h"
 #include "wkv6_head_decay.h"
 #include "wkv6_layernorm.h"
+#include "wkv6_selective_scan.h"
+#include "wkv6_short_conv.h"
 
 namespace {
 
@@ -147,7 +149,9 @@ PyObject* invoke(int (*fn)(A...), const char* name, PyObject* const* args, Py_ss
     X(wkv6_decay_lora_input_bf16) X(wkv6_finch_c2_prefill_lora_bf16) X(wkv6_prefill_lora_bf16) X(wkv6_decode_bf16)            \
     X(wkv6_finch_c2_decode_bf16) X(wkv6_append_bf16) X(wkv6_finch_c2_append_bf16) X(wkv6_key_compress_bf16)                   \
     X(wkv6_head_decay_prefill) X(wkv6_head_decay_decode) X(wkv6_head_decay_backward)                                          \
-    X(wkv6_layernorm_forward) X(wkv6_layernorm_backward)
+    X(wkv6_layernorm_forward) X(wkv6_layernorm_backward)                                                                      \
+    X(wkv6_selective_scan_prefill) X(wkv6_selective_scan_decode) X(wkv6_selective_scan_backward)                              \
+    X(wkv6_short_conv_prefill) X(wkv6_short_conv_decode) X(wkv6_short_conv_backward)
 
 #define X(name)                                                                                    \
     decltype(&::name) fn_##name = nullptr;                                                         \

@@ -1,0 +1,64 @@
+// The selective scan: what its kernels are told (selective_scan.hip, selective_scan_step.hip, selective_scan_backward.hip) and how long axes are cut.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "wkv6_launch.h"
+
+namespace wkv6 {
+
+constexpr int kScanChannels = 64;      // of a workgroup: a lane each
+constexpr int kScanChunk = 16;         // tokens that a workgroup takes at once; segments are whole multiples of it
+
+struct ScanArgs {
+    int B, T, D, N;
+    long long rows;                    // of the packed tensors
+    const void *x, *delta, *z, *b, *c; // z null: no gate
+    long long x_row, delta_row, z_row, bc_row;   // bytes from token to token
+    const float *a, *bias, *skip;      // bias, skip may be null
+    bool softplus;
+    const int* offsets;                // [B + 1] or null: B sequences of T rows
+    const float* state_in;             // null: zeros
+    int segs, seg_len;                 // a sequence's segments
+    // segs > 1: [segs][B][D][N], state_in in front of all, then what segment s - 1 leaves of nothing; behind them the segments' sums
+    // of step sizes, [segs][B][D], likewise
+    float* locals;
+};
+
+// segs segments of seg_len tokens, a multiple of kScanChunk.
+struct ScanPlan {
+    int segs, seg_len;
+};
+ScanPlan plan_scan(int B, int T, int D, int N);
+inline long long scan_blocks(int D) { return (D + kScanChannels - 1) / kScanChannels; }
+inline long long scan_local_floats(const ScanPlan& p, long long B, long long D, int N) { return p.segs > 1 ? p.segs * B * D * (N + 1) : 0; }
+constexpr int scan_threads(int N) { return 16 * N; }
+
+// state_out may be null.  With a.segs > 1 the segments' own states first.
+hipError_t launch_scan(const ScanArgs& a, void* out, float* state_out, bool f32_rows, bool f32_out, hipStream_t stream);
+
+// Gradients.  Tokens whose decays and states stay in registers on the way back; the states in front of them are kept in `states`.
+constexpr int scan_back_chunk(int N) { return N == 64 ? 8 : 16; }
+struct ScanGradients {
+    const void* dout;
+    const float* dstate_out;
+    void *dx, *ddelta, *db, *dc, *dz;
+    float *da, *dskip, *dbias, *dstate_in;
+    // workspace
+    float* states;                     // [place][D][N] in front of every chunk; sequence b's chunk i: place first row / chunk + i + b
+    float* behind;                     // segs > 1: [segs][B][D][N] what a segment hands to the one in front of it of nothing; behind
+                                       // them the sums of its step sizes [segs][B][D]
+    float* rows;                       // [rows][blocks][2 N]: shares of db and dc
+    float* weights;                    // [segs][B][D][N], then [segs][B][2][D]: shares of da, and of dskip and dbias
+};
+hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradients& g, bool f32, hipStream_t stream);
+
+// da, dskip, dbias (what is wanted of them) from g.weights; without sequences nought.
+hipError_t launch_scan_weights(const ScanArgs& a, const ScanGradients& g, hipStream_t stream);
+
+// The segments' own states, in a.locals (selective_scan.hip).
+hipError_t launch_scan_states(const ScanArgs& a, bool f32_rows, hipStream_t stream);
+
+// One token a sequence.
+hipError_t launch_scan_step(const ScanArgs& a, void* out, float* state_out, bool f32_rows, bool f32_out, hipStream_t stream);
+
+}  // namespace wkv6

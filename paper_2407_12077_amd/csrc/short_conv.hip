@@ -1,0 +1,409 @@
+// The short causal convolution of every channel over its own tokens, and its gradients, for gfx950:
+//
+//     p_t = bias + sum_j w[j] x_{t-W+1+j}    out = silu(p)
+//     dp_t = dout_t silu'(p_t)    dx_s = sum_j w[j] dp_{s+W-1-j}    dw[j] = sum_t dp_t x_{t-W+1+j}    dbias = sum_t dp_t
+//
+// A thread has eight channels of a run of tokens and keeps the inputs under its taps in registers, so a row is read once, but for the W - 1 rows
+// in front of a run (and behind it, of the gradients), which a neighbour reads too.
+#include "short_conv.h"
+
+#include "selective_scan_tiles.h"
+
+namespace wkv6 {
+namespace {
+
+using namespace scan;
+
+constexpr int kG = kConvGroup;
+
+struct Place {
+    long long row0;                    // of the sequence's first token
+    int len, first, end;               // tokens of the sequence; this thread's
+};
+// Tokens first .. end - 1 of sequence b for slice `slice` of segment `seg`.
+__device__ __forceinline__ Place place_of(const ConvArgs& a, int b, int seg, int slice, int run) {
+    Place p;
+    long long lo = static_cast<long long>(b) * a.T, len = a.T;
+    if (a.offsets) {
+        long long f = a.offsets[b], e = a.offsets[b + 1];
+        f = f < 0 ? 0 : f > a.rows ? a.rows : f;
+        e = e < 0 ? 0 : e > a.rows ? a.rows : e;
+        len = e - f;
+        len = len < 0 ? 0 : len > a.T ? a.T : len;
+        lo = f;
+    }
+    p.row0 = lo;
+    p.len = static_cast<int>(len);
+    const long long first = static_cast<long long>(seg) * a.seg_len + slice * run, end = first + run;
+    p.first = static_cast<int>(first < len ? first : len);
+    p.end = static_cast<int>(end < len ? end : len);
+    return p;
+}
+
+template <bool kF32>
+struct Row {
+    Raw<kF32, kG> raw;
+    __device__ __forceinline__ void get(float (&v)[kG]) const {
+#pragma unroll
+        for (int i = 0; i < kG; ++i) v[i] = raw[i];
+    }
+};
+
+template <int W>
+struct Taps {
+    float w[W][kG], bias[kG];
+    __device__ __forceinline__ void load(const ConvArgs& a, int ch) {
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j][i] = a.w[static_cast<long long>(ch + i) * W + j];
+            bias[i] = a.bias ? a.bias[ch + i] : 0.f;
+        }
+    }
+};
+
+// The threads of a workgroup: `lanes` side by side over groups of channels, 256 / lanes slices of `run` tokens one behind the other.
+template <int W, bool kF32>
+__global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* out, char* state_out, int across, int run) {
+    constexpr int kItem = kF32 ? 4 : 2, kBatch = 4;
+    const int column = threadIdx.x % a.lanes, slice = threadIdx.x / a.lanes;
+    const int block = blockIdx.x % across, at = blockIdx.x / across, b = at % a.B, seg = at / a.B;
+    const int ch = (block * a.lanes + column) * kG;
+    if (ch >= a.D) return;
+    const Place p = place_of(a, b, seg, slice, run);
+    const bool head = seg == 0 && slice == 0;
+    if (p.first >= p.end && !head) return;
+    const char* x = static_cast<const char*>(a.x) + p.row0 * a.x_row + ch * kItem;
+    const long long state_row = static_cast<long long>(a.D) * kItem, state_at = static_cast<long long>(b) * (W - 1) * state_row + ch * kItem;
+    Taps<W> taps;
+    taps.load(a, ch);
+    float win[W][kG];                                          // win[W - 1]: the token at hand
+    Row<kF32> front[W - 1];
+    if (head) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            front[j].raw.none();
+            if (a.state_in) front[j].raw.load(static_cast<const char*>(a.state_in) + state_at + j * state_row);
+        }
+        if (state_out) {                                       // (no other thread reads these channels' state_in, which may be state_out)
+            Row<kF32> last[W - 1];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) {
+                const int t = p.len - (W - 1) + j;             // below nought: of the old state
+#pragma unroll
+                for (int q = 0; q < W - 1; ++q)
+                    if (t + W - 1 == q) last[j] = front[q];
+                if (t >= 0) last[j].raw.load(x + t * a.x_row);
+            }
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) {
+                unsigned* to = reinterpret_cast<unsigned*>(state_out + state_at + j * state_row);
+#pragma unroll
+                for (int i = 0; i < Raw<kF32, kG>::kWords; i += 4)
+                    *reinterpret_cast<uint4v*>(to + i) = uint4v{last[j].raw.word[i], last[j].raw.word[i + 1], last[j].raw.word[i + 2], last[j].raw.word[i + 3]};
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) front[j].raw.load(x + (p.first - (W - 1) + j) * a.x_row);   // run >= W - 1: rows of the sequence
+    }
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) front[j].get(win[j + 1]);
+    Row<kF32> now[kBatch], next[kBatch];
+    auto ask = [&](int t, Row<kF32>(&r)[kBatch]) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            if (t + i < p.end) r[i].raw.load(x + (t + i) * a.x_row);
+    };
+    char* to = out + (p.row0 * a.D + ch) * kItem;
+    ask(p.first, now);
+    for (int t = p.first; t < p.end; t += kBatch) {
+        ask(t + kBatch, next);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            if (t + i >= p.end) break;
+            float y[kG];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                for (int e = 0; e < kG; ++e) win[j][e] = win[j + 1][e];
+            now[i].get(win[W - 1]);
+#pragma unroll
+            for (int e = 0; e < kG; ++e) {
+                float v = taps.bias[e];
+#pragma unroll
+                for (int j = 0; j < W; ++j) v = __builtin_fmaf(taps.w[j][e], win[j][e], v);
+                y[e] = a.silu ? v * sigmoid_of(v) : v;
+            }
+            store<kF32>(to + static_cast<long long>(t + i) * state_row, y);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) now[i] = next[i];
+    }
+}
+
+template <int W, bool kF32>
+__global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvArgs a, char* out, char* state_out, int groups) {
+    constexpr int kItem = kF32 ? 4 : 2;
+    const long long item = static_cast<long long>(blockIdx.x) * kConvThreads + threadIdx.x;
+    if (item >= static_cast<long long>(groups) * a.B) return;
+    const int b = static_cast<int>(item / groups), ch = static_cast<int>(item - static_cast<long long>(b) * groups) * kG;
+    const long long row = static_cast<long long>(a.D) * kItem, state_at = static_cast<long long>(b) * (W - 1) * row + ch * kItem;
+    Taps<W> taps;
+    Row<kF32> in[W];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        in[j].raw.none();
+        if (a.state_in) in[j].raw.load(static_cast<const char*>(a.state_in) + state_at + j * row);
+    }
+    in[W - 1].raw.load(static_cast<const char*>(a.x) + b * a.x_row + ch * kItem);
+    taps.load(a, ch);
+    float y[kG];
+#pragma unroll
+    for (int e = 0; e < kG; ++e) {
+        float v = taps.bias[e];
+#pragma unroll
+        for (int j = 0; j < W; ++j) v = __builtin_fmaf(taps.w[j][e], in[j].raw[e], v);
+        y[e] = a.silu ? v * sigmoid_of(v) : v;
+    }
+    store<kF32>(out + b * row + ch * kItem, y);
+    if (!state_out) return;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        unsigned* to = reinterpret_cast<unsigned*>(state_out + state_at + j * row);
+#pragma unroll
+        for (int i = 0; i < Raw<kF32, kG>::kWords; i += 4)
+            *reinterpret_cast<uint4v*>(to + i) = uint4v{in[j + 1].raw.word[i], in[j + 1].raw.word[i + 1], in[j + 1].raw.word[i + 2], in[j + 1].raw.word[i + 3]};
+    }
+}
+
+// Where segment seg of the sequence whose first token has this row leaves its sums: a segment of sequence b + 1 starts at least as many rows later as
+// b has, so no two places meet, and there are at most rows / seg_len + B of them.
+__device__ __forceinline__ long long sums_place(const ConvArgs& a, int b, long long row0, int seg) { return row0 / a.seg_len + seg + b; }
+
+template <int W, bool kF32>
+__global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a, const char* dout, const char* dstate_out, char* dx, char* dstate_in,
+                                                                     float* partials, int across, int run) {
+    constexpr int kItem = kF32 ? 4 : 2;
+    __shared__ float meet[kConvThreads / 2][(W + 1) * kG + 1];
+    const int column = threadIdx.x % a.lanes, slice = threadIdx.x / a.lanes;
+    const int block = blockIdx.x % across, at = blockIdx.x / across, b = at % a.B, seg = at / a.B;
+    const int ch = (block * a.lanes + column) * kG;
+    const bool there = ch < a.D;
+    const Place p = place_of(a, b, seg, slice, run);
+    const bool head = seg == 0 && slice == 0;
+    if (static_cast<long long>(seg) * a.seg_len >= p.len && seg > 0) return;      // (the whole workgroup)
+    float sums[W + 1][kG];
+#pragma unroll
+    for (int j = 0; j <= W; ++j)
+#pragma unroll
+        for (int e = 0; e < kG; ++e) sums[j][e] = 0.f;
+    if (there && (p.first < p.end || head)) {
+        const long long dense = static_cast<long long>(a.D) * kItem, state_at = static_cast<long long>(b) * (W - 1) * dense + ch * kItem;
+        const char* x = static_cast<const char*>(a.x) + p.row0 * a.x_row + ch * kItem;
+        const char* dy = dout + p.row0 * dense + ch * kItem;
+        char* to = dx + p.row0 * a.x_row + ch * kItem;
+        Taps<W> taps;
+        taps.load(a, ch);
+        float win[W][kG], dp[W][kG];                           // dp[W - 1]: of the token at hand
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < kG; ++e) dp[j][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            Row<kF32> r;
+            r.raw.none();
+            if (!head) r.raw.load(x + (p.first - (W - 1) + j) * a.x_row);
+            else if (a.state_in) r.raw.load(static_cast<const char*>(a.state_in) + state_at + j * dense);
+            r.get(win[j + 1]);
+        }
+        // Behind this thread's own tokens W - 1 more, whose dp its last inputs have a share in.
+        const int stop = p.first + (p.end - p.first) + W - 1;
+        constexpr int kBatch = 4;
+        Row<kF32> xs[2][kBatch], ds[2][kBatch];
+        auto ask = [&](int t, int which) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                xs[which][i].raw.none();
+                ds[which][i].raw.none();
+                if (t + i < stop && t + i < p.len) {
+                    xs[which][i].raw.load(x + (t + i) * a.x_row);
+                    ds[which][i].raw.load(dy + (t + i) * dense);
+                }
+            }
+        };
+        auto one = [&](int t, const Row<kF32>& xr, const Row<kF32>& dr) {
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                for (int e = 0; e < kG; ++e) {
+                    win[j][e] = win[j + 1][e];
+                    dp[j][e] = dp[j + 1][e];
+                }
+            xr.get(win[W - 1]);
+            dr.get(dp[W - 1]);
+            const bool own = t < p.end;
+#pragma unroll
+            for (int e = 0; e < kG; ++e) {
+                if (a.silu) {
+                    float v = taps.bias[e];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) v = __builtin_fmaf(taps.w[j][e], win[j][e], v);
+                    const float q = sigmoid_of(v);
+                    dp[W - 1][e] *= q * __builtin_fmaf(v, 1.f - q, 1.f);
+                }
+                if (own) {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) sums[j][e] = __builtin_fmaf(dp[W - 1][e], win[j][e], sums[j][e]);
+                    sums[W][e] += dp[W - 1][e];
+                }
+            }
+            const int s = t - (W - 1);                         // the input that has all its shares now
+            if (s < (head ? -(W - 1) : p.first) || s >= p.end) return;
+            char* place = to + s * a.x_row;
+            if (s < 0) {
+                if (!dstate_in) return;
+                place = dstate_in + state_at + t * dense;
+            }
+            float v[kG];
+#pragma unroll
+            for (int e = 0; e < kG; ++e) {
+                v[e] = 0.f;
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[e] = __builtin_fmaf(taps.w[j][e], dp[W - 1 - j][e], v[e]);
+            }
+            if (dstate_out && s >= p.len - (W - 1)) {
+                Row<kF32> r;
+                r.raw.load(dstate_out + state_at + (s - p.len + W - 1) * dense);
+#pragma unroll
+                for (int e = 0; e < kG; ++e) v[e] += r.raw[e];
+            }
+            store<kF32>(place, v);
+        };
+        ask(p.first, 0);
+        for (int t = p.first; t < stop; t += 2 * kBatch) {
+            ask(t + kBatch, 1);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (t + i < stop) one(t + i, xs[0][i], ds[0][i]);
+            ask(t + 2 * kBatch, 0);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (t + kBatch + i < stop) one(t + kBatch + i, xs[1][i], ds[1][i]);
+        }
+    }
+    if (!partials) return;
+    // the slices' sums meet, half of them at a time
+    for (int half = kConvThreads / 2; half >= a.lanes; half /= 2) {
+        if (static_cast<int>(threadIdx.x) >= half && static_cast<int>(threadIdx.x) < 2 * half)
+#pragma unroll
+            for (int j = 0; j <= W; ++j)
+#pragma unroll
+                for (int e = 0; e < kG; ++e) meet[threadIdx.x - half][j * kG + e] = sums[j][e];
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < half)
+#pragma unroll
+            for (int j = 0; j <= W; ++j)
+#pragma unroll
+                for (int e = 0; e < kG; ++e) sums[j][e] += meet[threadIdx.x][j * kG + e];
+        __syncthreads();
+    }
+    if (slice != 0 || !there) return;
+    float* to = partials + sums_place(a, b, p.row0, seg) * (W + 1) * a.D + ch;
+#pragma unroll
+    for (int j = 0; j <= W; ++j)
+#pragma unroll
+        for (int e = 0; e < kG; e += 4)
+            *reinterpret_cast<float4v*>(to + static_cast<long long>(j) * a.D + e) = float4v{sums[j][e], sums[j][e + 1], sums[j][e + 2], sums[j][e + 3]};
+}
+
+// dw [D][W] and dbias [D]: 64 values a workgroup, the segments' shares in sixteen turns, in the order of sequences and segments.
+constexpr int kFoldSlices = 16;
+__global__ __launch_bounds__(64 * kFoldSlices) void conv_fold_kernel(ConvArgs a, const float* partials, float* dw, float* dbias) {
+    __shared__ float meet[kFoldSlices][64];
+    const int lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), values = (a.W + 1) * a.D;
+    const int value = blockIdx.x * 64 + lane;
+    float sum = 0.f;
+    long long before = 0;                                      // segments of the sequences in front
+    for (int b = 0; b < a.B; ++b) {
+        const Place p = place_of(a, b, 0, 0, 1);
+        const long long segs = p.len > 0 ? (p.len - 1) / a.seg_len + 1 : 1;
+        for (long long s = (turn - before % kFoldSlices + kFoldSlices) % kFoldSlices; s < segs; s += kFoldSlices)
+            if (value < values) sum += partials[sums_place(a, b, p.row0, static_cast<int>(s)) * values + value];
+        before += segs;
+    }
+    meet[turn][lane] = sum;
+    __syncthreads();
+    if (turn != 0 || value >= values) return;
+#pragma unroll
+    for (int i = 1; i < kFoldSlices; ++i) sum += meet[i][lane];
+    const int tap = value / a.D, ch = value - tap * a.D;
+    if (tap == a.W) dbias[ch] = sum;
+    else dw[static_cast<long long>(ch) * a.W + tap] = sum;
+}
+
+template <typename F>
+hipError_t by_taps(int W, bool f32, F f) {
+    auto one = [&](auto w) { return f32 ? f(w, std::true_type()) : f(w, std::false_type()); };
+    if (W == 2) return one(std::integral_constant<int, 2>());
+    if (W == 3) return one(std::integral_constant<int, 3>());
+    return one(std::integral_constant<int, 4>());
+}
+
+int across_of(const ConvArgs& a) { return (a.D / kG + a.lanes - 1) / a.lanes; }
+
+}  // namespace
+
+ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward) {
+    ConvPlan p;
+    const int groups = D / kG;
+    p.lanes = 64;
+    while (p.lanes > 1 && p.lanes / 2 >= groups) p.lanes /= 2;
+    if (groups > 32 && groups < 256 && groups % 64 != 0 && groups % 64 <= 32) p.lanes = 32;
+    const int slices = kConvThreads / p.lanes, across = (groups + p.lanes - 1) / p.lanes;
+    int run = backward ? 32 : 16;
+    while (run > 4 && rows * across / (slices * run) < 1024) run /= 2;
+    p.seg_len = slices * run;
+    p.segs = T > 0 ? (T - 1) / p.seg_len + 1 : 1;
+    p.workgroups = static_cast<long long>(p.segs) * B * across;
+    return p;
+}
+
+hipError_t launch_conv(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream) {
+    return by_taps(a.W, f32, [&](auto w, auto wide) {
+        const int across = across_of(a);
+        hipLaunchKernelGGL((conv_kernel<decltype(w)::value, decltype(wide)::value>), dim3(static_cast<unsigned>(a.segs) * a.B * across), dim3(kConvThreads),
+                           0, stream, a, static_cast<char*>(out), static_cast<char*>(state_out), across, a.seg_len / (kConvThreads / a.lanes));
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_conv_step(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream) {
+    return by_taps(a.W, f32, [&](auto w, auto wide) {
+        const int groups = a.D / kG;
+        const long long items = static_cast<long long>(groups) * a.B;
+        hipLaunchKernelGGL((conv_step_kernel<decltype(w)::value, decltype(wide)::value>), dim3(static_cast<unsigned>((items + kConvThreads - 1) / kConvThreads)),
+                           dim3(kConvThreads), 0, stream, a, static_cast<char*>(out), static_cast<char*>(state_out), groups);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void* dstate_out, void* dx, float* dw, float* dbias, void* dstate_in,
+                                float* partials, bool f32, hipStream_t stream) {
+    const int across = across_of(a);
+    const hipError_t err = by_taps(a.W, f32, [&](auto w, auto wide) {
+        hipLaunchKernelGGL((conv_backward_kernel<decltype(w)::value, decltype(wide)::value>), dim3(static_cast<unsigned>(a.segs) * a.B * across),
+                           dim3(kConvThreads), 0, stream, a, static_cast<const char*>(dout), static_cast<const char*>(dstate_out), static_cast<char*>(dx),
+                           static_cast<char*>(dstate_in), dw ? partials : nullptr, across, a.seg_len / (kConvThreads / a.lanes));
+        return hipGetLastError();
+    });
+    return err != hipSuccess || !dw ? err : launch_conv_fold(a, dw, dbias, partials, stream);
+}
+
+hipError_t launch_conv_fold(const ConvArgs& a, float* dw, float* dbias, const float* partials, hipStream_t stream) {
+    hipLaunchKernelGGL(conv_fold_kernel, dim3((static_cast<unsigned>(a.D) * (a.W + 1) + 63) / 64), dim3(64 * kFoldSlices), 0, stream, a, partials, dw, dbias);
+    return hipGetLastError();
+}
+
+}  // namespace wkv6
