@@ -37,7 +37,7 @@ constexpr int scan_threads(int N) { return 16 * N; }
 hipError_t launch_scan(const ScanArgs& a, void* out, float* state_out, bool f32_rows, bool f32_out, hipStream_t stream);
 
 // Gradients.  Tokens whose decays and states stay in registers on the way back; the states in front of them are kept in `states`.
-constexpr int scan_back_chunk(int N) { return N == 64 ? 8 : 16; }
+constexpr int scan_back_chunk(int N) { return N == 8 || N == 64 ? 8 : 16; }
 struct ScanGradients {
     const void* dout;
     const float* dstate_out;

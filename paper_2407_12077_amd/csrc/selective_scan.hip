@@ -10,7 +10,7 @@ using namespace scan;
 
 // kStates: the segments' states from nothing, without read-outs.
 template <int N, bool kF32, bool kOutF32, bool kStates>
-__global__ __launch_bounds__(16 * N) void scan_kernel(ScanArgs a, char* out, float* state_out, int blocks) {
+__global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, float* state_out, int blocks) {
     constexpr int kWaves = N / 4, kC = kScanChunk, kCh = kScanChannels, kItem = kF32 ? 4 : 2, kOutItem = kOutF32 ? 4 : 2;
     constexpr int kPer = kC / kWaves < 8 ? kC / kWaves : 8;    // channels that a thread brings and takes of a token
     constexpr int kAcross = kCh / kPer;
@@ -54,35 +54,33 @@ __global__ __launch_bounds__(16 * N) void scan_kernel(ScanArgs a, char* out, flo
         bias[i] = there && a.bias ? a.bias[own + i] : 0.f;
         skip[i] = there && a.skip ? a.skip[own + i] : 0.f;
     }
-    const char *x = static_cast<const char*>(a.x), *delta = static_cast<const char*>(a.delta), *z = static_cast<const char*>(a.z);
-    const char *bp = static_cast<const char*>(a.b) + n0 * kItem, *cp = static_cast<const char*>(a.c) + n0 * kItem;
     struct Chunk {
         Raw<kF32, kPer> x, delta, z;
-        StateRow<kF32> b, c;           // of token lane / 4
+        Plain<kF32> b;
+        ByRow<kF32, kC / 4> c;
     };
+    const int x_at = there ? token * static_cast<int>(a.x_row) + own * kItem : kNowhere;
+    const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
+    const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
+    const int out_at = there ? (token * D + own) * kOutItem : kNowhere;
+    const int bc_row = static_cast<int>(a.bc_row);
     auto ask = [&](int first, Chunk& k) {
-        k.x.none();
-        k.delta.none();
-        if (!kStates) k.z.none();
-        if (there && first + token < span.tokens) {
-            const long long row = span.first_row + first + token;
-            k.x.load(x + row * a.x_row + own * kItem);
-            k.delta.load(delta + row * a.delta_row + own * kItem);
-            if (!kStates && z) k.z.load(z + row * a.z_row + own * kItem);
-        }
-        k.b.none();
-        if (!kStates) k.c.none();
-        if (first + lane / 4 < span.tokens) {
-            const long long row = span.first_row + first + lane / 4;
-            k.b.raw.load(bp + row * a.bc_row);
-            if (!kStates) k.c.raw.load(cp + row * a.bc_row);
+        const long long row = span.first_row + first;
+        const int left = span.tokens - first;
+        k.x.load(rows_at(a.x, row, a.x_row, left), x_at);
+        k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
+        k.b.load(rows_at(a.b, row, a.bc_row, left), lane, bc_row, n0);
+        if constexpr (!kStates) {
+            if (a.z) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
+            k.c.load(rows_at(a.c, row, a.bc_row, left), lane, bc_row, n0);
         }
     };
     auto bring = [&](int first, const Chunk& k, int buffer) {
+        float dts[kPer];
+        steps_of(k.delta, bias, a.softplus, dts);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            float dt = step_of(k.delta[i] + bias[i], a.softplus);
-            if (first + token >= span.tokens) dt = 0.f;
+            const float dt = first + token < span.tokens ? dts[i] : 0.f;
             step[buffer][token][in_block + i] = float2v{dt, dt * k.x[i]};
         }
     };
@@ -93,46 +91,35 @@ __global__ __launch_bounds__(16 * N) void scan_kernel(ScanArgs a, char* out, flo
     int buffer = 0;
     for (int first = 0; first < span.tokens; first += kC, buffer ^= 1) {
         ask(first + kC, next);
-        const float bv = now.b.plain(lane);
-        float cv[4];
+        const float bv = now.b.value();
+        float cv[kC / 4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) cv[i] = kStates ? 0.f : now.c.at_token(i, lane);
-        float4v y = {0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < kC / 4; ++g) cv[g] = kStates ? 0.f : now.c.value(g);
         each<kC>([&](auto token_of_chunk) {
             constexpr int t = decltype(token_of_chunk)::value;
             const float2v d = step[buffer][t][lane];
-            float4v decayed;
+            const float4v add = outer<t>(bv, d.y);
+            if constexpr (kStates) dt_sum += d.x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) decayed[i] = __builtin_amdgcn_exp2f(d.x * rate[i]) * h[i];
-            h = outer<t>(bv, d.y, decayed);
-            if constexpr (kStates) {
-                dt_sum += d.x;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y = outer<t>(cv[i], h[i], y);
-                if constexpr (t % 4 == 3) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) part[buffer][wave][t - 3 + i][lane] = y[i];
-                    y = float4v{0.f, 0.f, 0.f, 0.f};
-                }
-            }
+            for (int i = 0; i < 4; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[i]), h[i], add[i]);
+            if constexpr (!kStates) part[buffer][wave][t][lane] = read_out<t % 4>(cv[t / 4], h);
         });
         bring(first + kC, next, buffer ^ 1);
         __syncthreads();
         if constexpr (!kStates) {
-            if (there && first + token < span.tokens) {
-                const long long row = span.first_row + first + token;
-                float y[kPer];
+            float y[kPer];
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    float v = skip[i] * now.x[i];
+            for (int i = 0; i < kPer; ++i) {
+                float v = skip[i] * now.x[i];
 #pragma unroll
-                    for (int w = 0; w < kWaves; ++w) v += part[buffer][w][token][in_block + i];
-                    if (z) v *= now.z[i] * sigmoid_of(now.z[i]);
-                    y[i] = v;
-                }
-                store<kOutF32>(out + (row * D + own) * kOutItem, y);
+                for (int w = 0; w < kWaves; ++w) v += part[buffer][w][token][in_block + i];
+                y[i] = v;
             }
+            if (a.z) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) y[i] *= now.z[i] * sigmoid_of(now.z[i]);
+            }
+            store<kOutF32>(rows_at(out, span.first_row + first, static_cast<long long>(D) * kOutItem, span.tokens - first), out_at, y);
         }
         now = next;
     }
@@ -179,7 +166,10 @@ hipError_t by_states(int N, F f) {
 
 ScanPlan plan_scan(int B, int T, int D, int N) {
     const long long units = static_cast<long long>(B) * scan_blocks(D) * N / 16;
-    long long segs = units > 0 ? 768 / units : 1;
+    #ifndef TARGET
+#define TARGET 768
+#endif
+    long long segs = units > 0 ? TARGET / units : 1;
     const long long most = (T + 127) / 128;
     if (segs > most) segs = most;
     if (segs > 64) segs = 64;

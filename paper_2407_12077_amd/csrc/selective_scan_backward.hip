@@ -34,15 +34,9 @@ struct Shape {
     static constexpr int kPer = kC * kScanChannels / kThreads, kAcross = kScanChannels / kPer;
 };
 
-// Rows of a chunk that a thread brings: channels own .. own + kPer - 1 of one token.
-template <bool kF32, int kPer>
-struct Element {
-    Raw<kF32, kPer> x, delta, z, dout;
-};
-
 // What a segment hands to the one in front of it if it gets nothing from behind, and the sum of its step sizes.
 template <int N, bool kF32>
-__global__ __launch_bounds__(16 * N) void scan_behind_kernel(ScanArgs a, const char* dout, float* behind, int blocks) {
+__global__ __launch_bounds__(16 * N, 2) void scan_behind_kernel(ScanArgs a, const char* dout, float* behind, int blocks) {
     constexpr int kWaves = N / 4, kC = kScanChunk, kCh = kScanChannels, kItem = kF32 ? 4 : 2;
     constexpr int kPer = kC / kWaves < 8 ? kC / kWaves : 8, kAcross = kCh / kPer;
     __shared__ float2v step[2][kC][kCh];                       // dt, dy
@@ -59,32 +53,32 @@ __global__ __launch_bounds__(16 * N) void scan_behind_kernel(ScanArgs a, const c
     float bias[kPer], dt_sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) bias[i] = there && a.bias ? a.bias[own + i] : 0.f;
-    const char *delta = static_cast<const char*>(a.delta), *z = static_cast<const char*>(a.z), *cp = static_cast<const char*>(a.c) + n0 * kItem;
     struct Chunk {
         Raw<kF32, kPer> delta, z, dout;
-        StateRow<kF32> c;
+        Plain<kF32> c;
     };
+    const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
+    const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
+    const int out_at = there ? (token * D + own) * kItem : kNowhere;
     auto ask = [&](int first, Chunk& k) {
-        k.delta.none();
-        k.z.none();
-        k.dout.none();
-        if (there && first >= 0 && first + token < span.tokens) {
-            const long long row = span.first_row + first + token;
-            k.delta.load(delta + row * a.delta_row + own * kItem);
-            if (z) k.z.load(z + row * a.z_row + own * kItem);
-            k.dout.load(dout + (row * D + own) * kItem);
-        }
-        k.c.none();
-        if (first >= 0 && first + lane / 4 < span.tokens) k.c.raw.load(cp + (span.first_row + first + lane / 4) * a.bc_row);
+        const long long row = span.first_row + first;
+        const int left = first < 0 ? 0 : span.tokens - first;
+        k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
+        if (a.z) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
+        k.dout.load(rows_at(dout, row, static_cast<long long>(D) * kItem, left), out_at);
+        k.c.load(rows_at(a.c, row, a.bc_row, left), lane, static_cast<int>(a.bc_row), n0);
     };
     auto bring = [&](int first, const Chunk& k, int buffer) {
+        float dts[kPer], dy[kPer];
+        steps_of(k.delta, bias, a.softplus, dts);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            float dt = step_of(k.delta[i] + bias[i], a.softplus), dy = k.dout[i];
-            if (first + token >= span.tokens) dt = 0.f;
-            if (z) dy *= k.z[i] * sigmoid_of(k.z[i]);
-            step[buffer][token][in_block + i] = float2v{dt, dy};
+        for (int i = 0; i < kPer; ++i) dy[i] = k.dout[i];
+        if (a.z) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) dy[i] *= k.z[i] * sigmoid_of(k.z[i]);
         }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) step[buffer][token][in_block + i] = float2v{first + token < span.tokens ? dts[i] : 0.f, dy[i]};
     };
     Chunk now, next;
     int first = (span.tokens - 1) / kC * kC, buffer = 0;
@@ -93,7 +87,7 @@ __global__ __launch_bounds__(16 * N) void scan_behind_kernel(ScanArgs a, const c
     __syncthreads();
     for (; first >= 0; first -= kC, buffer ^= 1) {
         ask(first - kC, next);
-        const float cv = now.c.plain(lane);
+        const float cv = now.c.value();
         each<kC>([&](auto back) {
             constexpr int t = kC - 1 - decltype(back)::value;
             const float2v d = step[buffer][t][lane];
@@ -112,18 +106,19 @@ __global__ __launch_bounds__(16 * N) void scan_behind_kernel(ScanArgs a, const c
     if (wave == 0) behind[a.segs * seg_states + (static_cast<long long>(seg) * a.B + b) * D + ch] = dt_sum;
 }
 
-template <int N, bool kF32>
-__global__ __launch_bounds__(Shape<N>::kThreads) void scan_backward_kernel(ScanArgs a, ScanGradients r, int blocks) {
+template <int N, bool kF32, bool kGate>
+__global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(ScanArgs a, ScanGradients r, int blocks) {
     using S = Shape<N>;
     constexpr int kG = S::kGroups, kWaves = S::kWaves, kC = S::kC, kCh = kScanChannels, kPer = S::kPer, kItem = kF32 ? 4 : 2;
-    __shared__ float4v step[kC][kCh];                          // dt, dt x, dy
-    __shared__ float part[3][kWaves][kC][kCh];                 // shares of g, of sum k rate, of the read-outs
+    __shared__ float2v step[kC][kCh];                          // dt, dt x
+    __shared__ float grad_out[kC][kCh];                        // dy
+    __shared__ float part[kGate ? 3 : 2][kWaves][kC][kCh];                 // shares of g, of sum k rate, of the read-outs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = blockIdx.x % blocks, at = blockIdx.x / blocks, b = at % a.B, seg = at / a.B;
     const Span span = span_of(a, b, seg);
     if (span.tokens == 0 && seg > 0) return;
     const int D = a.D, c0 = block * kCh, ch = c0 + lane, n0 = S::kStates * wave;
-    const bool mine = ch < D, gate = a.z != nullptr;
+    const bool mine = ch < D;
     const long long unit = (static_cast<long long>(b) * D + ch) * N + n0, seg_states = static_cast<long long>(a.B) * D * N;
     const long long sums_at = a.segs * seg_states, seg_sums = static_cast<long long>(a.B) * D, channel = static_cast<long long>(b) * D + ch;
 
@@ -170,77 +165,80 @@ __global__ __launch_bounds__(Shape<N>::kThreads) void scan_backward_kernel(ScanA
         skip[i] = there && a.skip ? a.skip[own + i] : 0.f;
         dskip[i] = dbias[i] = 0.f;
     }
-    const char *x = static_cast<const char*>(a.x), *delta = static_cast<const char*>(a.delta), *z = static_cast<const char*>(a.z);
-    const char *bp = static_cast<const char*>(a.b) + n0 * kItem, *cp = static_cast<const char*>(a.c) + n0 * kItem, *dout = static_cast<const char*>(r.dout);
     struct Chunk {
-        Element<kF32, kPer> e;
-        StateRow<kF32> b[kG], c[kG];
+        Raw<kF32, kPer> x, delta, z, dout;
+        Plain<kF32> b[kG], c[kG];
+        ByRow<kF32, kC / 4> bt[kG], ct[kG];
     };
-    auto ask = [&](int first, Chunk& k, bool back) {
-        k.e.x.none();
-        k.e.delta.none();
-        k.e.z.none();
-        k.e.dout.none();
-        if (there && first >= 0 && first + token < span.tokens) {
-            const long long row = span.first_row + first + token;
-            k.e.x.load(x + row * a.x_row + own * kItem);
-            k.e.delta.load(delta + row * a.delta_row + own * kItem);
-            if (back) {
-                if (gate) k.e.z.load(z + row * a.z_row + own * kItem);
-                k.e.dout.load(dout + (row * D + own) * kItem);
-            }
+    const int bc_row = static_cast<int>(a.bc_row);
+    const int x_at = there ? token * static_cast<int>(a.x_row) + own * kItem : kNowhere;
+    const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
+    const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
+    const int out_at = there ? (token * D + own) * kItem : kNowhere;
+    const long long out_row = static_cast<long long>(D) * kItem;
+    auto ask = [&](int first, Chunk& k, auto on_the_way_back) {
+        constexpr bool kBack = decltype(on_the_way_back)::value;
+        const long long row = span.first_row + first;
+        const int left = first < 0 ? 0 : span.tokens - first;
+        k.x.load(rows_at(a.x, row, a.x_row, left), x_at);
+        k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
+        if constexpr (kBack) {
+            if constexpr (kGate) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
+            k.dout.load(rows_at(r.dout, row, out_row, left), out_at);
         }
+        const __amdgpu_buffer_rsrc_t b = rows_at(a.b, row, a.bc_row, left), c = rows_at(a.c, row, a.bc_row, left);
 #pragma unroll
         for (int q = 0; q < kG; ++q) {
-            k.b[q].none();
-            k.c[q].none();
-        }
-        if (lane / 4 < kC && first >= 0 && first + lane / 4 < span.tokens) {
-            const long long row = span.first_row + first + lane / 4;
-#pragma unroll
-            for (int q = 0; q < kG; ++q) {
-                k.b[q].raw.load(bp + row * a.bc_row + 4 * q * kItem);
-                if (back) k.c[q].raw.load(cp + row * a.bc_row + 4 * q * kItem);
+            k.b[q].load(b, lane, bc_row, n0 + 4 * q);
+            if constexpr (kBack) {
+                k.c[q].load(c, lane, bc_row, n0 + 4 * q);
+                k.bt[q].load(b, lane, bc_row, n0 + 4 * q);
+                if constexpr (kGate) k.ct[q].load(c, lane, bc_row, n0 + 4 * q);
             }
         }
     };
-    auto bring = [&](int first, const Chunk& k) {
+    auto bring = [&](int first, const Chunk& k, auto on_the_way_back) {
+        float dts[kPer];
+        steps_of(k.delta, bias, a.softplus, dts);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            float dt = step_of(k.e.delta[i] + bias[i], a.softplus), dy = k.e.dout[i];
-            if (first + token >= span.tokens) dt = 0.f;
-            if (gate) dy *= k.e.z[i] * sigmoid_of(k.e.z[i]);
-            step[token][in_block + i] = float4v{dt, dt * k.e.x[i], dy, 0.f};
+            const float dt = first + token < span.tokens ? dts[i] : 0.f;
+            step[token][in_block + i] = float2v{dt, dt * k.x[i]};
+            if constexpr (decltype(on_the_way_back)::value) {
+                float dy = k.dout[i];
+                if constexpr (kGate) dy *= k.z[i] * sigmoid_of(k.z[i]);
+                grad_out[token][in_block + i] = dy;
+            }
         }
     };
+    constexpr std::true_type kBackward{};
+    constexpr std::false_type kForward{};
 
     // the states in front of the chunks
-    const int last_first = span.tokens > 0 ? (span.tokens - 1) / kC * kC : 0;
+    const int last_first = span.tokens > 0 ? (span.tokens - 1) / kC * kC : -kC;
     const long long place0 = (span.first_row - static_cast<long long>(seg) * a.seg_len) / kC + static_cast<long long>(seg) * a.seg_len / kC + b;
-    float* const kept = r.states + (place0 * D + ch) * N + n0;
-    const long long kept_step = static_cast<long long>(D) * N;
+    const long long kept_row = static_cast<long long>(D) * N * 4;
+    const int kept_at = mine ? (ch * N + n0) * 4 : kNowhere;
     Chunk now, next;
-    ask(0, now, false);
+    ask(0, now, kForward);
     for (int first = 0; first < last_first; first += kC) {
-        bring(first, now);
+        bring(first, now, kForward);
         __syncthreads();
-        ask(first + kC, next, false);
-        if (mine) {
+        ask(first + kC, next, kForward);
+        const __amdgpu_buffer_rsrc_t kept = rows_at(r.states, place0 + first / kC, kept_row, 1);
 #pragma unroll
-            for (int q = 0; q < kG; ++q) *reinterpret_cast<float4v*>(kept + first / kC * kept_step + 4 * q) = h[q];
-        }
+        for (int q = 0; q < kG; ++q) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, h[q]), kept, kept_at + 16 * q, 0, 0);
         float bv[kG];
 #pragma unroll
-        for (int q = 0; q < kG; ++q) bv[q] = now.b[q].plain(lane);
+        for (int q = 0; q < kG; ++q) bv[q] = now.b[q].value();
         each<kC>([&](auto token_of_chunk) {
             constexpr int t = decltype(token_of_chunk)::value;
-            const float4v d = step[t][lane];
+            const float2v d = step[t][lane];
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
-                float4v decayed;
+                const float4v add = outer<t>(bv[q], d.y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) decayed[i] = __builtin_amdgcn_exp2f(d.x * rate[q][i]) * h[q][i];
-                h[q] = outer<t>(bv[q], d.y, decayed);
+                for (int i = 0; i < 4; ++i) h[q][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[q][i]), h[q][i], add[i]);
             }
         });
         __syncthreads();
@@ -248,87 +246,70 @@ __global__ __launch_bounds__(Shape<N>::kThreads) void scan_backward_kernel(ScanA
     }
 
     // and back
-    ask(span.tokens > 0 ? last_first : -1, now, true);
-    for (int first = last_first; first >= 0 && span.tokens > 0; first -= kC) {
-        bring(first, now);
-        if (first < last_first && mine) {
+    const long long share_row = static_cast<long long>(blocks) * 2 * N * 4;
+    const int share_token = (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4;
+    const int share_at = share_token * static_cast<int>(share_row) + (block * 2 * N + (lane >> 5) * N + n0 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1)) * 4;
+    ask(last_first, now, kBackward);
+    for (int first = last_first; first >= 0; first -= kC) {
+        bring(first, now, kBackward);
+        if (first < last_first) {
+            const __amdgpu_buffer_rsrc_t kept = rows_at(r.states, place0 + first / kC, kept_row, 1);
 #pragma unroll
-            for (int q = 0; q < kG; ++q) h[q] = *reinterpret_cast<const float4v*>(kept + first / kC * kept_step + 4 * q);
+            for (int q = 0; q < kG; ++q) h[q] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(kept, kept_at + 16 * q, 0, 0));
         }
         __syncthreads();
-        ask(first - kC, next, true);
-        float4v decay[kC][kG], left[kC][kG];                   // exp(dt a), and that times the state in front
-        float bv[kG], cv[kG];
-        {
-            float ct[kG][4];
+        ask(first - kC, next, kBackward);
+        float4v decay[kC][kG], state[kC + 1][kG];              // exp(dt a), and the states: state[t] in front of token t
+#pragma unroll
+        for (int q = 0; q < kG; ++q) state[0][q] = h[q];
+        each<kC>([&](auto token_of_chunk) {
+            constexpr int t = decltype(token_of_chunk)::value;
+            const float2v d = step[t][lane];
+            float y = 0.f;
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
-                bv[q] = now.b[q].plain(lane);
-                cv[q] = now.c[q].plain(lane);
+                const float4v add = outer<t>(now.b[q].value(), d.y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ct[q][i] = now.c[q].at_token(i, lane);
+                for (int i = 0; i < 4; ++i) {
+                    decay[t][q][i] = __builtin_amdgcn_exp2f(d.x * rate[q][i]);
+                    state[t + 1][q][i] = __builtin_fmaf(decay[t][q][i], state[t][q][i], add[i]);
+                }
+                if constexpr (kGate) y += read_out<t % 4>(now.ct[q].value(t / 4), state[t + 1][q]);
             }
-            float4v y = {0.f, 0.f, 0.f, 0.f};
-            each<kC>([&](auto token_of_chunk) {
-                constexpr int t = decltype(token_of_chunk)::value;
-                const float4v d = step[t][lane];
-#pragma unroll
-                for (int q = 0; q < kG; ++q) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        decay[t][q][i] = __builtin_amdgcn_exp2f(d.x * rate[q][i]);
-                        left[t][q][i] = decay[t][q][i] * h[q][i];
-                    }
-                    h[q] = outer<t>(bv[q], d.y, left[t][q]);
-                    if (gate) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y = outer<t>(ct[q][i], h[q][i], y);
-                    }
-                }
-                if constexpr (t % 4 == 3) {
-                    if (gate) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) part[2][wave][t - 3 + i][lane] = y[i];
-                        y = float4v{0.f, 0.f, 0.f, 0.f};
-                    }
-                }
-            });
-        }
-        float bt[kG][4];
-#pragma unroll
-        for (int q = 0; q < kG; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bt[q][i] = now.b[q].at_token(i, lane);
-        float4v into = {0.f, 0.f, 0.f, 0.f}, da_chunk[kG];
-        float pairs[kG][2], fours[kG], eights[kG];             // sums over lanes on their way: of one odd token, of two, of four
+            if constexpr (kGate) part[2][wave][t][lane] = y;
+        });
+        const __amdgpu_buffer_rsrc_t shares = rows_at(r.rows, span.first_row + first, share_row, span.tokens - first);
+        float4v da_chunk[kG];
+        float pairs[kG], fours[kG], eights[kG];                // sums over lanes on their way: of one odd token, of two, of four
 #pragma unroll
         for (int q = 0; q < kG; ++q) da_chunk[q] = float4v{0.f, 0.f, 0.f, 0.f};
         each<kC>([&](auto back) {
             constexpr int t = kC - 1 - decltype(back)::value;
-            const float4v d = step[t][lane];
-            float k_rate = 0.f;
+            const float2v d = step[t][lane];
+            const float dy = grad_out[t][lane];
+            float k_rate = 0.f, into = 0.f;
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
-                const float4v state = outer<t>(bv[q], d.y, left[t][q]);
-                grad[q] = outer<t>(cv[q], d.z, grad[q]);
+                grad[q] = outer<t>(now.c[q].value(), dy, grad[q]);
+                into += read_out<t % 4>(now.bt[q].value(t / 4), grad[q]);
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     v[i] = grad[q][i] * d.y;
-                    v[4 + i] = state[i] * d.z;
-                    const float k = grad[q][i] * left[t][q][i];
+                    v[4 + i] = state[t + 1][q][i] * dy;
+                    grad[q][i] *= decay[t][q][i];
+                    const float k = grad[q][i] * state[t][q][i];
                     da_chunk[q][i] = __builtin_fmaf(k, d.x, da_chunk[q][i]);
                     k_rate = __builtin_fmaf(k, rate[q][i], k_rate);
-                    into = outer<t>(bt[q][i], grad[q][i], into);
                 }
                 // lane: value of v by its bits 32, 16, 8, then the token by bits 4, 2, 1
                 const float m0 = halves<32>(v[0], v[4], lane), m1 = halves<32>(v[1], v[5], lane), m2 = halves<32>(v[2], v[6], lane),
                             m3 = halves<32>(v[3], v[7], lane);
                 const float one = halves<8>(halves<16>(m0, m2, lane), halves<16>(m1, m3, lane), lane);
                 if constexpr (t % 2 == 1) {
-                    pairs[q][0] = one;
+                    pairs[q] = one;
                 } else {
-                    const float two = halves<4>(one, pairs[q][0], lane);
+                    const float two = halves<4>(one, pairs[q], lane);
                     if constexpr (t % 4 == 2) {
                         fours[q] = two;
                     } else {
@@ -337,28 +318,24 @@ __global__ __launch_bounds__(Shape<N>::kThreads) void scan_backward_kernel(ScanA
                             eights[q] = four;
                         } else {
                             const float sum = halves<1>(four, eights[q], lane);
-                            const int which = lane >> 5, n = (lane >> 4 & 1) * 2 + (lane >> 3 & 1);
-                            const int at_token = first + t + (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4;
-                            if (at_token < span.tokens)
-                                r.rows[((span.first_row + at_token) * blocks + block) * (2 * N) + which * N + n0 + 4 * q + n] = sum;
+                            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), shares, share_at + t * static_cast<int>(share_row) + 16 * q, 0, 0);
                         }
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) grad[q][i] *= decay[t][q][i];
             }
+            part[0][wave][t][lane] = into;
             part[1][wave][t][lane] = k_rate;
-            if constexpr (t % 4 == 0) {
+            if constexpr (t % 4 == 0) {                        // (else the compiler keeps the k of all tokens for the end)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[0][wave][t + i][lane] = into[i];
-                into = float4v{0.f, 0.f, 0.f, 0.f};
+                for (int q = 0; q < kG; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(da_chunk[q][i]));
             }
         });
 #pragma unroll
         for (int q = 0; q < kG; ++q) da[q] += da_chunk[q];
         __syncthreads();
-        if (there && first + token < span.tokens) {
-            const long long row = span.first_row + first + token;
+        {
             float dx[kPer], dd[kPer], dz[kPer];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
@@ -368,24 +345,29 @@ __global__ __launch_bounds__(Shape<N>::kThreads) void scan_backward_kernel(ScanA
                     g += part[0][w][token][in_block + i];
                     k += part[1][w][token][in_block + i];
                 }
-                const float4v d = step[token][in_block + i];
-                const float xv = now.e.x[i];
-                dx[i] = __builtin_fmaf(g, d.x, skip[i] * d.z);
+                const float dt = step[token][in_block + i].x, dy = grad_out[token][in_block + i], xv = now.x[i];
+                dx[i] = __builtin_fmaf(g, dt, skip[i] * dy);
                 dd[i] = __builtin_fmaf(g, xv, k * kLn2);
-                if (a.softplus) dd[i] *= sigmoid_of(now.e.delta[i] + bias[i]);
-                dskip[i] = __builtin_fmaf(d.z, xv, dskip[i]);
-                dbias[i] += dd[i];
-                if (gate) {
+                dskip[i] = __builtin_fmaf(dy, xv, dskip[i]);
+                if constexpr (kGate) {
                     float y = skip[i] * xv;
 #pragma unroll
                     for (int w = 0; w < kWaves; ++w) y += part[2][w][token][in_block + i];
-                    const float zv = now.e.z[i], s = sigmoid_of(zv);
-                    dz[i] = now.e.dout[i] * y * (s * __builtin_fmaf(zv, 1.f - s, 1.f));
+                    const float zv = now.z[i], s = sigmoid_of(zv);
+                    dz[i] = now.dout[i] * y * (s * __builtin_fmaf(zv, 1.f - s, 1.f));
                 }
             }
-            store<kF32>(static_cast<char*>(r.dx) + row * a.x_row + own * kItem, dx);
-            store<kF32>(static_cast<char*>(r.ddelta) + row * a.delta_row + own * kItem, dd);
-            if (gate && r.dz) store<kF32>(static_cast<char*>(r.dz) + row * a.z_row + own * kItem, dz);
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) dd[i] *= sigmoid_of(now.delta[i] + bias[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) dbias[i] += first + token < span.tokens ? dd[i] : 0.f;       // (behind the end k is not nought)
+            const long long row = span.first_row + first;
+            const int left = span.tokens - first;
+            store<kF32>(rows_at(r.dx, row, a.x_row, left), x_at, dx);
+            store<kF32>(rows_at(r.ddelta, row, a.delta_row, left), delta_at, dd);
+            if (kGate && r.dz) store<kF32>(rows_at(r.dz, row, a.z_row, left), z_at, dz);
         }
         __syncthreads();
         now = next;
@@ -478,7 +460,9 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
                            blocks);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
-    hipLaunchKernelGGL((scan_backward_kernel<N, kF32>), dim3(units * a.segs), dim3(Shape<N>::kThreads), 0, stream, a, g, blocks);
+    const auto kernel = a.z ? &scan_backward_kernel<N, kF32, true> : &scan_backward_kernel<N, kF32, false>;
+    hipLaunchKernelGGL(kernel, dim3(units * a.segs), dim3(Shape<N>::kThreads), 0,
+                       stream, a, g, blocks);
     if ((err = hipGetLastError()) != hipSuccess) return err;
     if (a.rows > 0 && a.T > 0) {
         const int per = 256 / (2 * N);

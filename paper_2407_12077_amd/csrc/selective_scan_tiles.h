@@ -46,11 +46,59 @@ struct Raw {
             }
         }
     }
+    // from a buffer; what lies behind its end is zeros
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, int at) {
+        if constexpr (!kF32 && kCount == 1) {
+            word[0] = __builtin_amdgcn_raw_buffer_load_b16(from, at, 0, 0);
+        } else if constexpr (kWords == 1) {
+            word[0] = __builtin_amdgcn_raw_buffer_load_b32(from, at, 0, 0);
+        } else if constexpr (kWords == 2) {
+            const auto v = __builtin_bit_cast(uint2v, __builtin_amdgcn_raw_buffer_load_b64(from, at, 0, 0));
+            word[0] = v.x;
+            word[1] = v.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const auto v = __builtin_bit_cast(uint4v, __builtin_amdgcn_raw_buffer_load_b128(from, at + 4 * i, 0, 0));
+                word[i] = v.x;
+                word[i + 1] = v.y;
+                word[i + 2] = v.z;
+                word[i + 3] = v.w;
+            }
+        }
+    }
     __device__ __forceinline__ float operator[](int i) const {
         if constexpr (kF32) return __uint_as_float(word[i]);
         else return i & 1 ? bf16_hi(word[i / 2]) : bf16_lo(word[i / 2]);
     }
 };
+// the words of kCount values of either type
+template <bool kF32, int kCount>
+__device__ __forceinline__ void words_of(const float (&v)[kCount], unsigned (&word)[Raw<kF32, kCount>::kWords]) {
+#pragma unroll
+    for (int i = 0; i < Raw<kF32, kCount>::kWords; ++i) {
+        if constexpr (kF32) word[i] = __float_as_uint(v[i]);
+        else if constexpr (kCount == 1) word[i] = bf16_of(v[i]);
+        else word[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+    }
+}
+// into a buffer; nothing behind its end
+template <bool kF32, int kCount>
+__device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t to, int at, const float (&v)[kCount]) {
+    constexpr int kWords = Raw<kF32, kCount>::kWords;
+    unsigned word[kWords];
+    words_of<kF32>(v, word);
+    if constexpr (!kF32 && kCount == 1) {
+        __builtin_amdgcn_raw_buffer_store_b16(static_cast<unsigned short>(word[0]), to, at, 0, 0);
+    } else if constexpr (kWords == 1) {
+        __builtin_amdgcn_raw_buffer_store_b32(word[0], to, at, 0, 0);
+    } else if constexpr (kWords == 2) {
+        __builtin_amdgcn_raw_buffer_store_b64(uint2v{word[0], word[1]}, to, at, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4) __builtin_amdgcn_raw_buffer_store_b128(uint4v{word[i], word[i + 1], word[i + 2], word[i + 3]}, to, at + 4 * i, 0, 0);
+    }
+}
 template <bool kF32, int kCount>
 __device__ __forceinline__ void store(char* p, const float (&v)[kCount]) {
     if constexpr (kF32) {
@@ -79,6 +127,16 @@ __device__ __forceinline__ float softplus_of(float v) {
 }
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
 __device__ __forceinline__ float step_of(float v, bool softplus) { return softplus ? softplus_of(v) : v; }
+
+template <bool kF32, int kCount>
+__device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const float (&bias)[kCount], bool softplus, float (&dt)[kCount]) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) dt[i] = delta[i] + bias[i];
+    if (softplus) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) dt[i] = softplus_of(dt[i]);
+    }
+}
 
 // A workgroup's rows: tokens of sequence b from the segment's first on; first_row is that token's row.
 struct Span {
@@ -114,25 +172,54 @@ __device__ __forceinline__ void each(F f) {
     each_of(f, std::make_integer_sequence<int, kCount>());
 }
 
-// b or c of a chunk, as operands of outer products (4 x 4 x 1 matrix instructions of sixteen blocks, of whose first operand one block is
-// taken for all): a block of four lanes belongs to a token.  plain: its four states.  at_token(n): state n in the lane that has the token's
-// number modulo four, nothing in the others, so that the product lands in that row of the result and four tokens share one.
-template <bool kF32>
-struct StateRow {
-    Raw<kF32, 4> raw;
-    __device__ __forceinline__ void none() { raw.none(); }
-    __device__ __forceinline__ float plain(int lane) const {
-        const float low = lane & 1 ? raw[1] : raw[0], high = lane & 1 ? raw[3] : raw[2];
-        return lane & 2 ? high : low;
-    }
-    __device__ __forceinline__ float at_token(int n, int lane) const { return (lane & 3) == (lane >> 2 & 3) ? raw[n] : 0.f; }
-};
+// `left` rows of row_bytes, `first` rows behind base: what lies behind them is not read, and stores there are dropped.  All of it is the same in a
+// wave, so addresses cost no vector instruction.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* base, long long first, long long row_bytes, int left) {
+    return chunk_rsrc(static_cast<const char*>(base), first * row_bytes, (first + (left < 0 ? 0 : left)) * row_bytes);
+}
+constexpr int kNowhere = 0x7fffff00;   // an offset behind the end of any such rows
 
-// c + (rows of one block of a) x b: c[i] += a(lane 4 kBlock + i) b
+// c[0] h[0] + c[1] h[1] + c[2] h[2] + c[3] h[3] where c's values lie in lanes 4 kFirst .. 4 kFirst + 3 of every row of sixteen lanes: operands that
+// come from another lane cost nothing, but the compiler makes moves of them in front of a multiply-add.  A register that a vector
+// instruction has written may be read from other lanes two states later: the s_nop, here and not where the compiler could move it.
+template <int kFirst>
+__device__ __forceinline__ float read_out(float c, float4v h) {
+    float y;
+    asm("s_nop 1\n\t"
+        "v_mul_f32_dpp %0, %1, %2 row_newbcast:%c6 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%c7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%c8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%c9 row_mask:0xf bank_mask:0xf"
+        : "=&v"(y)
+        : "v"(c), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "n"(4 * kFirst), "n"(4 * kFirst + 1), "n"(4 * kFirst + 2), "n"(4 * kFirst + 3));
+    return y;
+}
+
+// c[i] + a(lane 4 kBlock + i) b for i < 4, of every lane's b and c: a 4 x 4 x 1 matrix instruction of sixteen blocks of four lanes, of whose first
+// operand one block is taken for all.
 template <int kBlock>
-__device__ __forceinline__ float4v outer(float a, float b, float4v c) {
+__device__ __forceinline__ float4v outer(float a, float b, float4v c = float4v{0.f, 0.f, 0.f, 0.f}) {
     return __builtin_amdgcn_mfma_f32_4x4x1f32(a, b, c, 4, kBlock, 0);
 }
+
+// A chunk's b or c for one wave's four states: in the order of outer(), and of read_out() by groups of four tokens.  Tokens behind `left`: zeros.
+template <bool kF32>
+struct Plain {
+    Raw<kF32, 1> raw;                  // state lane % 4 of token lane / 4
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rows, int lane, int row_bytes, int n0) {
+        raw.load(rows, lane / 4 * row_bytes + (n0 + lane % 4) * (kF32 ? 4 : 2));
+    }
+    __device__ __forceinline__ float value() const { return raw[0]; }
+};
+template <bool kF32, int kGroups>
+struct ByRow {
+    Raw<kF32, 1> raw[kGroups];         // [g]: state lane % 4 of token 4 g + lane / 4 % 4
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rows, int lane, int row_bytes, int n0) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) raw[g].load(rows, (4 * g + lane / 4 % 4) * row_bytes + (n0 + lane % 4) * (kF32 ? 4 : 2));
+    }
+    __device__ __forceinline__ float value(int g) const { return raw[g][0]; }
+};
 
 }  // namespace scan
 }  // namespace wkv6
