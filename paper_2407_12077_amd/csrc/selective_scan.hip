@@ -9,8 +9,8 @@ namespace {
 using namespace scan;
 
 // kStates: the segments' states from nothing, without read-outs.
-template <int N, bool kF32, bool kOutF32, bool kStates>
-__global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, float* state_out, int blocks) {
+template <int N, bool kF32, bool kOutF32, bool kStates, bool kGate>
+__global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs a, char* out, float* state_out, int blocks) {
     constexpr int kWaves = N / 4, kC = kScanChunk, kCh = kScanChannels, kItem = kF32 ? 4 : 2, kOutItem = kOutF32 ? 4 : 2;
     constexpr int kPer = kC / kWaves < 8 ? kC / kWaves : 8;    // channels that a thread brings and takes of a token
     constexpr int kAcross = kCh / kPer;
@@ -34,6 +34,7 @@ __global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, 
         rate = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0) * kLog2e;
         if (!kStates && a.segs > 1) {
             h = *reinterpret_cast<const float4v*>(a.locals + unit);
+#pragma unroll 4
             for (int q = 1; q <= seg; ++q) {
                 const float sum = a.locals[sums_at + q * seg_sums + static_cast<long long>(b) * D + ch];
                 const float4v local = *reinterpret_cast<const float4v*>(a.locals + q * seg_states + unit);
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, 
         k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
         k.b.load(rows_at(a.b, row, a.bc_row, left), lane, bc_row, n0);
         if constexpr (!kStates) {
-            if (a.z) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
+            if constexpr (kGate) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
             k.c.load(rows_at(a.c, row, a.bc_row, left), lane, bc_row, n0);
         }
     };
@@ -84,17 +85,28 @@ __global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, 
             step[buffer][token][in_block + i] = float2v{dt, dt * k.x[i]};
         }
     };
-    Chunk now, next;
+    auto leave = [&](int first, int left, const Chunk& k, int buffer) {
+        float y[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            y[i] = skip[i] * k.x[i];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) y[i] += part[buffer][w][token][in_block + i];
+            if constexpr (kGate) y[i] *= k.z[i] * sigmoid_of(k.z[i]);
+        }
+        store<kOutF32>(rows_at(out, span.first_row + first, static_cast<long long>(D) * kOutItem, left), out_at, y);
+    };
+    Chunk before = {}, now, next;
     ask(0, now);
     bring(0, now, 0);
-    __syncthreads();
-    int buffer = 0;
-    for (int first = 0; first < span.tokens; first += kC, buffer ^= 1) {
+    // Between two barriers: a chunk's read-outs, the states of the chunk behind it, and the step sizes of the one behind that; without a branch, so that they
+    // hide one another's latencies.
+    int buffer = 0, first = 0;
+    for (; first < span.tokens; first += kC, buffer ^= 1) {
+        __syncthreads();
         ask(first + kC, next);
+        if constexpr (!kStates) leave(first - kC, first > 0 ? kC : 0, before, buffer ^ 1);     // (nothing in the first turn)
         const float bv = now.b.value();
-        float cv[kC / 4];
-#pragma unroll
-        for (int g = 0; g < kC / 4; ++g) cv[g] = kStates ? 0.f : now.c.value(g);
         each<kC>([&](auto token_of_chunk) {
             constexpr int t = decltype(token_of_chunk)::value;
             const float2v d = step[buffer][t][lane];
@@ -102,26 +114,15 @@ __global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, 
             if constexpr (kStates) dt_sum += d.x;
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[i]), h[i], add[i]);
-            if constexpr (!kStates) part[buffer][wave][t][lane] = read_out<t % 4>(cv[t / 4], h);
+            if constexpr (!kStates) part[buffer][wave][t][lane] = read_out<t % 4>(now.c.value(t / 4), h);
         });
         bring(first + kC, next, buffer ^ 1);
-        __syncthreads();
-        if constexpr (!kStates) {
-            float y[kPer];
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                float v = skip[i] * now.x[i];
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) v += part[buffer][w][token][in_block + i];
-                y[i] = v;
-            }
-            if (a.z) {
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) y[i] *= now.z[i] * sigmoid_of(now.z[i]);
-            }
-            store<kOutF32>(rows_at(out, span.first_row + first, static_cast<long long>(D) * kOutItem, span.tokens - first), out_at, y);
-        }
+        before = now;
         now = next;
+    }
+    if (!kStates && span.tokens > 0) {
+        __syncthreads();
+        leave(first - kC, span.tokens - (first - kC), before, buffer ^ 1);
     }
     if (!mine) return;
     if constexpr (kStates) {
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(16 * N, 2) void scan_kernel(ScanArgs a, char* out, 
 template <int N, bool kF32>
 hipError_t launch_states(const ScanArgs& a, hipStream_t stream) {
     const int blocks = static_cast<int>(scan_blocks(a.D));
-    hipLaunchKernelGGL((scan_kernel<N, kF32, true, true>), dim3(static_cast<unsigned>(blocks) * a.B * (a.segs - 1)), dim3(scan_threads(N)), 0, stream, a,
+    hipLaunchKernelGGL((scan_kernel<N, kF32, true, true, false>), dim3(static_cast<unsigned>(blocks) * a.B * (a.segs - 1)), dim3(scan_threads(N)), 0, stream, a,
                        nullptr, nullptr, blocks);
     return hipGetLastError();
 }
@@ -146,7 +147,8 @@ hipError_t launch(const ScanArgs& a, void* out, float* state_out, hipStream_t st
         const hipError_t err = launch_states<N, kF32>(a, stream);
         if (err != hipSuccess) return err;
     }
-    hipLaunchKernelGGL((scan_kernel<N, kF32, kOutF32, false>), dim3(static_cast<unsigned>(blocks) * a.B * a.segs), dim3(scan_threads(N)), 0, stream, a,
+    const auto kernel = a.z ? &scan_kernel<N, kF32, kOutF32, false, true> : &scan_kernel<N, kF32, kOutF32, false, false>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks) * a.B * a.segs), dim3(scan_threads(N)), 0, stream, a,
                        static_cast<char*>(out), state_out, blocks);
     return hipGetLastError();
 }
@@ -165,12 +167,10 @@ hipError_t by_states(int N, F f) {
 }  // namespace
 
 ScanPlan plan_scan(int B, int T, int D, int N) {
-    const long long units = static_cast<long long>(B) * scan_blocks(D) * N / 16;
-    #ifndef TARGET
-#define TARGET 768
-#endif
-    long long segs = units > 0 ? TARGET / units : 1;
-    const long long most = (T + 127) / 128;
+    const long long workgroups = B * scan_blocks(D), units = workgroups * N / 16;
+    if (units == 0 || (units > 320 && workgroups >= 256)) return {1, T};
+    long long segs = 2048 / units;
+    const long long most = T > 1024 ? T / 64 : T > 512 ? 16 : (T + 31) / 32;
     if (segs > most) segs = most;
     if (segs > 64) segs = 64;
     if (segs < 2) return {1, T};

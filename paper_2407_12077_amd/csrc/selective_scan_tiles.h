@@ -131,10 +131,9 @@ __device__ __forceinline__ float step_of(float v, bool softplus) { return softpl
 template <bool kF32, int kCount>
 __device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const float (&bias)[kCount], bool softplus, float (&dt)[kCount]) {
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) dt[i] = delta[i] + bias[i];
-    if (softplus) {
-#pragma unroll
-        for (int i = 0; i < kCount; ++i) dt[i] = softplus_of(dt[i]);
+    for (int i = 0; i < kCount; ++i) {
+        const float v = delta[i] + bias[i], s = softplus_of(v);        // (no branch: what surrounds this is one block to the compiler)
+        dt[i] = softplus ? s : v;
     }
 }
 
