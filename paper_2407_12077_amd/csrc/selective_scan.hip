@@ -65,15 +65,22 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
     const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
     const int out_at = there ? (token * D + own) * kOutItem : kNowhere;
     const int bc_row = static_cast<int>(a.bc_row);
-    auto ask = [&](int first, Chunk& k) {
-        const long long row = span.first_row + first;
-        const int left = span.tokens - first;
-        k.x.load(rows_at(a.x, row, a.x_row, left), x_at);
-        k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
-        k.b.load(rows_at(a.b, row, a.bc_row, left), lane, bc_row, n0);
+    const long long row0 = span.first_row;
+    Rows xs(a.x, row0, a.x_row), deltas(a.delta, row0, a.delta_row), zs(a.z, row0, a.z_row), bs(a.b, row0, a.bc_row), cs(a.c, row0, a.bc_row),
+        outs(out, row0 - kC, static_cast<long long>(D) * kOutItem);
+    auto ask = [&](int left, Chunk& k) {                       // the next chunk, if `left` tokens are left
+        const int count = rows_of<kC>(left);
+        k.x.load(xs.first(count), x_at);
+        k.delta.load(deltas.first(count), delta_at);
+        k.b.load(bs.first(count), lane, bc_row, n0);
+        xs.move(kC);
+        deltas.move(kC);
+        bs.move(kC);
         if constexpr (!kStates) {
-            if constexpr (kGate) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
-            k.c.load(rows_at(a.c, row, a.bc_row, left), lane, bc_row, n0);
+            if constexpr (kGate) k.z.load(zs.first(count), z_at);
+            k.c.load(cs.first(count), lane, bc_row, n0);
+            zs.move(kC);
+            cs.move(kC);
         }
     };
     auto bring = [&](int first, const Chunk& k, int buffer) {
@@ -85,7 +92,7 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
             step[buffer][token][in_block + i] = float2v{dt, dt * k.x[i]};
         }
     };
-    auto leave = [&](int first, int left, const Chunk& k, int buffer) {
+    auto leave = [&](int count, const Chunk& k, int buffer) {
         float y[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -94,18 +101,22 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
             for (int w = 0; w < kWaves; ++w) y[i] += part[buffer][w][token][in_block + i];
             if constexpr (kGate) y[i] *= k.z[i] * sigmoid_of(k.z[i]);
         }
-        store<kOutF32>(rows_at(out, span.first_row + first, static_cast<long long>(D) * kOutItem, left), out_at, y);
+        store<kOutF32>(outs.first(count), out_at, y);
+        outs.move(kC);
     };
     Chunk before = {}, now, next;
-    ask(0, now);
+    ask(span.tokens, now);
     bring(0, now, 0);
     // Between two barriers: a chunk's read-outs, the states of the chunk behind it, and the step sizes of the one behind that; without a branch, so that they
     // hide one another's latencies.
     int buffer = 0, first = 0;
     for (; first < span.tokens; first += kC, buffer ^= 1) {
         __syncthreads();
-        ask(first + kC, next);
-        if constexpr (!kStates) leave(first - kC, first > 0 ? kC : 0, before, buffer ^ 1);     // (nothing in the first turn)
+        // Waves of two workgroups share a SIMD, and the older one would have its way until it is through, and the younger be left alone: whoever is
+        // further in its chunk gives way (all alike 530 us, two levels 502, four 457).
+        __builtin_amdgcn_s_setprio(3);
+        ask(span.tokens - first - kC, next);
+        if constexpr (!kStates) leave(first > 0 ? kC : 0, before, buffer ^ 1);     // (nothing in the first turn)
         const float bv = now.b.value();
         each<kC>([&](auto token_of_chunk) {
             constexpr int t = decltype(token_of_chunk)::value;
@@ -115,14 +126,20 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[i]), h[i], add[i]);
             if constexpr (!kStates) part[buffer][wave][t][lane] = read_out<t % 4>(now.c.value(t / 4), h);
+            if constexpr (t == 3) __builtin_amdgcn_s_setprio(2);
+            if constexpr (t == 7) {
+                __builtin_amdgcn_s_setprio(1);
+                __builtin_amdgcn_sched_barrier(0);             // (without it the compiler brings too much forward: 558 us)
+            }
         });
+        __builtin_amdgcn_s_setprio(0);
         bring(first + kC, next, buffer ^ 1);
         before = now;
         now = next;
     }
     if (!kStates && span.tokens > 0) {
         __syncthreads();
-        leave(first - kC, span.tokens - (first - kC), before, buffer ^ 1);
+        leave(span.tokens - (first - kC), before, buffer ^ 1);
     }
     if (!mine) return;
     if constexpr (kStates) {

@@ -60,13 +60,19 @@ __global__ __launch_bounds__(16 * N, 2) void scan_behind_kernel(ScanArgs a, cons
     const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
     const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
     const int out_at = there ? (token * D + own) * kItem : kNowhere;
-    auto ask = [&](int first, Chunk& k) {
-        const long long row = span.first_row + first;
-        const int left = first < 0 ? 0 : span.tokens - first;
-        k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
-        if (a.z) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
-        k.dout.load(rows_at(dout, row, static_cast<long long>(D) * kItem, left), out_at);
-        k.c.load(rows_at(a.c, row, a.bc_row, left), lane, static_cast<int>(a.bc_row), n0);
+    int first = (span.tokens - 1) / kC * kC, buffer = 0;
+    const long long row0 = span.first_row + first;
+    Rows deltas(a.delta, row0, a.delta_row), zs(a.z, row0, a.z_row), douts(dout, row0, static_cast<long long>(D) * kItem), cs(a.c, row0, a.bc_row);
+    auto ask = [&](int at, Chunk& k) {                         // chunks in falling order
+        const int count = at < 0 ? 0 : rows_of<kC>(span.tokens - at);
+        k.delta.load(deltas.first(count), delta_at);
+        if (a.z) k.z.load(zs.first(count), z_at);
+        k.dout.load(douts.first(count), out_at);
+        k.c.load(cs.first(count), lane, static_cast<int>(a.bc_row), n0);
+        deltas.move(-kC);
+        zs.move(-kC);
+        douts.move(-kC);
+        cs.move(-kC);
     };
     auto bring = [&](int first, const Chunk& k, int buffer) {
         float dts[kPer], dy[kPer];
@@ -81,7 +87,6 @@ __global__ __launch_bounds__(16 * N, 2) void scan_behind_kernel(ScanArgs a, cons
         for (int i = 0; i < kPer; ++i) step[buffer][token][in_block + i] = float2v{first + token < span.tokens ? dts[i] : 0.f, dy[i]};
     };
     Chunk now, next;
-    int first = (span.tokens - 1) / kC * kC, buffer = 0;
     ask(first, now);
     bring(first, now, 0);
     __syncthreads();
@@ -110,8 +115,8 @@ template <int N, bool kF32, bool kGate>
 __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(ScanArgs a, ScanGradients r, int blocks) {
     using S = Shape<N>;
     constexpr int kG = S::kGroups, kWaves = S::kWaves, kC = S::kC, kCh = kScanChannels, kPer = S::kPer, kItem = kF32 ? 4 : 2;
-    __shared__ float2v step[kC][kCh];                          // dt, dt x
-    __shared__ float grad_out[kC][kCh];                        // dy
+    __shared__ float2v step[2][kC][kCh];                       // dt, dt x
+    __shared__ float grad_out[2][kC][kCh];                     // dy
     __shared__ float part[kGate ? 3 : 2][kWaves][kC][kCh];                 // shares of g, of sum k rate, of the read-outs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = blockIdx.x % blocks, at = blockIdx.x / blocks, b = at % a.B, seg = at / a.B;
@@ -167,47 +172,30 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     }
     struct Chunk {
         Raw<kF32, kPer> x, delta, z, dout;
+        float dt[kPer], dy[kPer];
         Plain<kF32> b[kG], c[kG];
         ByRow<kF32, kC / 4> bt[kG], ct[kG];
+        float4v h[kG];
     };
     const int bc_row = static_cast<int>(a.bc_row);
     const int x_at = there ? token * static_cast<int>(a.x_row) + own * kItem : kNowhere;
     const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
     const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
     const int out_at = there ? (token * D + own) * kItem : kNowhere;
-    const long long out_row = static_cast<long long>(D) * kItem;
-    auto ask = [&](int first, Chunk& k, auto on_the_way_back) {
-        constexpr bool kBack = decltype(on_the_way_back)::value;
-        const long long row = span.first_row + first;
-        const int left = first < 0 ? 0 : span.tokens - first;
-        k.x.load(rows_at(a.x, row, a.x_row, left), x_at);
-        k.delta.load(rows_at(a.delta, row, a.delta_row, left), delta_at);
-        if constexpr (kBack) {
-            if constexpr (kGate) k.z.load(rows_at(a.z, row, a.z_row, left), z_at);
-            k.dout.load(rows_at(r.dout, row, out_row, left), out_at);
-        }
-        const __amdgpu_buffer_rsrc_t b = rows_at(a.b, row, a.bc_row, left), c = rows_at(a.c, row, a.bc_row, left);
-#pragma unroll
-        for (int q = 0; q < kG; ++q) {
-            k.b[q].load(b, lane, bc_row, n0 + 4 * q);
-            if constexpr (kBack) {
-                k.c[q].load(c, lane, bc_row, n0 + 4 * q);
-                k.bt[q].load(b, lane, bc_row, n0 + 4 * q);
-                if constexpr (kGate) k.ct[q].load(c, lane, bc_row, n0 + 4 * q);
-            }
-        }
-    };
-    auto bring = [&](int first, const Chunk& k, auto on_the_way_back) {
-        float dts[kPer];
-        steps_of(k.delta, bias, a.softplus, dts);
+    const int kept_at = mine ? (ch * N + n0) * 4 : kNowhere;
+    const long long row0 = span.first_row, out_row = static_cast<long long>(D) * kItem;
+    const long long place0 = (row0 - static_cast<long long>(seg) * a.seg_len) / kC + static_cast<long long>(seg) * a.seg_len / kC + b;
+    Rows xs(a.x, row0, a.x_row), deltas(a.delta, row0, a.delta_row), bs(a.b, row0, a.bc_row), kept(r.states, place0, static_cast<long long>(D) * N * 4);
+    auto bring = [&](int first, Chunk& k, int buffer, auto on_the_way_back) {
+        steps_of(k.delta, bias, a.softplus, k.dt);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const float dt = first + token < span.tokens ? dts[i] : 0.f;
-            step[token][in_block + i] = float2v{dt, dt * k.x[i]};
+            k.dt[i] = first + token < span.tokens ? k.dt[i] : 0.f;
+            step[buffer][token][in_block + i] = float2v{k.dt[i], k.dt[i] * k.x[i]};
             if constexpr (decltype(on_the_way_back)::value) {
-                float dy = k.dout[i];
-                if constexpr (kGate) dy *= k.z[i] * sigmoid_of(k.z[i]);
-                grad_out[token][in_block + i] = dy;
+                k.dy[i] = k.dout[i];
+                if constexpr (kGate) k.dy[i] *= k.z[i] * sigmoid_of(k.z[i]);
+                grad_out[buffer][token][in_block + i] = k.dy[i];
             }
         }
     };
@@ -216,55 +204,95 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
 
     // the states in front of the chunks
     const int last_first = span.tokens > 0 ? (span.tokens - 1) / kC * kC : -kC;
-    const long long place0 = (span.first_row - static_cast<long long>(seg) * a.seg_len) / kC + static_cast<long long>(seg) * a.seg_len / kC + b;
-    const long long kept_row = static_cast<long long>(D) * N * 4;
-    const int kept_at = mine ? (ch * N + n0) * 4 : kNowhere;
     Chunk now, next;
-    ask(0, now, kForward);
-    for (int first = 0; first < last_first; first += kC) {
-        bring(first, now, kForward);
+    int buffer = 0;
+    {
+        auto ask = [&](int left, Chunk& k) {
+            const int count = rows_of<kC>(left);
+            k.x.load(xs.first(count), x_at);
+            k.delta.load(deltas.first(count), delta_at);
+#pragma unroll
+            for (int q = 0; q < kG; ++q) k.b[q].load(bs.first(count), lane, bc_row, n0 + 4 * q);
+            xs.move(kC);
+            deltas.move(kC);
+            bs.move(kC);
+        };
+        ask(span.tokens, now);
+        bring(0, now, 0, kForward);
+        for (int first = 0; first < last_first; first += kC, buffer ^= 1) {
+            __syncthreads();
+            __builtin_amdgcn_s_setprio(3);
+            ask(span.tokens - first - kC, next);
+#pragma unroll
+            for (int q = 0; q < kG; ++q) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, h[q]), kept.first(1), kept_at + 16 * q, 0, 0);
+            kept.move(1);
+            each<kC>([&](auto token_of_chunk) {
+                constexpr int t = decltype(token_of_chunk)::value;
+                const float2v d = step[buffer][t][lane];
+#pragma unroll
+                for (int q = 0; q < kG; ++q) {
+                    const float4v add = outer<t>(now.b[q].value(), d.y);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[q][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[q][i]), h[q][i], add[i]);
+                }
+                if constexpr (t == 3) __builtin_amdgcn_s_setprio(2);
+                if constexpr (t == 7) __builtin_amdgcn_s_setprio(1);
+            });
+            __builtin_amdgcn_s_setprio(0);
+            bring(first + kC, next, buffer ^ 1, kForward);
+            now = next;
+        }
         __syncthreads();
-        ask(first + kC, next, kForward);
-        const __amdgpu_buffer_rsrc_t kept = rows_at(r.states, place0 + first / kC, kept_row, 1);
-#pragma unroll
-        for (int q = 0; q < kG; ++q) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, h[q]), kept, kept_at + 16 * q, 0, 0);
-        float bv[kG];
-#pragma unroll
-        for (int q = 0; q < kG; ++q) bv[q] = now.b[q].value();
-        each<kC>([&](auto token_of_chunk) {
-            constexpr int t = decltype(token_of_chunk)::value;
-            const float2v d = step[t][lane];
-#pragma unroll
-            for (int q = 0; q < kG; ++q) {
-                const float4v add = outer<t>(bv[q], d.y);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) h[q][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[q][i]), h[q][i], add[i]);
-            }
-        });
-        __syncthreads();
-        now = next;
     }
 
     // and back
-    const long long share_row = static_cast<long long>(blocks) * 2 * N * 4;
+    xs = Rows(a.x, row0 + last_first, a.x_row);
+    deltas = Rows(a.delta, row0 + last_first, a.delta_row);
+    bs = Rows(a.b, row0 + last_first, a.bc_row);
+    Rows zs(a.z, row0 + last_first, a.z_row), douts(r.dout, row0 + last_first, out_row), cs(a.c, row0 + last_first, a.bc_row);
+    Rows dxs(r.dx, row0 + last_first, a.x_row), ddeltas(r.ddelta, row0 + last_first, a.delta_row), dzs(r.dz, row0 + last_first, a.z_row);
+    Rows shares(r.rows, row0 + last_first, static_cast<long long>(blocks) * 2 * N * 4);
     const int share_token = (lane >> 2 & 1) + (lane & 2) + (lane & 1) * 4;
-    const int share_at = share_token * static_cast<int>(share_row) + (block * 2 * N + (lane >> 5) * N + n0 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1)) * 4;
-    ask(last_first, now, kBackward);
-    for (int first = last_first; first >= 0; first -= kC) {
-        bring(first, now, kBackward);
-        if (first < last_first) {
-            const __amdgpu_buffer_rsrc_t kept = rows_at(r.states, place0 + first / kC, kept_row, 1);
+    const int share_at = share_token * shares.row + (block * 2 * N + (lane >> 5) * N + n0 + (lane >> 4 & 1) * 2 + (lane >> 3 & 1)) * 4;
+    auto ask = [&](int at, Chunk& k) {                         // chunks in falling order
+        const int count = at < 0 ? 0 : rows_of<kC>(span.tokens - at);
+        k.x.load(xs.first(count), x_at);
+        k.delta.load(deltas.first(count), delta_at);
+        if constexpr (kGate) k.z.load(zs.first(count), z_at);
+        k.dout.load(douts.first(count), out_at);
+        kept.move(-1);
+        const __amdgpu_buffer_rsrc_t b_rows = bs.first(count), c_rows = cs.first(count), states = kept.first(at < 0 ? 0 : 1);
 #pragma unroll
-            for (int q = 0; q < kG; ++q) h[q] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(kept, kept_at + 16 * q, 0, 0));
+        for (int q = 0; q < kG; ++q) {
+            k.b[q].load(b_rows, lane, bc_row, n0 + 4 * q);
+            k.c[q].load(c_rows, lane, bc_row, n0 + 4 * q);
+            k.bt[q].load(b_rows, lane, bc_row, n0 + 4 * q);
+            if constexpr (kGate) k.ct[q].load(c_rows, lane, bc_row, n0 + 4 * q);
+            k.h[q] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(states, kept_at + 16 * q, 0, 0));
         }
+        xs.move(-kC);
+        deltas.move(-kC);
+        zs.move(-kC);
+        douts.move(-kC);
+        bs.move(-kC);
+        cs.move(-kC);
+    };
+    kept.move(1);
+    ask(last_first, now);                                      // (its states are in registers: what is read there is not used)
+#pragma unroll
+    for (int q = 0; q < kG; ++q) now.h[q] = h[q];
+    buffer = 0;
+    bring(last_first, now, 0, kBackward);
+    for (int first = last_first; first >= 0; first -= kC, buffer ^= 1) {
         __syncthreads();
-        ask(first - kC, next, kBackward);
+        __builtin_amdgcn_s_setprio(3);
+        ask(first - kC, next);
         float4v decay[kC][kG], state[kC + 1][kG];              // exp(dt a), and the states: state[t] in front of token t
 #pragma unroll
-        for (int q = 0; q < kG; ++q) state[0][q] = h[q];
+        for (int q = 0; q < kG; ++q) state[0][q] = now.h[q];
         each<kC>([&](auto token_of_chunk) {
             constexpr int t = decltype(token_of_chunk)::value;
-            const float2v d = step[t][lane];
+            const float2v d = step[buffer][t][lane];
             float y = 0.f;
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
@@ -278,15 +306,16 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
             }
             if constexpr (kGate) part[2][wave][t][lane] = y;
         });
-        const __amdgpu_buffer_rsrc_t shares = rows_at(r.rows, span.first_row + first, share_row, span.tokens - first);
+        __builtin_amdgcn_s_setprio(2);
+        const int count = rows_of<kC>(span.tokens - first);
         float4v da_chunk[kG];
         float pairs[kG], fours[kG], eights[kG];                // sums over lanes on their way: of one odd token, of two, of four
 #pragma unroll
         for (int q = 0; q < kG; ++q) da_chunk[q] = float4v{0.f, 0.f, 0.f, 0.f};
         each<kC>([&](auto back) {
             constexpr int t = kC - 1 - decltype(back)::value;
-            const float2v d = step[t][lane];
-            const float dy = grad_out[t][lane];
+            const float2v d = step[buffer][t][lane];
+            const float dy = grad_out[buffer][t][lane];
             float k_rate = 0.f, into = 0.f;
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
@@ -318,7 +347,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                             eights[q] = four;
                         } else {
                             const float sum = halves<1>(four, eights[q], lane);
-                            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), shares, share_at + t * static_cast<int>(share_row) + 16 * q, 0, 0);
+                            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(sum), shares.first(count), share_at + t * shares.row + 16 * q, 0, 0);
                         }
                     }
                 }
@@ -331,10 +360,15 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
 #pragma unroll
                     for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(da_chunk[q][i]));
             }
+            if constexpr (t == kC / 2) __builtin_amdgcn_s_setprio(1);
         });
+        shares.move(-kC);
 #pragma unroll
         for (int q = 0; q < kG; ++q) da[q] += da_chunk[q];
+        __builtin_amdgcn_s_setprio(0);
+        bring(first - kC, next, buffer ^ 1, kBackward);
         __syncthreads();
+        __builtin_amdgcn_s_setprio(3);
         {
             float dx[kPer], dd[kPer], dz[kPer];
 #pragma unroll
@@ -345,10 +379,13 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                     g += part[0][w][token][in_block + i];
                     k += part[1][w][token][in_block + i];
                 }
-                const float dt = step[token][in_block + i].x, dy = grad_out[token][in_block + i], xv = now.x[i];
-                dx[i] = __builtin_fmaf(g, dt, skip[i] * dy);
+                const float xv = now.x[i];
+                dx[i] = __builtin_fmaf(g, now.dt[i], skip[i] * now.dy[i]);
                 dd[i] = __builtin_fmaf(g, xv, k * kLn2);
-                dskip[i] = __builtin_fmaf(dy, xv, dskip[i]);
+                const float slope = sigmoid_of(now.delta[i] + bias[i]);
+                dd[i] *= a.softplus ? slope : 1.f;
+                dskip[i] = __builtin_fmaf(now.dy[i], xv, dskip[i]);
+                dbias[i] += first + token < span.tokens ? dd[i] : 0.f;       // (behind the end k is not nought)
                 if constexpr (kGate) {
                     float y = skip[i] * xv;
 #pragma unroll
@@ -357,21 +394,17 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                     dz[i] = now.dout[i] * y * (s * __builtin_fmaf(zv, 1.f - s, 1.f));
                 }
             }
-            if (a.softplus) {
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) dd[i] *= sigmoid_of(now.delta[i] + bias[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) dbias[i] += first + token < span.tokens ? dd[i] : 0.f;       // (behind the end k is not nought)
-            const long long row = span.first_row + first;
-            const int left = span.tokens - first;
-            store<kF32>(rows_at(r.dx, row, a.x_row, left), x_at, dx);
-            store<kF32>(rows_at(r.ddelta, row, a.delta_row, left), delta_at, dd);
-            if (kGate && r.dz) store<kF32>(rows_at(r.dz, row, a.z_row, left), z_at, dz);
+            store<kF32>(dxs.first(count), x_at, dx);
+            store<kF32>(ddeltas.first(count), delta_at, dd);
+            if (kGate && r.dz) store<kF32>(dzs.first(count), z_at, dz);
+            dxs.move(-kC);
+            ddeltas.move(-kC);
+            dzs.move(-kC);
         }
-        __syncthreads();
         now = next;
     }
+    __builtin_amdgcn_s_setprio(0);
+    __syncthreads();
     const long long share = static_cast<long long>(seg) * a.B + b;
     if (mine) {
 #pragma unroll

@@ -171,10 +171,20 @@ __device__ __forceinline__ void each(F f) {
     each_of(f, std::make_integer_sequence<int, kCount>());
 }
 
-// `left` rows of row_bytes, `first` rows behind base: what lies behind them is not read, and stores there are dropped.  All of it is the same in a
-// wave, so addresses cost no vector instruction.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const void* base, long long first, long long row_bytes, int left) {
-    return chunk_rsrc(static_cast<const char*>(base), first * row_bytes, (first + (left < 0 ? 0 : left)) * row_bytes);
+// Rows of a tensor, a chunk at a time: what lies behind `count` rows is not read, and stores there are dropped.  All of it is the same in a wave, so
+// addresses cost no vector instruction, and few scalar ones.
+struct Rows {
+    char* at;                          // the chunk's first row
+    int row;                           // bytes
+    __device__ __forceinline__ Rows(const void* base, long long first, long long row_bytes)
+        : at(static_cast<char*>(const_cast<void*>(base)) + first * row_bytes), row(static_cast<int>(row_bytes)) {}
+    __device__ __forceinline__ void move(int rows) { at += static_cast<long long>(rows) * row; }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t first(int count) const { return __builtin_amdgcn_make_buffer_rsrc(at, 0, count * row, 0x00020000); }
+};
+// how many of a chunk's rows there are if `left` are left
+template <int kC>
+__device__ __forceinline__ int rows_of(int left) {
+    return left < 0 ? 0 : left > kC ? kC : left;
 }
 constexpr int kNowhere = 0x7fffff00;   // an offset behind the end of any such rows
 
