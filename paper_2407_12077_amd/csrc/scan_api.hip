@@ -99,21 +99,39 @@ struct ScanSpace {
     wkv6::ScanPlan plan;
     long long locals = 0, states = 0, rows = 0, weights = 0, floats = 0;
 };
-bool scan_space(int B, int T, int D, int N, long long rows, bool backward, ScanSpace* s) {
-    s->plan = wkv6::plan_scan(B, T, D, N);
+bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, bool backward, ScanSpace* s) {
+    s->plan = plan;
     const long long blocks = wkv6::scan_blocks(D);
-    if (!wkv6::fits_a_launch(B * blocks * s->plan.segs, wkv6::scan_threads(N))) return false;
-    s->locals = four(wkv6::scan_local_floats(s->plan, B, D, N));
+    if (!wkv6::fits_a_launch(B * blocks * plan.segs, wkv6::scan_threads(N))) return false;
+    s->locals = four(wkv6::scan_local_floats(plan, B, D, N));
     s->floats = s->locals;
     if (backward) {
-        if (!wkv6::fits_a_launch(rows * 2 * N + 256, 1)) return false;
-        const long long chunk = wkv6::scan_back_chunk(N);
-        s->states = (rows / chunk + B + 1) * D * N;
+        if (!wkv6::fits_a_launch((rows + 3) / 4, 256)) return false;
+        s->states = (rows / wkv6::scan_back_chunk(N) + B + 1) * D * N;
         s->rows = rows * blocks * 2 * N;
-        s->weights = static_cast<long long>(s->plan.segs) * B * D * (N + 2);
+        s->weights = static_cast<long long>(plan.segs) * B * D * (N + 2);
         s->floats = 2 * s->locals + s->states + s->rows + s->weights;
     }
     return true;
+}
+bool scan_space(int B, int T, int D, int N, long long rows, bool packed, bool backward, ScanSpace* s) {
+    return space_of(wkv6::plan_scan(B, T, D, N, packed ? rows : -1, backward), B, D, N, rows, backward, s);
+}
+// For calls with offsets or, if there are B T rows, without.  A prefill's rows are not known: for any that fit.
+long long scan_bytes(int B, int T, int D, int N, long long rows, bool backward) {
+    ScanSpace s;
+    long long most = 0;
+    if (!backward || rows == static_cast<long long>(B) * T) {
+        if (!scan_space(B, T, D, N, rows, false, backward, &s)) return -1;
+        most = s.floats;
+    }
+    if (backward) {
+        if (!scan_space(B, T, D, N, rows, true, true, &s)) return -1;
+    } else {
+        const int segs = wkv6::scan_most_segments(B, T, D, true);
+        if (!space_of({segs, 0}, B, D, N, 0, false, &s)) return -1;
+    }
+    return 4 * (s.floats > most ? s.floats : most);
 }
 
 // ---------------------------------------------------------------------------------------------- convolution
@@ -162,14 +180,12 @@ extern "C" {
 
 long long wkv6_selective_scan_workspace_bytes(int B, int T, int D, int N) {
     if (!states_fit(N) || !channels_fit(D) || !sizes_fit(B, T, D, 0)) return -1;
-    ScanSpace s;
-    return B == 0 ? 0 : scan_space(B, T, D, N, 0, false, &s) ? 4 * s.floats : -1;
+    return B == 0 ? 0 : scan_bytes(B, T, D, N, 0, false);
 }
 
 long long wkv6_selective_scan_backward_workspace_bytes(int B, int T, int D, int N, long long rows) {
     if (!states_fit(N) || !channels_fit(D) || !sizes_fit(B, T, D, rows)) return -1;
-    ScanSpace s;
-    return B == 0 ? 0 : scan_space(B, T, D, N, rows, true, &s) ? 4 * s.floats : -1;
+    return B == 0 ? 0 : scan_bytes(B, T, D, N, rows, true);
 }
 
 int wkv6_selective_scan_prefill(int B, int T, int D, int N, long long rows, const void* x, long long x_stride, const void* delta,
@@ -185,7 +201,7 @@ int wkv6_selective_scan_prefill(int B, int T, int D, int N, long long rows, cons
     if (call.any_rows() && !out) return WKV6_ERR_NULL;
     if (any_misaligned(out) || any_misaligned(state_out)) return WKV6_ERR_ALIGN;
     ScanSpace s;
-    if (!scan_space(B, T, D, N, rows, false, &s)) return WKV6_ERR_SHAPE;
+    if (!scan_space(B, T, D, N, rows, offsets != nullptr, false, &s)) return WKV6_ERR_SHAPE;
     if ((status = check_workspace(workspace, workspace_bytes, 4 * s.floats)) != WKV6_OK) return status;
     wkv6::ScanArgs args = call.args(s.plan);
     args.locals = static_cast<float*>(workspace);
@@ -230,7 +246,7 @@ int wkv6_selective_scan_backward(int B, int T, int D, int N, long long rows, con
                        static_cast<const void*>(dz)) || any_misaligned(dstate_out, static_cast<const float*>(dstate_in)))
         return WKV6_ERR_ALIGN;
     ScanSpace s;
-    if (!scan_space(B, T, D, N, rows, true, &s)) return WKV6_ERR_SHAPE;
+    if (!scan_space(B, T, D, N, rows, offsets != nullptr, true, &s)) return WKV6_ERR_SHAPE;
     if ((status = check_workspace(workspace, workspace_bytes, 4 * s.floats)) != WKV6_OK) return status;
     wkv6::ScanArgs args = call.args(s.plan);
     float* at = static_cast<float*>(workspace);

@@ -24,11 +24,19 @@ struct ScanArgs {
     float* locals;
 };
 
-// segs segments of seg_len tokens, a multiple of kScanChunk.
+// segs segments of seg_len tokens, a multiple of kScanChunk.  packed_rows: of a call with offsets, else -1.
+//
+// By what a call is modelled to take, in microseconds: a chunk takes a workgroup `alone` if it has a compute unit to itself, and `share` of
+// a unit that is full; the pieces' own states cost three quarters of the walk itself (of gradients, both ways, two fifths), and every piece adds
+// up what the pieces in front of it leave.  Measured, whole and cut: 4 x 4096 x 4096 430 and 394 us, 5 x 4096 x 4096 456 and 498, 8 x 4096 x 4096 459 and 776,
+// 1 x 512 x 1024 33 and 13.4; gradients of 4 x 2048 x 4096 757 and 703, 8 x 2048 x 4096 937 and 1350.
 struct ScanPlan {
     int segs, seg_len;
 };
-ScanPlan plan_scan(int B, int T, int D, int N);
+constexpr int kScanMostSegments = 64;
+constexpr int kScanPackedSegments = 8; // of a packed call with a workgroup for every compute unit: its locals are as many times the states
+int scan_most_segments(int B, int T, int D, bool packed);
+ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward);
 inline long long scan_blocks(int D) { return (D + kScanChannels - 1) / kScanChannels; }
 inline long long scan_local_floats(const ScanPlan& p, long long B, long long D, int N) { return p.segs > 1 ? p.segs * B * D * (N + 1) : 0; }
 constexpr int scan_threads(int N) { return 16 * N; }

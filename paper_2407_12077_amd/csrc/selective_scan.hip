@@ -3,6 +3,9 @@
 //     dt_t = softplus(delta_t + bias)    h_t[n] = exp(dt_t a[n]) h_{t-1}[n] + dt_t b_t[n] x_t    out_t = (sum_n c_t[n] h_t[n] + skip x_t) silu(z_t)
 #include "selective_scan_tiles.h"
 
+#include <algorithm>
+#include <cmath>
+
 namespace wkv6 {
 namespace {
 
@@ -183,17 +186,40 @@ hipError_t by_states(int N, F f) {
 
 }  // namespace
 
-ScanPlan plan_scan(int B, int T, int D, int N) {
-    const long long workgroups = B * scan_blocks(D), units = workgroups * N / 16;
-    if (units == 0 || (units > 320 && workgroups >= 256)) return {1, T};
-    long long segs = 2048 / units;
-    const long long most = T > 1024 ? T / 64 : T > 512 ? 16 : (T + 31) / 32;
-    if (segs > most) segs = most;
-    if (segs > 64) segs = 64;
-    if (segs < 2) return {1, T};
-    long long len = (T + segs - 1) / segs;
-    len = (len + kScanChunk - 1) / kScanChunk * kScanChunk;
-    return {static_cast<int>((T + len - 1) / len), static_cast<int>(len)};
+int scan_most_segments(int B, int T, int D, bool packed) {
+    const int most = packed && B * scan_blocks(D) >= compute_units() ? kScanPackedSegments : kScanMostSegments;
+    const int pairs = (T + kScanChunk - 1) / kScanChunk / 2;
+    return pairs < 2 ? 1 : pairs < most ? pairs : most;
+}
+
+ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward) {
+    const double chunks = (T + kScanChunk - 1) / kScanChunk, workgroups = static_cast<double>(B) * scan_blocks(D), units = compute_units();
+    if (workgroups < 1) return {1, T};
+    // microseconds of a chunk, and workgroups that a compute unit holds; N = 8, 16, 32, 64
+    static constexpr double kAlone[2][4] = {{1.7, 1.46, 1.87, 2.9}, {6.9, 5.5, 7.5, 15.4}}, kShare[2][4] = {{0.9, 0.85, 1.47, 2.9}, {3.2, 3.6, 7.4, 15.2}};
+    static constexpr int kHeld[2][4] = {{5, 3, 2, 1}, {4, 2, 1, 1}};
+    const int which = N == 8 ? 0 : N == 16 ? 1 : N == 32 ? 2 : 3, held = kHeld[backward][which];
+    const double alone = kAlone[backward][which], share = kShare[backward][which];
+    const double packed_work = (static_cast<double>(packed_rows) / kScanChunk + 0.5 * B) * scan_blocks(D) * share / units;
+    // one walk over pieces of `len` chunks: rounds of as many workgroups as there is room for, and a last one
+    auto walk = [&](double segs, double len) {
+        const double count = workgroups * segs;
+        if (packed_rows >= 0) return std::max(len * alone, packed_work * (1 + 0.55 * units / count));
+        const double rounds = std::floor(count / (units * held)), rest = count - rounds * units * held;
+        return rounds * len * std::max(alone, share * held) + (rest > 0 ? len * std::max(alone, share * std::ceil(rest / units)) : 0);
+    };
+    double best = walk(1, chunks);
+    ScanPlan plan{1, T};
+    const int most = scan_most_segments(B, T, D, packed_rows >= 0);
+    for (int segs = 2; segs <= most; ++segs) {
+        const double len = std::ceil(chunks / segs), work = packed_rows >= 0 ? packed_work : workgroups * segs * len * share / units;
+        const double time = walk(std::ceil(chunks / len), len) + (backward ? 0.4 : 0.75) * std::max(len * alone, work) + (backward ? 8 : 2) + 0.3 * segs;
+        if (time >= best) continue;
+        best = time;
+        plan.seg_len = static_cast<int>(len) * kScanChunk;
+        plan.segs = (T - 1) / plan.seg_len + 1;
+    }
+    return plan;
 }
 
 hipError_t launch_scan(const ScanArgs& a, void* out, float* state_out, bool f32_rows, bool f32_out, hipStream_t stream) {

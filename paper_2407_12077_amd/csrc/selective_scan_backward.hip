@@ -365,7 +365,6 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
         shares.move(-kC);
 #pragma unroll
         for (int q = 0; q < kG; ++q) da[q] += da_chunk[q];
-        __builtin_amdgcn_s_setprio(0);
         bring(first - kC, next, buffer ^ 1, kBackward);
         __syncthreads();
         __builtin_amdgcn_s_setprio(3);
@@ -429,16 +428,17 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     }
 }
 
-// db and dc of a row: the blocks' shares, in their order.
-template <bool kF32>
-__global__ __launch_bounds__(256) void scan_rows_kernel(ScanArgs a, const float* shares, char* db, char* dc, int blocks, int per) {
-    const int N2 = 2 * a.N, value = threadIdx.x % N2;
-    const long long row = static_cast<long long>(blockIdx.x) * per + threadIdx.x / N2;
+// db and dc of a row: a wave adds the blocks' shares, lanes four values of a block each, as many blocks at once as it has lanes for.
+template <int N, bool kF32>
+__global__ __launch_bounds__(256) void scan_rows_kernel(ScanArgs a, const float* shares, char* db, char* dc, int blocks) {
+    constexpr int kAcross = 2 * N / 4, kAtOnce = 64 / kAcross;
+    const int lane = threadIdx.x & 63;
+    const long long row = static_cast<long long>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= a.rows) return;
     if (a.offsets) {                                           // rows of nobody keep what they hold
-        long long lo = 0, hi = a.B;                            // the last sequence that starts at or in front of the row
+        int lo = 0, hi = a.B;                                  // the sequences that start at or in front of the row
         while (lo < hi) {
-            const long long mid = (lo + hi) / 2;
+            const int mid = lo + (hi - lo) / 2;
             if (a.offsets[mid] <= row) lo = mid + 1;
             else hi = mid;
         }
@@ -446,32 +446,47 @@ __global__ __launch_bounds__(256) void scan_rows_kernel(ScanArgs a, const float*
         const long long first = a.offsets[lo - 1] < 0 ? 0 : a.offsets[lo - 1];
         if (row >= a.offsets[lo] || row - first >= a.T) return;
     }
-    const float* p = shares + row * blocks * N2 + value;
-    float sum = 0.f;
-    for (int i = 0; i < blocks; ++i) sum += p[static_cast<long long>(i) * N2];
-    const int n = value % a.N;
-    const float v[1] = {sum};
-    store<kF32>((value < a.N ? db : dc) + row * a.bc_row + n * (kF32 ? 4 : 2), v);
+    const float4v* p = reinterpret_cast<const float4v*>(shares + row * blocks * (2 * N)) + lane;
+    float4v sum = {0.f, 0.f, 0.f, 0.f};
+    const int mine = lane / kAcross;
+#pragma unroll 8
+    for (int i = mine; i < blocks; i += kAtOnce, p += 64) sum += __builtin_nontemporal_load(p);
+#pragma unroll
+    for (int m = kAcross; m < 64; m *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m);
+    if (mine != 0) return;
+    const int value = 4 * (lane % kAcross);
+    const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    store<kF32>((value < N ? db : dc) + row * a.bc_row + value % N * (kF32 ? 4 : 2), v);
 }
 
-// da, dskip, dbias: the segments' shares in the order of sequences and segments.
-__global__ __launch_bounds__(256) void scan_weights_kernel(ScanArgs a, const float* shares, float* da, float* dskip, float* dbias) {
-    __shared__ float meet[4][64];
+// da, dskip, dbias: the segments' shares, sixteen turns of them, in the order of sequences and segments.
+constexpr int kTurns = 16;
+__global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(ScanArgs a, const float* shares, float* da, float* dskip, float* dbias) {
+    __shared__ float meet[kTurns][64];
     const int lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long states = static_cast<long long>(a.D) * a.N, value = static_cast<long long>(blockIdx.x) * 64 + lane;
     const bool there = value < states + 2 * a.D;
     const float* from = value < states ? shares + value : shares + a.segs * a.B * states + (value - states);
     const long long stride = value < states ? states : 2 * a.D;
     float sum = 0.f;
-    for (int b = turn; b < a.B; b += 4)
-        for (int s = 0; s < a.segs; ++s) {
-            if (s > 0 && span_of(a, b, s).tokens == 0) break;
-            if (there) sum += from[(static_cast<long long>(s) * a.B + b) * stride];
+    long long before = 0;                                      // segments of the sequences in front
+    for (int b = 0; b < a.B; ++b) {
+        int segs = 1;
+        if (a.segs > 1) {
+            const int tokens = tokens_of(a, b);
+            segs = tokens > 0 ? (tokens - 1) / a.seg_len + 1 : 1;
         }
+        for (int s = static_cast<int>((turn + kTurns - before % kTurns) % kTurns); s < segs; s += kTurns)
+            if (there) sum += from[(static_cast<long long>(s) * a.B + b) * stride];
+        before += segs;
+    }
     meet[turn][lane] = sum;
     __syncthreads();
     if (turn != 0 || !there) return;
-    sum = (meet[0][lane] + meet[1][lane]) + (meet[2][lane] + meet[3][lane]);
+#pragma unroll
+    for (int i = 1; i < kTurns; ++i) sum += meet[i][lane];
     if (value < states) {
         if (da) da[value] = sum;
     } else if (value < states + a.D) {
@@ -498,9 +513,8 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
                        stream, a, g, blocks);
     if ((err = hipGetLastError()) != hipSuccess) return err;
     if (a.rows > 0 && a.T > 0) {
-        const int per = 256 / (2 * N);
-        hipLaunchKernelGGL((scan_rows_kernel<kF32>), dim3(static_cast<unsigned>((a.rows + per - 1) / per)), dim3(256), 0, stream, a, g.rows,
-                           static_cast<char*>(g.db), static_cast<char*>(g.dc), blocks, per);
+        hipLaunchKernelGGL((scan_rows_kernel<N, kF32>), dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, stream, a, g.rows,
+                           static_cast<char*>(g.db), static_cast<char*>(g.dc), blocks);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     return launch_scan_weights(a, g, stream);
@@ -511,7 +525,7 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
 hipError_t launch_scan_weights(const ScanArgs& a, const ScanGradients& g, hipStream_t stream) {
     if (!g.da && !g.dskip && !g.dbias) return hipSuccess;
     const long long values = static_cast<long long>(a.D) * (a.N + 2);
-    hipLaunchKernelGGL(scan_weights_kernel, dim3(static_cast<unsigned>((values + 63) / 64)), dim3(256), 0, stream, a, g.weights, g.da, g.dskip, g.dbias);
+    hipLaunchKernelGGL(scan_weights_kernel, dim3(static_cast<unsigned>((values + 63) / 64)), dim3(64 * kTurns), 0, stream, a, g.weights, g.da, g.dskip, g.dbias);
     return hipGetLastError();
 }
 

@@ -137,25 +137,28 @@ __device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const f
     }
 }
 
-// A workgroup's rows: tokens of sequence b from the segment's first on; first_row is that token's row.
+// A sequence's first row, and its tokens.
+__device__ __forceinline__ long long first_row_of(const ScanArgs& a, int b) {
+    if (!a.offsets) return static_cast<long long>(b) * a.T;
+    const long long f = a.offsets[b];
+    return f < 0 ? 0 : f > a.rows ? a.rows : f;
+}
+__device__ __forceinline__ int tokens_of(const ScanArgs& a, int b) {
+    if (!a.offsets) return a.T;
+    const long long e = a.offsets[b + 1], len = (e < 0 ? 0 : e > a.rows ? a.rows : e) - first_row_of(a, b);
+    return static_cast<int>(len < 0 ? 0 : len > a.T ? a.T : len);
+}
+
+// A workgroup's rows: those of a segment of sequence b.
 struct Span {
     long long first_row;
     int tokens;                        // of this segment, 0: none
     bool last;                         // the sequence ends in it (or has no tokens, and this is the first segment)
 };
 __device__ __forceinline__ Span span_of(const ScanArgs& a, int b, int seg) {
-    long long lo = static_cast<long long>(b) * a.T, len = a.T;
-    if (a.offsets) {
-        long long f = a.offsets[b], e = a.offsets[b + 1];
-        f = f < 0 ? 0 : f > a.rows ? a.rows : f;
-        e = e < 0 ? 0 : e > a.rows ? a.rows : e;
-        len = e - f;
-        len = len < 0 ? 0 : len > a.T ? a.T : len;
-        lo = f;
-    }
-    const long long from = static_cast<long long>(seg) * a.seg_len, left = len - from;
+    const long long from = static_cast<long long>(seg) * a.seg_len, left = tokens_of(a, b) - from;
     Span s;
-    s.first_row = lo + from;
+    s.first_row = first_row_of(a, b) + from;
     s.tokens = static_cast<int>(left < 0 ? 0 : left > a.seg_len ? a.seg_len : left);
     s.last = left <= a.seg_len && (left > 0 || seg == 0);
     return s;
