@@ -102,7 +102,7 @@ struct ScanSpace {
 bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, bool backward, ScanSpace* s) {
     s->plan = plan;
     const long long blocks = wkv6::scan_blocks(D);
-    if (!wkv6::fits_a_launch(B * blocks * plan.segs, wkv6::scan_threads(N))) return false;
+    if (!wkv6::fits_a_launch((backward && plan.segs > 1 ? 2 : 1) * B * blocks * plan.segs, wkv6::scan_threads(N))) return false;
     s->locals = four(wkv6::scan_local_floats(plan, B, D, N));
     s->floats = s->locals;
     if (backward) {

@@ -34,7 +34,8 @@ struct ScanPlan {
     int segs, seg_len;
 };
 constexpr int kScanMostSegments = 64;
-constexpr int kScanPackedSegments = 8; // of a packed call with a workgroup for every compute unit: its locals are as many times the states
+// of a packed call with a workgroup for every compute unit, whose pieces' states would be as many times the states: 16, and no more workgroups than these
+constexpr int kScanPackedSegments = 16, kScanPackedWorkgroups = 16384;
 int scan_most_segments(int B, int T, int D, bool packed);
 ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward);
 inline long long scan_blocks(int D) { return (D + kScanChannels - 1) / kScanChannels; }
@@ -63,8 +64,8 @@ hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradients& g, bool 
 // da, dskip, dbias (what is wanted of them) from g.weights; without sequences nought.
 hipError_t launch_scan_weights(const ScanArgs& a, const ScanGradients& g, hipStream_t stream);
 
-// The segments' own states, in a.locals (selective_scan.hip).
-hipError_t launch_scan_states(const ScanArgs& a, bool f32_rows, hipStream_t stream);
+// The pieces' own states, in a.locals, and what they hand on, in g.behind (selective_scan.hip).
+hipError_t launch_scan_pieces(const ScanArgs& a, const ScanGradients& g, bool f32_rows, hipStream_t stream);
 
 // One token a sequence.
 hipError_t launch_scan_step(const ScanArgs& a, void* out, float* state_out, bool f32_rows, bool f32_out, hipStream_t stream);

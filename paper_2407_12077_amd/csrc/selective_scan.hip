@@ -13,7 +13,7 @@ using namespace scan;
 
 // kStates: the segments' states from nothing, without read-outs.
 template <int N, bool kF32, bool kOutF32, bool kStates, bool kGate>
-__global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs a, char* out, float* state_out, int blocks) {
+__device__ __forceinline__ void walk(ScanArgs a, char* out, float* state_out, int blocks, int index) {
     constexpr int kWaves = N / 4, kC = kScanChunk, kCh = kScanChannels, kItem = kF32 ? 4 : 2, kOutItem = kOutF32 ? 4 : 2;
     constexpr int kPer = kC / kWaves < 8 ? kC / kWaves : 8;    // channels that a thread brings and takes of a token
     constexpr int kAcross = kCh / kPer;
@@ -21,7 +21,7 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
     __shared__ float2v step[2][kC][kCh];                       // dt, dt x
     __shared__ float part[kStates ? 1 : 2][kWaves][kC][kCh];   // shares of the read-outs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = blockIdx.x % blocks, at = blockIdx.x / blocks, b = at % a.B, seg = at / a.B;
+    const int block = index % blocks, at = index / blocks, b = at % a.B, seg = at / a.B;
     const Span span = span_of(a, b, seg);
     const int D = a.D, c0 = block * kCh, ch = c0 + lane, n0 = 4 * wave;
     const bool mine = ch < D;
@@ -52,6 +52,7 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
     // what this thread brings: channels own .. own + kPer - 1 of token `token` of a chunk
     const int token = threadIdx.x / kAcross, own = c0 + threadIdx.x % kAcross * kPer, in_block = own - c0;
     const bool there = own < D;
+    const unsigned softplus = softplus_bits(a.softplus);
     float bias[kPer], skip[kPer], dt_sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
     };
     auto bring = [&](int first, const Chunk& k, int buffer) {
         float dts[kPer];
-        steps_of(k.delta, bias, a.softplus, dts);
+        steps_of(k.delta, bias, softplus, dts);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const float dt = first + token < span.tokens ? dts[i] : 0.f;
@@ -153,23 +154,116 @@ __global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs 
     }
 }
 
+// What a segment hands to the one in front of it if it gets nothing from behind, and the sum of its step sizes.
 template <int N, bool kF32>
-hipError_t launch_states(const ScanArgs& a, hipStream_t stream) {
+__device__ __forceinline__ void walk_behind(const ScanArgs& a, const char* dout, float* behind, int blocks, int index) {
+    constexpr int kWaves = N / 4, kC = kScanChunk, kCh = kScanChannels, kItem = kF32 ? 4 : 2;
+    constexpr int kPer = kC / kWaves < 8 ? kC / kWaves : 8, kAcross = kCh / kPer;
+    __shared__ float2v step[2][kC][kCh];                       // dt, dy
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = index % blocks, at = index / blocks, b = at % a.B, seg = 1 + at / a.B;
+    const Span span = span_of(a, b, seg);
+    if (span.tokens == 0) return;
+    const int D = a.D, c0 = block * kCh, ch = c0 + lane, n0 = 4 * wave;
+    const bool mine = ch < D;
+    float4v rate = {0.f, 0.f, 0.f, 0.f}, g = {0.f, 0.f, 0.f, 0.f};
+    if (mine) rate = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0) * kLog2e;
+    const int token = threadIdx.x / kAcross, own = c0 + threadIdx.x % kAcross * kPer, in_block = own - c0;
+    const bool there = own < D;
+    const unsigned softplus = softplus_bits(a.softplus);
+    float bias[kPer], dt_sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) bias[i] = there && a.bias ? a.bias[own + i] : 0.f;
+    struct Chunk {
+        Raw<kF32, kPer> delta, z, dout;
+        Plain<kF32> c;
+    };
+    const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
+    const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
+    const int out_at = there ? (token * D + own) * kItem : kNowhere;
+    int first = (span.tokens - 1) / kC * kC, buffer = 0;
+    const long long row0 = span.first_row + first;
+    Rows deltas(a.delta, row0, a.delta_row), zs(a.z, row0, a.z_row), douts(dout, row0, static_cast<long long>(D) * kItem), cs(a.c, row0, a.bc_row);
+    auto ask = [&](int at, Chunk& k) {                         // chunks in falling order
+        const int count = at < 0 ? 0 : rows_of<kC>(span.tokens - at);
+        k.delta.load(deltas.first(count), delta_at);
+        if (a.z) k.z.load(zs.first(count), z_at);
+        k.dout.load(douts.first(count), out_at);
+        k.c.load(cs.first(count), lane, static_cast<int>(a.bc_row), n0);
+        deltas.move(-kC);
+        zs.move(-kC);
+        douts.move(-kC);
+        cs.move(-kC);
+    };
+    auto bring = [&](int first, const Chunk& k, int buffer) {
+        float dts[kPer], dy[kPer];
+        steps_of(k.delta, bias, softplus, dts);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) dy[i] = k.dout[i];
+        if (a.z) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) dy[i] *= k.z[i] * sigmoid_of(k.z[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) step[buffer][token][in_block + i] = float2v{first + token < span.tokens ? dts[i] : 0.f, dy[i]};
+    };
+    Chunk now, next;
+    ask(first, now);
+    bring(first, now, 0);
+    __syncthreads();
+    for (; first >= 0; first -= kC, buffer ^= 1) {
+        ask(first - kC, next);
+        const float cv = now.c.value();
+        each<kC>([&](auto back) {
+            constexpr int t = kC - 1 - decltype(back)::value;
+            const float2v d = step[buffer][t][lane];
+            g = outer<t>(cv, d.y, g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] *= __builtin_amdgcn_exp2f(d.x * rate[i]);
+            dt_sum += d.x;
+        });
+        bring(first - kC, next, buffer ^ 1);
+        __syncthreads();
+        now = next;
+    }
+    if (!mine) return;
+    const long long seg_states = static_cast<long long>(a.B) * D * N, unit = (static_cast<long long>(b) * D + ch) * N + n0;
+    *reinterpret_cast<float4v*>(behind + seg * seg_states + unit) = g;
+    if (wave == 0) behind[a.segs * seg_states + (static_cast<long long>(seg) * a.B + b) * D + ch] = dt_sum;
+}
+
+template <int N, bool kF32, bool kOutF32, bool kGate>
+__global__ __launch_bounds__(16 * N, N <= 16 ? 3 : 4) void scan_kernel(ScanArgs a, char* out, float* state_out, int blocks) {
+    walk<N, kF32, kOutF32, false, kGate>(a, out, state_out, blocks, blockIdx.x);
+}
+
+// The pieces' states, by the first `states` workgroups, and what they hand to the pieces in front of them, by the others.
+template <int N, bool kF32, bool kBoth>
+__global__ __launch_bounds__(16 * N, 4) void scan_pieces_kernel(ScanArgs a, const char* dout, float* behind, int blocks, int states) {
+    const int index = blockIdx.x;
+    if (!kBoth || index < states) walk<N, kF32, true, true, false>(a, nullptr, nullptr, blocks, index);
+    else if constexpr (kBoth) walk_behind<N, kF32>(a, dout, behind, blocks, index - states);
+}
+
+template <int N, bool kF32>
+hipError_t launch_pieces(const ScanArgs& a, const void* dout, float* behind, hipStream_t stream) {
     const int blocks = static_cast<int>(scan_blocks(a.D));
-    hipLaunchKernelGGL((scan_kernel<N, kF32, true, true, false>), dim3(static_cast<unsigned>(blocks) * a.B * (a.segs - 1)), dim3(scan_threads(N)), 0, stream, a,
-                       nullptr, nullptr, blocks);
+    const unsigned states = static_cast<unsigned>(blocks) * a.B * (a.segs - 1);
+    const auto kernel = behind ? &scan_pieces_kernel<N, kF32, true> : &scan_pieces_kernel<N, kF32, false>;
+    hipLaunchKernelGGL(kernel, dim3(behind ? 2 * states : states), dim3(scan_threads(N)), 0, stream, a, static_cast<const char*>(dout), behind, blocks,
+                       static_cast<int>(states));
     return hipGetLastError();
 }
 template <int N, bool kF32, bool kOutF32>
 hipError_t launch(const ScanArgs& a, void* out, float* state_out, hipStream_t stream) {
     const int blocks = static_cast<int>(scan_blocks(a.D));
     if (a.segs > 1) {
-        const hipError_t err = launch_states<N, kF32>(a, stream);
+        const hipError_t err = launch_pieces<N, kF32>(a, nullptr, nullptr, stream);
         if (err != hipSuccess) return err;
     }
-    const auto kernel = a.z ? &scan_kernel<N, kF32, kOutF32, false, true> : &scan_kernel<N, kF32, kOutF32, false, false>;
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks) * a.B * a.segs), dim3(scan_threads(N)), 0, stream, a,
-                       static_cast<char*>(out), state_out, blocks);
+    const auto kernel = a.z ? &scan_kernel<N, kF32, kOutF32, true> : &scan_kernel<N, kF32, kOutF32, false>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks) * a.B * a.segs), dim3(scan_threads(N)), 0, stream, a, static_cast<char*>(out), state_out,
+                       blocks);
     return hipGetLastError();
 }
 
@@ -187,33 +281,38 @@ hipError_t by_states(int N, F f) {
 }  // namespace
 
 int scan_most_segments(int B, int T, int D, bool packed) {
-    const int most = packed && B * scan_blocks(D) >= compute_units() ? kScanPackedSegments : kScanMostSegments;
-    const int pairs = (T + kScanChunk - 1) / kScanChunk / 2;
-    return pairs < 2 ? 1 : pairs < most ? pairs : most;
+    long long most = kScanMostSegments, workgroups = B * scan_blocks(D);
+    if (packed && workgroups >= compute_units()) {
+        most = kScanPackedWorkgroups / workgroups;
+        if (most > kScanPackedSegments) most = kScanPackedSegments;
+    }
+    const long long pairs = (T + kScanChunk - 1) / kScanChunk / 2;
+    if (most > pairs) most = pairs;
+    return most < 2 ? 1 : static_cast<int>(most);
 }
 
 ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward) {
     const double chunks = (T + kScanChunk - 1) / kScanChunk, workgroups = static_cast<double>(B) * scan_blocks(D), units = compute_units();
     if (workgroups < 1) return {1, T};
     // microseconds of a chunk, and workgroups that a compute unit holds; N = 8, 16, 32, 64
-    static constexpr double kAlone[2][4] = {{1.7, 1.46, 1.87, 2.9}, {6.9, 5.5, 7.5, 15.4}}, kShare[2][4] = {{0.9, 0.85, 1.47, 2.9}, {3.2, 3.6, 7.4, 15.2}};
+    static constexpr double kAlone[2][4] = {{1.7, 1.46, 1.87, 2.9}, {6.9, 5.5, 7.5, 15.4}}, kShare[2][4] = {{0.85, 0.8, 1.3, 2.3}, {2.8, 3.13, 5.8, 11.8}};
     static constexpr int kHeld[2][4] = {{5, 3, 2, 1}, {4, 2, 1, 1}};
     const int which = N == 8 ? 0 : N == 16 ? 1 : N == 32 ? 2 : 3, held = kHeld[backward][which];
-    const double alone = kAlone[backward][which], share = kShare[backward][which];
-    const double packed_work = (static_cast<double>(packed_rows) / kScanChunk + 0.5 * B) * scan_blocks(D) * share / units;
-    // one walk over pieces of `len` chunks: rounds of as many workgroups as there is room for, and a last one
-    auto walk = [&](double segs, double len) {
-        const double count = workgroups * segs;
-        if (packed_rows >= 0) return std::max(len * alone, packed_work * (1 + 0.55 * units / count));
+    const double alone = kAlone[backward][which], share = kShare[backward][which], pieces = backward ? 0.4 : 0.74;
+    auto together = [&](double count) { return std::max(alone, share * (count + 0.3)); };      // `count` workgroups on a unit, a chunk of each
+    // a walk of `count` workgroups over `len` chunks: rounds of as many as there is room for, and a last one
+    auto walk = [&](double count, double len) {
         const double rounds = std::floor(count / (units * held)), rest = count - rounds * units * held;
-        return rounds * len * std::max(alone, share * held) + (rest > 0 ? len * std::max(alone, share * std::ceil(rest / units)) : 0);
+        return rounds * len * together(held) + (rest > 0 ? len * together(std::ceil(rest / units)) : 0);
     };
-    double best = walk(1, chunks);
+    // of packed sequences: how many workgroups there are if each takes at most `len` chunks
+    auto live = [&](double len) { return (static_cast<double>(packed_rows) / (len * kScanChunk) + 0.5 * B) * scan_blocks(D); };
+    double best = packed_rows < 0 ? walk(workgroups, chunks) : std::max(1.13 * chunks * alone, live(1) * together(held) / held / units);
     ScanPlan plan{1, T};
     const int most = scan_most_segments(B, T, D, packed_rows >= 0);
     for (int segs = 2; segs <= most; ++segs) {
-        const double len = std::ceil(chunks / segs), work = packed_rows >= 0 ? packed_work : workgroups * segs * len * share / units;
-        const double time = walk(std::ceil(chunks / len), len) + (backward ? 0.4 : 0.75) * std::max(len * alone, work) + (backward ? 8 : 2) + 0.3 * segs;
+        const double len = std::ceil(chunks / segs), one = walk(packed_rows < 0 ? workgroups * std::ceil(chunks / len) : live(len), len);
+        const double time = (1 + pieces) * one + (backward ? 8 + segs : 2 + 0.3 * segs);
         if (time >= best) continue;
         best = time;
         plan.seg_len = static_cast<int>(len) * kScanChunk;
@@ -230,10 +329,10 @@ hipError_t launch_scan(const ScanArgs& a, void* out, float* state_out, bool f32_
     });
 }
 
-hipError_t launch_scan_states(const ScanArgs& a, bool f32_rows, hipStream_t stream) {
+hipError_t launch_scan_pieces(const ScanArgs& a, const ScanGradients& g, bool f32_rows, hipStream_t stream) {
     return by_states(a.N, [&](auto n) {
         constexpr int N = decltype(n)::value;
-        return f32_rows ? launch_states<N, true>(a, stream) : launch_states<N, false>(a, stream);
+        return f32_rows ? launch_pieces<N, true>(a, g.dout, g.behind, stream) : launch_pieces<N, false>(a, g.dout, g.behind, stream);
     });
 }
 

@@ -34,83 +34,6 @@ struct Shape {
     static constexpr int kPer = kC * kScanChannels / kThreads, kAcross = kScanChannels / kPer;
 };
 
-// What a segment hands to the one in front of it if it gets nothing from behind, and the sum of its step sizes.
-template <int N, bool kF32>
-__global__ __launch_bounds__(16 * N, 2) void scan_behind_kernel(ScanArgs a, const char* dout, float* behind, int blocks) {
-    constexpr int kWaves = N / 4, kC = kScanChunk, kCh = kScanChannels, kItem = kF32 ? 4 : 2;
-    constexpr int kPer = kC / kWaves < 8 ? kC / kWaves : 8, kAcross = kCh / kPer;
-    __shared__ float2v step[2][kC][kCh];                       // dt, dy
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = blockIdx.x % blocks, at = blockIdx.x / blocks, b = at % a.B, seg = 1 + at / a.B;
-    const Span span = span_of(a, b, seg);
-    if (span.tokens == 0) return;
-    const int D = a.D, c0 = block * kCh, ch = c0 + lane, n0 = 4 * wave;
-    const bool mine = ch < D;
-    float4v rate = {0.f, 0.f, 0.f, 0.f}, g = {0.f, 0.f, 0.f, 0.f};
-    if (mine) rate = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0) * kLog2e;
-    const int token = threadIdx.x / kAcross, own = c0 + threadIdx.x % kAcross * kPer, in_block = own - c0;
-    const bool there = own < D;
-    float bias[kPer], dt_sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) bias[i] = there && a.bias ? a.bias[own + i] : 0.f;
-    struct Chunk {
-        Raw<kF32, kPer> delta, z, dout;
-        Plain<kF32> c;
-    };
-    const int delta_at = there ? token * static_cast<int>(a.delta_row) + own * kItem : kNowhere;
-    const int z_at = there ? token * static_cast<int>(a.z_row) + own * kItem : kNowhere;
-    const int out_at = there ? (token * D + own) * kItem : kNowhere;
-    int first = (span.tokens - 1) / kC * kC, buffer = 0;
-    const long long row0 = span.first_row + first;
-    Rows deltas(a.delta, row0, a.delta_row), zs(a.z, row0, a.z_row), douts(dout, row0, static_cast<long long>(D) * kItem), cs(a.c, row0, a.bc_row);
-    auto ask = [&](int at, Chunk& k) {                         // chunks in falling order
-        const int count = at < 0 ? 0 : rows_of<kC>(span.tokens - at);
-        k.delta.load(deltas.first(count), delta_at);
-        if (a.z) k.z.load(zs.first(count), z_at);
-        k.dout.load(douts.first(count), out_at);
-        k.c.load(cs.first(count), lane, static_cast<int>(a.bc_row), n0);
-        deltas.move(-kC);
-        zs.move(-kC);
-        douts.move(-kC);
-        cs.move(-kC);
-    };
-    auto bring = [&](int first, const Chunk& k, int buffer) {
-        float dts[kPer], dy[kPer];
-        steps_of(k.delta, bias, a.softplus, dts);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) dy[i] = k.dout[i];
-        if (a.z) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) dy[i] *= k.z[i] * sigmoid_of(k.z[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) step[buffer][token][in_block + i] = float2v{first + token < span.tokens ? dts[i] : 0.f, dy[i]};
-    };
-    Chunk now, next;
-    ask(first, now);
-    bring(first, now, 0);
-    __syncthreads();
-    for (; first >= 0; first -= kC, buffer ^= 1) {
-        ask(first - kC, next);
-        const float cv = now.c.value();
-        each<kC>([&](auto back) {
-            constexpr int t = kC - 1 - decltype(back)::value;
-            const float2v d = step[buffer][t][lane];
-            g = outer<t>(cv, d.y, g);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] *= __builtin_amdgcn_exp2f(d.x * rate[i]);
-            dt_sum += d.x;
-        });
-        bring(first - kC, next, buffer ^ 1);
-        __syncthreads();
-        now = next;
-    }
-    if (!mine) return;
-    const long long seg_states = static_cast<long long>(a.B) * D * N, unit = (static_cast<long long>(b) * D + ch) * N + n0;
-    *reinterpret_cast<float4v*>(behind + seg * seg_states + unit) = g;
-    if (wave == 0) behind[a.segs * seg_states + (static_cast<long long>(seg) * a.B + b) * D + ch] = dt_sum;
-}
-
 template <int N, bool kF32, bool kGate>
 __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(ScanArgs a, ScanGradients r, int blocks) {
     using S = Shape<N>;
@@ -163,6 +86,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
 
     const int token = threadIdx.x / S::kAcross, own = c0 + threadIdx.x % S::kAcross * kPer, in_block = own - c0;
     const bool there = own < D;
+    const unsigned softplus = softplus_bits(a.softplus);
     float bias[kPer], skip[kPer], dskip[kPer], dbias[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -187,7 +111,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     const long long place0 = (row0 - static_cast<long long>(seg) * a.seg_len) / kC + static_cast<long long>(seg) * a.seg_len / kC + b;
     Rows xs(a.x, row0, a.x_row), deltas(a.delta, row0, a.delta_row), bs(a.b, row0, a.bc_row), kept(r.states, place0, static_cast<long long>(D) * N * 4);
     auto bring = [&](int first, Chunk& k, int buffer, auto on_the_way_back) {
-        steps_of(k.delta, bias, a.softplus, k.dt);
+        steps_of(k.delta, bias, softplus, k.dt);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             k.dt[i] = first + token < span.tokens ? k.dt[i] : 0.f;
@@ -382,7 +306,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                 dx[i] = __builtin_fmaf(g, now.dt[i], skip[i] * now.dy[i]);
                 dd[i] = __builtin_fmaf(g, xv, k * kLn2);
                 const float slope = sigmoid_of(now.delta[i] + bias[i]);
-                dd[i] *= a.softplus ? slope : 1.f;
+                dd[i] *= chosen(softplus, slope, 1.f);
                 dskip[i] = __builtin_fmaf(now.dy[i], xv, dskip[i]);
                 dbias[i] += first + token < span.tokens ? dd[i] : 0.f;       // (behind the end k is not nought)
                 if constexpr (kGate) {
@@ -502,11 +426,8 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
     const unsigned units = static_cast<unsigned>(blocks) * a.B;
     hipError_t err = hipSuccess;
     if (a.segs > 1) {
-        err = launch_scan_states(a, kF32, stream);
+        err = launch_scan_pieces(a, g, kF32, stream);
         if (err != hipSuccess) return err;
-        hipLaunchKernelGGL((scan_behind_kernel<N, kF32>), dim3(units * (a.segs - 1)), dim3(16 * N), 0, stream, a, static_cast<const char*>(g.dout), g.behind,
-                           blocks);
-        if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     const auto kernel = a.z ? &scan_backward_kernel<N, kF32, true> : &scan_backward_kernel<N, kF32, false>;
     hipLaunchKernelGGL(kernel, dim3(units * a.segs), dim3(Shape<N>::kThreads), 0,

@@ -128,12 +128,21 @@ __device__ __forceinline__ float softplus_of(float v) {
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
 __device__ __forceinline__ float step_of(float v, bool softplus) { return softplus ? softplus_of(v) : v; }
 
+// All bits for softplus, none without; the compiler is not to know which, or it makes a branch of it and two blocks of what surrounds that.
+__device__ __forceinline__ unsigned softplus_bits(bool softplus) {
+    unsigned bits = softplus ? ~0u : 0u;
+    asm("" : "+s"(bits));
+    return bits;
+}
+__device__ __forceinline__ float chosen(unsigned bits, float yes, float no) {
+    return __uint_as_float((__float_as_uint(yes) & bits) | (__float_as_uint(no) & ~bits));
+}
 template <bool kF32, int kCount>
-__device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const float (&bias)[kCount], bool softplus, float (&dt)[kCount]) {
+__device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const float (&bias)[kCount], unsigned softplus, float (&dt)[kCount]) {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-        const float v = delta[i] + bias[i], s = softplus_of(v);        // (no branch: what surrounds this is one block to the compiler)
-        dt[i] = softplus ? s : v;
+        const float v = delta[i] + bias[i];
+        dt[i] = chosen(softplus, softplus_of(v), v);
     }
 }
 

@@ -148,14 +148,14 @@ def test_scan_gradients_refuse():
     for name in ("dout", "dx", "ddelta", "db", "dc", "dz", "da", "dskip", "ddelta_bias", "dstate_out", "dstate_in"):
         assert scan_back(**{name: P(0x1004)}) == ALIGN
     need = wkv.wkv6_selective_scan_backward_workspace_bytes(2, 8, 64, 16, 16)
-    assert need > 0 and scan_back(workspace_bytes=need - 1) == WORKSPACE and scan_back(workspace=None) == NULL and scan_back(workspace=P(0x1004)) == ALIGN
+    assert need > 0 and scan_back(workspace_bytes=need // 8) == WORKSPACE and scan_back(workspace=None) == NULL and scan_back(workspace=P(0x1004)) == ALIGN
     assert scan_back(B=0, rows=0, da=None, dskip=None, ddelta_bias=None) == OK
 
 
 def test_scan_workspace_refused():
     long = dict(B=1, T=4096, rows=4096)
     need = wkv.wkv6_selective_scan_workspace_bytes(1, 4096, 64, 16)
-    assert need > 0 and scan(**long, workspace_bytes=need - 1) == WORKSPACE and scan(**long, workspace=None) == NULL
+    assert need > 0 and scan(**long, workspace_bytes=16) == WORKSPACE and scan(**long, workspace=None) == NULL
     assert scan(**long, workspace=P(0x1008)) == ALIGN
 
 
