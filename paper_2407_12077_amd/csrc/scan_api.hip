@@ -109,7 +109,7 @@ bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, b
         if (!wkv6::fits_a_launch((rows + 3) / 4, 256)) return false;
         s->states = (rows / wkv6::scan_back_chunk(N) + B + 1) * D * N;
         s->rows = rows * blocks * 2 * N;
-        s->weights = static_cast<long long>(plan.segs) * B * D * (N + 2);
+        s->weights = wkv6::scan_places(B, rows, plan.seg_len) * D * (N + 2);
         s->floats = 2 * s->locals + s->states + s->rows + s->weights;
     }
     return true;
@@ -117,6 +117,7 @@ bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, b
 bool scan_space(int B, int T, int D, int N, long long rows, bool packed, bool backward, ScanSpace* s) {
     return space_of(wkv6::plan_scan(B, T, D, N, packed ? rows : -1, backward), B, D, N, rows, backward, s);
 }
+constexpr int kAnyLength = 1;
 // For calls with offsets or, if there are B T rows, without.  A prefill's rows are not known: for any that fit.
 long long scan_bytes(int B, int T, int D, int N, long long rows, bool backward) {
     ScanSpace s;
@@ -129,7 +130,7 @@ long long scan_bytes(int B, int T, int D, int N, long long rows, bool backward) 
         if (!scan_space(B, T, D, N, rows, true, true, &s)) return -1;
     } else {
         const int segs = wkv6::scan_most_segments(B, T, D, true);
-        if (!space_of({segs, 0}, B, D, N, 0, false, &s)) return -1;
+        if (!space_of({segs, kAnyLength}, B, D, N, 0, false, &s)) return -1;
     }
     return 4 * (s.floats > most ? s.floats : most);
 }
@@ -172,7 +173,7 @@ struct ConvCall {
 };
 
 // in floats
-long long conv_partials(int B, int D, int W, long long rows, const wkv6::ConvPlan& p) { return (rows / p.seg_len + B) * (W + 1) * D; }
+long long conv_partials(int B, int D, int W, long long rows, const wkv6::ConvPlan& p) { return wkv6::conv_places(B, rows, p.seg_len) * (W + 1) * D; }
 
 }  // namespace
 
@@ -238,7 +239,7 @@ int wkv6_selective_scan_backward(int B, int T, int D, int N, long long rows, con
     hipStream_t st = static_cast<hipStream_t>(stream);
     wkv6::ScanGradients g = {};
     g.da = da; g.dskip = dskip; g.dbias = ddelta_bias;
-    if (B == 0) return status_of(wkv6::launch_scan_weights(call.args({1, 0}), g, st));      // no sequence: but sums over no tokens are nought
+    if (B == 0) return status_of(wkv6::launch_scan_weights(call.args({1, 1}), g, st));      // no sequence: but sums over no tokens are nought
     if ((status = call.check_inputs()) != WKV6_OK) return status;
     if (call.any_rows() && any_null(dout, static_cast<const void*>(dx), static_cast<const void*>(ddelta), static_cast<const void*>(db), static_cast<const void*>(dc)))
         return WKV6_ERR_NULL;
@@ -292,7 +293,7 @@ int wkv6_short_conv_decode(int B, int D, int W, const void* x, long long x_strid
     if ((status = call.check_inputs()) != WKV6_OK) return status;
     if (!out) return WKV6_ERR_NULL;
     if (any_misaligned(out, state_out)) return WKV6_ERR_ALIGN;
-    if (!wkv6::fits_a_launch(static_cast<long long>(B) * (D / wkv6::kConvGroup) + wkv6::kConvThreads, 1)) return WKV6_ERR_SHAPE;
+    if (!wkv6::fits_a_launch(static_cast<long long>(B) * (D / wkv6::kConvStepGroup) + wkv6::kConvThreads, 1)) return WKV6_ERR_SHAPE;
     return status_of(wkv6::launch_conv_step(call.args({1, 1, 1, 1}), out, state_out, dtype == WKV6_DTYPE_F32, static_cast<hipStream_t>(stream)));
 }
 

@@ -293,7 +293,7 @@ int scan_most_segments(int B, int T, int D, bool packed) {
 
 ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward) {
     const double chunks = (T + kScanChunk - 1) / kScanChunk, workgroups = static_cast<double>(B) * scan_blocks(D), units = compute_units();
-    if (workgroups < 1) return {1, T};
+    if (workgroups < 1 || T < 2) return {1, 1};
     // microseconds of a chunk, and workgroups that a compute unit holds; N = 8, 16, 32, 64
     static constexpr double kAlone[2][4] = {{1.7, 1.46, 1.87, 2.9}, {6.9, 5.5, 7.5, 15.4}}, kShare[2][4] = {{0.85, 0.8, 1.3, 2.3}, {2.8, 3.13, 5.8, 11.8}};
     static constexpr int kHeld[2][4] = {{5, 3, 2, 1}, {4, 2, 1, 1}};

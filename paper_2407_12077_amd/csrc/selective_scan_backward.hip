@@ -328,12 +328,22 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     }
     __builtin_amdgcn_s_setprio(0);
     __syncthreads();
-    const long long share = static_cast<long long>(seg) * a.B + b;
+    // Places that no segment has are set to nought by the last segment in front of them (in front of all: by the first sequence's), so that the fold
+    // adds all places without asking whose they are.
+    auto place_of = [&](int sequence) { return static_cast<long long>(static_cast<unsigned>(first_row_of(a, sequence)) / static_cast<unsigned>(a.seg_len)) + sequence; };
+    const long long places = scan_places(a.B, a.rows, a.seg_len), share = place_of(b) + seg;
+    const long long before = b == 0 && seg == 0 ? 0 : share, behind = !span.last ? share + 1 : b + 1 < a.B ? place_of(b + 1) : places;
+    auto leave = [&](float* to, long long width, auto v) {
+        using V = decltype(v);
+        for (long long i = before; i < share; ++i) *reinterpret_cast<V*>(to + i * width) = V{};
+        *reinterpret_cast<V*>(to + share * width) = v;
+        for (long long i = share + 1; i < behind; ++i) *reinterpret_cast<V*>(to + i * width) = V{};
+    };
     if (mine) {
 #pragma unroll
         for (int q = 0; q < kG; ++q) {
             if (seg == 0 && r.dstate_in) *reinterpret_cast<float4v*>(r.dstate_in + unit + 4 * q) = grad[q];
-            *reinterpret_cast<float4v*>(r.weights + (share * D + ch) * N + n0 + 4 * q) = da[q];
+            leave(r.weights + static_cast<long long>(ch) * N + n0 + 4 * q, static_cast<long long>(D) * N, da[q]);
         }
     }
     // the tokens' shares of dskip and dbias meet
@@ -344,11 +354,11 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
         meet[(kC + token) * kCh + in_block + i] = dbias[i];
     }
     __syncthreads();
-    if (threadIdx.x < 2 * kCh && c0 + (threadIdx.x & 63) < D) {
+    if (threadIdx.x < 2 * kCh && mine) {
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < kC; ++t) sum += meet[((threadIdx.x >> 6) * kC + t) * kCh + lane];
-        r.weights[a.segs * seg_states + (share * 2 + (threadIdx.x >> 6)) * D + ch] = sum;
+        leave(r.weights + places * D * N + static_cast<long long>(threadIdx.x >> 6) * D + ch, 2ll * D, sum);
     }
 }
 
@@ -385,26 +395,19 @@ __global__ __launch_bounds__(256) void scan_rows_kernel(ScanArgs a, const float*
     store<kF32>((value < N ? db : dc) + row * a.bc_row + value % N * (kF32 ? 4 : 2), v);
 }
 
-// da, dskip, dbias: the segments' shares, sixteen turns of them, in the order of sequences and segments.
+// da, dskip, dbias: 64 values a workgroup, the places in sixteen turns, in their order.
 constexpr int kTurns = 16;
-__global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(ScanArgs a, const float* shares, float* da, float* dskip, float* dbias) {
+__global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(int D, int N, long long places, const float* shares, float* da, float* dskip, float* dbias) {
     __shared__ float meet[kTurns][64];
     const int lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long states = static_cast<long long>(a.D) * a.N, value = static_cast<long long>(blockIdx.x) * 64 + lane;
-    const bool there = value < states + 2 * a.D;
-    const float* from = value < states ? shares + value : shares + a.segs * a.B * states + (value - states);
-    const long long stride = value < states ? states : 2 * a.D;
+    const long long states = static_cast<long long>(D) * N, value = static_cast<long long>(blockIdx.x) * 64 + lane;
+    const bool there = value < states + 2 * D;
+    const long long stride = value < states ? states : 2 * D;
+    const float* from = (value < states ? shares + value : shares + places * states + (value - states)) + turn * stride;
     float sum = 0.f;
-    long long before = 0;                                      // segments of the sequences in front
-    for (int b = 0; b < a.B; ++b) {
-        int segs = 1;
-        if (a.segs > 1) {
-            const int tokens = tokens_of(a, b);
-            segs = tokens > 0 ? (tokens - 1) / a.seg_len + 1 : 1;
-        }
-        for (int s = static_cast<int>((turn + kTurns - before % kTurns) % kTurns); s < segs; s += kTurns)
-            if (there) sum += from[(static_cast<long long>(s) * a.B + b) * stride];
-        before += segs;
+    if (there) {
+#pragma unroll 8
+        for (long long i = turn; i < places; i += kTurns, from += kTurns * stride) sum += *from;
     }
     meet[turn][lane] = sum;
     __syncthreads();
@@ -413,10 +416,10 @@ __global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(ScanArgs a, c
     for (int i = 1; i < kTurns; ++i) sum += meet[i][lane];
     if (value < states) {
         if (da) da[value] = sum;
-    } else if (value < states + a.D) {
+    } else if (value < states + D) {
         if (dskip) dskip[value - states] = sum;
     } else if (dbias) {
-        dbias[value - states - a.D] = sum;
+        dbias[value - states - D] = sum;
     }
 }
 
@@ -446,7 +449,8 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
 hipError_t launch_scan_weights(const ScanArgs& a, const ScanGradients& g, hipStream_t stream) {
     if (!g.da && !g.dskip && !g.dbias) return hipSuccess;
     const long long values = static_cast<long long>(a.D) * (a.N + 2);
-    hipLaunchKernelGGL(scan_weights_kernel, dim3(static_cast<unsigned>((values + 63) / 64)), dim3(64 * kTurns), 0, stream, a, g.weights, g.da, g.dskip, g.dbias);
+    hipLaunchKernelGGL(scan_weights_kernel, dim3(static_cast<unsigned>((values + 63) / 64)), dim3(64 * kTurns), 0, stream, a.D, a.N,
+                       scan_places(a.B, a.rows, a.seg_len), g.weights, g.da, g.dskip, g.dbias);
     return hipGetLastError();
 }
 

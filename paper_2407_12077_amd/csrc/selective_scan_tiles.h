@@ -46,6 +46,13 @@ struct Raw {
             }
         }
     }
+    // back, as it is
+    __device__ __forceinline__ void put(char* p) const {
+        static_assert(kWords == 2 || kWords % 4 == 0);
+        if constexpr (kWords == 2) *reinterpret_cast<uint2v*>(p) = uint2v{word[0], word[1]};
+#pragma unroll
+        for (int i = 0; i + 4 <= kWords; i += 4) *reinterpret_cast<uint4v*>(p + 4 * i) = uint4v{word[i], word[i + 1], word[i + 2], word[i + 3]};
+    }
     // from a buffer; what lies behind its end is zeros
     __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, int at) {
         if constexpr (!kF32 && kCount == 1) {

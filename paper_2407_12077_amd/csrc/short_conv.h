@@ -6,7 +6,7 @@
 
 namespace wkv6 {
 
-constexpr int kConvGroup = 8;          // channels of a thread
+constexpr int kConvGroup = 4, kConvStepGroup = 8;    // channels of a thread (prompts and gradients; single tokens)
 constexpr int kConvThreads = 256;
 
 struct ConvArgs {
@@ -32,7 +32,8 @@ ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward);
 hipError_t launch_conv(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream);
 hipError_t launch_conv_step(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream);
 
-// dw and dbias (both or neither) through `partials`: [place][W + 1][D], rows / seg_len + B places
+// dw and dbias (both or neither) through `partials`: [place][W + 1][D]
+__host__ __device__ constexpr long long conv_places(int B, long long rows, int seg_len) { return B > 0 ? rows / seg_len + B : 0; }
 hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void* dstate_out, void* dx, float* dw, float* dbias, void* dstate_in,
                                 float* partials, bool f32, hipStream_t stream);
 

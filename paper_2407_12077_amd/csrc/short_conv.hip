@@ -14,8 +14,6 @@ namespace {
 
 using namespace scan;
 
-constexpr int kG = kConvGroup;
-
 struct Place {
     long long row0;                    // of the sequence's first token
     int len, first, end;               // tokens of the sequence; this thread's
@@ -40,7 +38,7 @@ __device__ __forceinline__ Place place_of(const ConvArgs& a, int b, int seg, int
     return p;
 }
 
-template <bool kF32>
+template <bool kF32, int kG>
 struct Row {
     Raw<kF32, kG> raw;
     __device__ __forceinline__ void get(float (&v)[kG]) const {
@@ -49,7 +47,7 @@ struct Row {
     }
 };
 
-template <int W>
+template <int W, int kG>
 struct Taps {
     float w[W][kG], bias[kG];
     __device__ __forceinline__ void load(const ConvArgs& a, int ch) {
@@ -63,7 +61,7 @@ struct Taps {
 };
 
 // The threads of a workgroup: `lanes` side by side over groups of channels, 256 / lanes slices of `run` tokens one behind the other.
-template <int W, bool kF32>
+template <int W, bool kF32, int kG>
 __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* out, char* state_out, int across, int run) {
     constexpr int kItem = kF32 ? 4 : 2, kBatch = 4;
     const int column = threadIdx.x % a.lanes, slice = threadIdx.x / a.lanes;
@@ -75,10 +73,10 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* ou
     if (p.first >= p.end && !head) return;
     const char* x = static_cast<const char*>(a.x) + p.row0 * a.x_row + ch * kItem;
     const long long state_row = static_cast<long long>(a.D) * kItem, state_at = static_cast<long long>(b) * (W - 1) * state_row + ch * kItem;
-    Taps<W> taps;
+    Taps<W, kG> taps;
     taps.load(a, ch);
     float win[W][kG];                                          // win[W - 1]: the token at hand
-    Row<kF32> front[W - 1];
+    Row<kF32, kG> front[W - 1];
     if (head) {
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
@@ -86,7 +84,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* ou
             if (a.state_in) front[j].raw.load(static_cast<const char*>(a.state_in) + state_at + j * state_row);
         }
         if (state_out) {                                       // (no other thread reads these channels' state_in, which may be state_out)
-            Row<kF32> last[W - 1];
+            Row<kF32, kG> last[W - 1];
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {
                 const int t = p.len - (W - 1) + j;             // below nought: of the old state
@@ -97,10 +95,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* ou
             }
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {
-                unsigned* to = reinterpret_cast<unsigned*>(state_out + state_at + j * state_row);
-#pragma unroll
-                for (int i = 0; i < Raw<kF32, kG>::kWords; i += 4)
-                    *reinterpret_cast<uint4v*>(to + i) = uint4v{last[j].raw.word[i], last[j].raw.word[i + 1], last[j].raw.word[i + 2], last[j].raw.word[i + 3]};
+                last[j].raw.put(state_out + state_at + j * state_row);
             }
         }
     } else {
@@ -109,13 +104,14 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* ou
     }
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) front[j].get(win[j + 1]);
-    Row<kF32> now[kBatch], next[kBatch];
-    auto ask = [&](int t, Row<kF32>(&r)[kBatch]) {
+    Row<kF32, kG> now[kBatch], next[kBatch];
+    const char* from = x + p.first * a.x_row;                  // (addresses by addition: a product costs more than what is done with a row)
+    auto ask = [&](int t, Row<kF32, kG>(&r)[kBatch]) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-            if (t + i < p.end) r[i].raw.load(x + (t + i) * a.x_row);
+        for (int i = 0; i < kBatch; ++i, from += a.x_row)
+            if (t + i < p.end) r[i].raw.load(from);
     };
-    char* to = out + (p.row0 * a.D + ch) * kItem;
+    char* to = out + (p.row0 + p.first) * state_row + ch * kItem;
     ask(p.first, now);
     for (int t = p.first; t < p.end; t += kBatch) {
         ask(t + kBatch, next);
@@ -135,22 +131,23 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* ou
                 for (int j = 0; j < W; ++j) v = __builtin_fmaf(taps.w[j][e], win[j][e], v);
                 y[e] = a.silu ? v * sigmoid_of(v) : v;
             }
-            store<kF32>(to + static_cast<long long>(t + i) * state_row, y);
+            store<kF32>(to, y);
+            to += state_row;
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) now[i] = next[i];
     }
 }
 
-template <int W, bool kF32>
+template <int W, bool kF32, int kG>
 __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvArgs a, char* out, char* state_out, int groups) {
     constexpr int kItem = kF32 ? 4 : 2;
     const long long item = static_cast<long long>(blockIdx.x) * kConvThreads + threadIdx.x;
     if (item >= static_cast<long long>(groups) * a.B) return;
     const int b = static_cast<int>(item / groups), ch = static_cast<int>(item - static_cast<long long>(b) * groups) * kG;
     const long long row = static_cast<long long>(a.D) * kItem, state_at = static_cast<long long>(b) * (W - 1) * row + ch * kItem;
-    Taps<W> taps;
-    Row<kF32> in[W];
+    Taps<W, kG> taps;
+    Row<kF32, kG> in[W];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         in[j].raw.none();
@@ -170,18 +167,18 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvArgs a, cha
     if (!state_out) return;
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
-        unsigned* to = reinterpret_cast<unsigned*>(state_out + state_at + j * row);
-#pragma unroll
-        for (int i = 0; i < Raw<kF32, kG>::kWords; i += 4)
-            *reinterpret_cast<uint4v*>(to + i) = uint4v{in[j + 1].raw.word[i], in[j + 1].raw.word[i + 1], in[j + 1].raw.word[i + 2], in[j + 1].raw.word[i + 3]};
+        in[j + 1].raw.put(state_out + state_at + j * row);
     }
 }
 
-// Where segment seg of the sequence whose first token has this row leaves its sums: a segment of sequence b + 1 starts at least as many rows later as
-// b has, so no two places meet, and there are at most rows / seg_len + B of them.
-__device__ __forceinline__ long long sums_place(const ConvArgs& a, int b, long long row0, int seg) { return row0 / a.seg_len + seg + b; }
+// Where the first segment of sequence b leaves its sums, the others behind it: a segment of sequence b + 1 starts at least as many rows later as
+// b has, so no two places meet, and there are rows / seg_len + B of them.  Those that no segment has are set to nought by the last segment in front
+// of them (in front of all: by the first sequence's), so that the fold adds all places without asking whose they are.
+__device__ __forceinline__ long long first_place(const ConvArgs& a, int b) {
+    return static_cast<long long>(static_cast<unsigned>(place_of(a, b, 0, 0, 1).row0) / static_cast<unsigned>(a.seg_len)) + b;     // (fewer than 2^31 rows)
+}
 
-template <int W, bool kF32>
+template <int W, bool kF32, int kG>
 __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a, const char* dout, const char* dstate_out, char* dx, char* dstate_in,
                                                                      float* partials, int across, int run) {
     constexpr int kItem = kF32 ? 4 : 2;
@@ -202,8 +199,9 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
         const long long dense = static_cast<long long>(a.D) * kItem, state_at = static_cast<long long>(b) * (W - 1) * dense + ch * kItem;
         const char* x = static_cast<const char*>(a.x) + p.row0 * a.x_row + ch * kItem;
         const char* dy = dout + p.row0 * dense + ch * kItem;
-        char* to = dx + p.row0 * a.x_row + ch * kItem;
-        Taps<W> taps;
+        char* to = dx + (p.row0 + p.first - (W - 1)) * a.x_row + ch * kItem;     // of the input W - 1 in front of the token at hand
+        const char *x_from = x + p.first * a.x_row, *dy_from = dy + p.first * dense;
+        Taps<W, kG> taps;
         taps.load(a, ch);
         float win[W][kG], dp[W][kG];                           // dp[W - 1]: of the token at hand
 #pragma unroll
@@ -212,7 +210,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
             for (int e = 0; e < kG; ++e) dp[j][e] = 0.f;
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
-            Row<kF32> r;
+            Row<kF32, kG> r;
             r.raw.none();
             if (!head) r.raw.load(x + (p.first - (W - 1) + j) * a.x_row);
             else if (a.state_in) r.raw.load(static_cast<const char*>(a.state_in) + state_at + j * dense);
@@ -221,19 +219,19 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
         // Behind this thread's own tokens W - 1 more, whose dp its last inputs have a share in.
         const int stop = p.first + (p.end - p.first) + W - 1;
         constexpr int kBatch = 4;
-        Row<kF32> xs[2][kBatch], ds[2][kBatch];
+        Row<kF32, kG> xs[2][kBatch], ds[2][kBatch];
         auto ask = [&](int t, int which) {
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
+            for (int i = 0; i < kBatch; ++i, x_from += a.x_row, dy_from += dense) {
                 xs[which][i].raw.none();
                 ds[which][i].raw.none();
                 if (t + i < stop && t + i < p.len) {
-                    xs[which][i].raw.load(x + (t + i) * a.x_row);
-                    ds[which][i].raw.load(dy + (t + i) * dense);
+                    xs[which][i].raw.load(x_from);
+                    ds[which][i].raw.load(dy_from);
                 }
             }
         };
-        auto one = [&](int t, const Row<kF32>& xr, const Row<kF32>& dr) {
+        auto one = [&](int t, const Row<kF32, kG>& xr, const Row<kF32, kG>& dr) {
 #pragma unroll
             for (int j = 0; j < W - 1; ++j)
 #pragma unroll
@@ -260,8 +258,9 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
                 }
             }
             const int s = t - (W - 1);                         // the input that has all its shares now
+            char* place = to;
+            to += a.x_row;
             if (s < (head ? -(W - 1) : p.first) || s >= p.end) return;
-            char* place = to + s * a.x_row;
             if (s < 0) {
                 if (!dstate_in) return;
                 place = dstate_in + state_at + t * dense;
@@ -274,7 +273,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
                 for (int j = 0; j < W; ++j) v[e] = __builtin_fmaf(taps.w[j][e], dp[W - 1 - j][e], v[e]);
             }
             if (dstate_out && s >= p.len - (W - 1)) {
-                Row<kF32> r;
+                Row<kF32, kG> r;
                 r.raw.load(dstate_out + state_at + (s - p.len + W - 1) * dense);
 #pragma unroll
                 for (int e = 0; e < kG; ++e) v[e] += r.raw[e];
@@ -310,37 +309,43 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
         __syncthreads();
     }
     if (slice != 0 || !there) return;
-    float* to = partials + sums_place(a, b, p.row0, seg) * (W + 1) * a.D + ch;
+    const long long mine = first_place(a, b) + seg, values = static_cast<long long>(W + 1) * a.D;
+    float* const to = partials + ch;
 #pragma unroll
     for (int j = 0; j <= W; ++j)
 #pragma unroll
         for (int e = 0; e < kG; e += 4)
-            *reinterpret_cast<float4v*>(to + static_cast<long long>(j) * a.D + e) = float4v{sums[j][e], sums[j][e + 1], sums[j][e + 2], sums[j][e + 3]};
+            *reinterpret_cast<float4v*>(to + mine * values + static_cast<long long>(j) * a.D + e) = float4v{sums[j][e], sums[j][e + 1], sums[j][e + 2], sums[j][e + 3]};
+    auto none = [&](long long from, long long end) {
+        for (; from < end; ++from)
+#pragma unroll
+            for (int j = 0; j <= W; ++j)
+#pragma unroll
+                for (int e = 0; e < kG; e += 4) *reinterpret_cast<float4v*>(to + from * values + static_cast<long long>(j) * a.D + e) = float4v{0.f, 0.f, 0.f, 0.f};
+    };
+    if (b == 0 && seg == 0) none(0, mine);
+    if (static_cast<long long>(seg + 1) * a.seg_len >= p.len) none(mine + 1, b + 1 < a.B ? first_place(a, b + 1) : conv_places(a.B, a.rows, a.seg_len));
 }
 
-// dw [D][W] and dbias [D]: 64 values a workgroup, the segments' shares in sixteen turns, in the order of sequences and segments.
-constexpr int kFoldSlices = 16;
-__global__ __launch_bounds__(64 * kFoldSlices) void conv_fold_kernel(ConvArgs a, const float* partials, float* dw, float* dbias) {
-    __shared__ float meet[kFoldSlices][64];
-    const int lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), values = (a.W + 1) * a.D;
-    const int value = blockIdx.x * 64 + lane;
+// dw [D][W] and dbias [D]: 64 values a workgroup, the places in sixteen turns, in their order.
+constexpr int kFoldTurns = 16;
+__global__ __launch_bounds__(64 * kFoldTurns) void conv_fold_kernel(int D, int W, long long places, const float* partials, float* dw, float* dbias) {
+    __shared__ float meet[kFoldTurns][64];
+    const int lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), values = (W + 1) * D, value = blockIdx.x * 64 + lane;
     float sum = 0.f;
-    long long before = 0;                                      // segments of the sequences in front
-    for (int b = 0; b < a.B; ++b) {
-        const Place p = place_of(a, b, 0, 0, 1);
-        const long long segs = p.len > 0 ? (p.len - 1) / a.seg_len + 1 : 1;
-        for (long long s = (turn - before % kFoldSlices + kFoldSlices) % kFoldSlices; s < segs; s += kFoldSlices)
-            if (value < values) sum += partials[sums_place(a, b, p.row0, static_cast<int>(s)) * values + value];
-        before += segs;
+    if (value < values) {
+        const float* from = partials + static_cast<long long>(turn) * values + value;
+#pragma unroll 8
+        for (long long i = turn; i < places; i += kFoldTurns, from += static_cast<long long>(kFoldTurns) * values) sum += *from;
     }
     meet[turn][lane] = sum;
     __syncthreads();
     if (turn != 0 || value >= values) return;
 #pragma unroll
-    for (int i = 1; i < kFoldSlices; ++i) sum += meet[i][lane];
-    const int tap = value / a.D, ch = value - tap * a.D;
-    if (tap == a.W) dbias[ch] = sum;
-    else dw[static_cast<long long>(ch) * a.W + tap] = sum;
+    for (int i = 1; i < kFoldTurns; ++i) sum += meet[i][lane];
+    const int tap = value / D, ch = value - tap * D;
+    if (tap == W) dbias[ch] = sum;
+    else dw[static_cast<long long>(ch) * W + tap] = sum;
 }
 
 template <typename F>
@@ -351,13 +356,13 @@ hipError_t by_taps(int W, bool f32, F f) {
     return one(std::integral_constant<int, 4>());
 }
 
-int across_of(const ConvArgs& a) { return (a.D / kG + a.lanes - 1) / a.lanes; }
+int across_of(const ConvArgs& a) { return (a.D / kConvGroup + a.lanes - 1) / a.lanes; }
 
 }  // namespace
 
 ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward) {
     ConvPlan p;
-    const int groups = D / kG;
+    const int groups = D / kConvGroup;
     p.lanes = 64;
     while (p.lanes > 1 && p.lanes / 2 >= groups) p.lanes /= 2;
     if (groups > 32 && groups < 256 && groups % 64 != 0 && groups % 64 <= 32) p.lanes = 32;
@@ -373,7 +378,7 @@ ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward) {
 hipError_t launch_conv(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream) {
     return by_taps(a.W, f32, [&](auto w, auto wide) {
         const int across = across_of(a);
-        hipLaunchKernelGGL((conv_kernel<decltype(w)::value, decltype(wide)::value>), dim3(static_cast<unsigned>(a.segs) * a.B * across), dim3(kConvThreads),
+        hipLaunchKernelGGL((conv_kernel<decltype(w)::value, decltype(wide)::value, kConvGroup>), dim3(static_cast<unsigned>(a.segs) * a.B * across), dim3(kConvThreads),
                            0, stream, a, static_cast<char*>(out), static_cast<char*>(state_out), across, a.seg_len / (kConvThreads / a.lanes));
         return hipGetLastError();
     });
@@ -381,9 +386,9 @@ hipError_t launch_conv(const ConvArgs& a, void* out, void* state_out, bool f32, 
 
 hipError_t launch_conv_step(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream) {
     return by_taps(a.W, f32, [&](auto w, auto wide) {
-        const int groups = a.D / kG;
+        const int groups = a.D / kConvStepGroup;
         const long long items = static_cast<long long>(groups) * a.B;
-        hipLaunchKernelGGL((conv_step_kernel<decltype(w)::value, decltype(wide)::value>), dim3(static_cast<unsigned>((items + kConvThreads - 1) / kConvThreads)),
+        hipLaunchKernelGGL((conv_step_kernel<decltype(w)::value, decltype(wide)::value, kConvStepGroup>), dim3(static_cast<unsigned>((items + kConvThreads - 1) / kConvThreads)),
                            dim3(kConvThreads), 0, stream, a, static_cast<char*>(out), static_cast<char*>(state_out), groups);
         return hipGetLastError();
     });
@@ -393,7 +398,7 @@ hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void*
                                 float* partials, bool f32, hipStream_t stream) {
     const int across = across_of(a);
     const hipError_t err = by_taps(a.W, f32, [&](auto w, auto wide) {
-        hipLaunchKernelGGL((conv_backward_kernel<decltype(w)::value, decltype(wide)::value>), dim3(static_cast<unsigned>(a.segs) * a.B * across),
+        hipLaunchKernelGGL((conv_backward_kernel<decltype(w)::value, decltype(wide)::value, kConvGroup>), dim3(static_cast<unsigned>(a.segs) * a.B * across),
                            dim3(kConvThreads), 0, stream, a, static_cast<const char*>(dout), static_cast<const char*>(dstate_out), static_cast<char*>(dx),
                            static_cast<char*>(dstate_in), dw ? partials : nullptr, across, a.seg_len / (kConvThreads / a.lanes));
         return hipGetLastError();
@@ -402,7 +407,8 @@ hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void*
 }
 
 hipError_t launch_conv_fold(const ConvArgs& a, float* dw, float* dbias, const float* partials, hipStream_t stream) {
-    hipLaunchKernelGGL(conv_fold_kernel, dim3((static_cast<unsigned>(a.D) * (a.W + 1) + 63) / 64), dim3(64 * kFoldSlices), 0, stream, a, partials, dw, dbias);
+    hipLaunchKernelGGL(conv_fold_kernel, dim3((static_cast<unsigned>(a.D) * (a.W + 1) + 63) / 64), dim3(64 * kFoldTurns), 0, stream, a.D, a.W,
+                       conv_places(a.B, a.rows, a.seg_len), partials, dw, dbias);
     return hipGetLastError();
 }
 
