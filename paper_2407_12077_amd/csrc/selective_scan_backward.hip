@@ -226,7 +226,10 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                     decay[t][q][i] = __builtin_amdgcn_exp2f(d.x * rate[q][i]);
                     state[t + 1][q][i] = __builtin_fmaf(decay[t][q][i], state[t][q][i], add[i]);
                 }
-                if constexpr (kGate) y += read_out<t % 4>(now.ct[q].value(t / 4), state[t + 1][q]);
+                if constexpr (kGate) {
+                    const float share = read_out<t % 4>(now.ct[q].value(t / 4), state[t + 1][q]);
+                    y = q == 0 ? share : y + share;
+                }
             }
             if constexpr (kGate) part[2][wave][t][lane] = y;
         });
@@ -244,7 +247,8 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
                 grad[q] = outer<t>(now.c[q].value(), dy, grad[q]);
-                into += read_out<t % 4>(now.bt[q].value(t / 4), grad[q]);
+                const float share = read_out<t % 4>(now.bt[q].value(t / 4), grad[q]);
+                into = q == 0 ? share : into + share;
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
