@@ -122,14 +122,15 @@ __device__ __forceinline__ void walk(ScanArgs a, char* out, float* state_out, in
         ask(span.tokens - first - kC, next);
         if constexpr (!kStates) leave(first > 0 ? kC : 0, before, buffer ^ 1);     // (nothing in the first turn)
         const float bv = now.b.value();
+        float dt_chunk = 0.f;
         each<kC>([&](auto token_of_chunk) {
             constexpr int t = decltype(token_of_chunk)::value;
             const float2v d = step[buffer][t][lane];
             const float4v add = outer<t>(bv, d.y);
-            if constexpr (kStates) dt_sum += d.x;
+            if constexpr (kStates) dt_chunk += d.x;
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d.x * rate[i]), h[i], add[i]);
-            if constexpr (!kStates) part[buffer][wave][t][lane] = read_out<t % 4>(now.c.value(t / 4), h);
+            if constexpr (!kStates) part[buffer][wave][t][lane] = read_out<t % 4>(now.c.value(t / 4), h, h[0]);
             if constexpr (t == 3) __builtin_amdgcn_s_setprio(2);
             if constexpr (t == 7) {
                 __builtin_amdgcn_s_setprio(1);
@@ -137,6 +138,7 @@ __device__ __forceinline__ void walk(ScanArgs a, char* out, float* state_out, in
             }
         });
         __builtin_amdgcn_s_setprio(0);
+        if constexpr (kStates) dt_sum += dt_chunk;
         bring(first + kC, next, buffer ^ 1);
         before = now;
         now = next;
@@ -214,14 +216,16 @@ __device__ __forceinline__ void walk_behind(const ScanArgs& a, const char* dout,
     for (; first >= 0; first -= kC, buffer ^= 1) {
         ask(first - kC, next);
         const float cv = now.c.value();
+        float dt_chunk = 0.f;
         each<kC>([&](auto back) {
             constexpr int t = kC - 1 - decltype(back)::value;
             const float2v d = step[buffer][t][lane];
             g = outer<t>(cv, d.y, g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) g[i] *= __builtin_amdgcn_exp2f(d.x * rate[i]);
-            dt_sum += d.x;
+            dt_chunk += d.x;
         });
+        dt_sum += dt_chunk;
         bring(first - kC, next, buffer ^ 1);
         __syncthreads();
         now = next;

@@ -227,7 +227,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                     state[t + 1][q][i] = __builtin_fmaf(decay[t][q][i], state[t][q][i], add[i]);
                 }
                 if constexpr (kGate) {
-                    const float share = read_out<t % 4>(now.ct[q].value(t / 4), state[t + 1][q]);
+                    const float share = read_out<t % 4>(now.ct[q].value(t / 4), state[t + 1][q], state[t + 1][q][0]);
                     y = q == 0 ? share : y + share;
                 }
             }
@@ -247,13 +247,16 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
 #pragma unroll
             for (int q = 0; q < kG; ++q) {
                 grad[q] = outer<t>(now.c[q].value(), dy, grad[q]);
-                const float share = read_out<t % 4>(now.bt[q].value(t / 4), grad[q]);
-                into = q == 0 ? share : into + share;
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     v[i] = grad[q][i] * d.y;
                     v[4 + i] = state[t + 1][q][i] * dy;
+                }
+                const float share = read_out<t % 4>(now.bt[q].value(t / 4), grad[q], v[0]);
+                into = q == 0 ? share : into + share;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
                     grad[q][i] *= decay[t][q][i];
                     const float k = grad[q][i] * state[t][q][i];
                     da_chunk[q][i] = __builtin_fmaf(k, d.x, da_chunk[q][i]);

@@ -208,18 +208,20 @@ __device__ __forceinline__ int rows_of(int left) {
 constexpr int kNowhere = 0x7fffff00;   // an offset behind the end of any such rows
 
 // c[0] h[0] + c[1] h[1] + c[2] h[2] + c[3] h[3] where c's values lie in lanes 4 kFirst .. 4 kFirst + 3 of every row of sixteen lanes: operands that
-// come from another lane cost nothing, but the compiler makes moves of them in front of a multiply-add.  A register that a vector
-// instruction has written may be read from other lanes two states later: the s_nop, here and not where the compiler could move it.
+// come from another lane cost nothing, but the compiler makes moves of them in front of a multiply-add.  It does not know what is in here, so it
+// keeps no distance to it: a register that a vector instruction has written may be read from other lanes two states later (the s_nop, here and
+// not where the compiler could move it), and one that a matrix instruction has written only after more.  h has to come from vector
+// instructions, or `after` from one that has read it, for which the compiler has waited.
 template <int kFirst>
-__device__ __forceinline__ float read_out(float c, float4v h) {
+__device__ __forceinline__ float read_out(float c, float4v h, float after) {
     float y;
     asm("s_nop 1\n\t"
-        "v_mul_f32_dpp %0, %1, %2 row_newbcast:%c6 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%c7 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%c8 row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%c9 row_mask:0xf bank_mask:0xf"
+        "v_mul_f32_dpp %0, %1, %2 row_newbcast:%c7 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%c8 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%c9 row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%c10 row_mask:0xf bank_mask:0xf"
         : "=&v"(y)
-        : "v"(c), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "n"(4 * kFirst), "n"(4 * kFirst + 1), "n"(4 * kFirst + 2), "n"(4 * kFirst + 3));
+        : "v"(c), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "v"(after), "n"(4 * kFirst), "n"(4 * kFirst + 1), "n"(4 * kFirst + 2), "n"(4 * kFirst + 3));
     return y;
 }
 

@@ -205,8 +205,11 @@ class Conv(Rows):
         self.dout = normal(R, D).to(dtype)
         self.dstate_out = normal(self.B, W - 1, D).to(dtype) if state else None
 
+    def blank_out(self):
+        return torch.full((self.rows, self.D), UNTOUCHED, dtype=self.dtype, device="cuda")
+
     def prefill(self, state_out="new"):
-        out = torch.full((self.rows, self.D), UNTOUCHED, dtype=self.dtype, device="cuda")
+        out = self.blank_out()
         if isinstance(state_out, str):
             state_out = torch.full((self.B, self.W - 1, self.D), float("nan"), dtype=self.dtype, device="cuda")
         wkv.wkv6_short_conv_prefill(self.B, self.T, self.D, self.W, self.rows, self.x, self.stride, self.w, self.bias, int(self.silu), self.offsets,

@@ -188,6 +188,64 @@ def test_workspace_sizes():
         assert fore(B, T, D, N) % 16 == 0 and back(B, T, D, N, B * T) % 16 == 0
 
 
+# ---------------------------------------------------------------------------------------------- launches
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    return lu.build_fake(tmp_path_factory.mktemp("fake_hip"))
+
+
+def scan_call(B, T, D, N, rows=None, dtype=BF16, out=BF16, space=BIG, gate=True):
+    inputs = [lu.at(0), D, lu.at(1), D, lu.at(2), 1, lu.at(3), lu.at(4), lu.at(5), N, lu.at(6), lu.at(7) if gate else None, D]
+    return ("wkv6_selective_scan_prefill", [B, T, D, N, B * T if rows is None else rows, *inputs, None if rows is None else lu.at(8), lu.at(9), lu.at(10), lu.at(11),
+                                            dtype, out, lu.at(12), space, None])
+
+
+def back_call(B, T, D, N, rows=None, dtype=BF16, space=BIG, weights=True):
+    inputs = [lu.at(0), D, lu.at(1), D, lu.at(2), 1, lu.at(3), lu.at(4), lu.at(5), N, lu.at(6), lu.at(7), D]
+    w = [lu.at(20 + i) if weights else None for i in range(3)]
+    return ("wkv6_selective_scan_backward", [B, T, D, N, B * T if rows is None else rows, *inputs, None if rows is None else lu.at(8), lu.at(9), lu.at(10), lu.at(11),
+                                             *(lu.at(13 + i) for i in range(5)), *w, lu.at(18), dtype, lu.at(12), space, None])
+
+
+def conv_back_call(B, T, D, W, rows=None, dtype=BF16, space=BIG, weights=True):
+    return ("wkv6_short_conv_backward", [B, T, D, W, B * T if rows is None else rows, lu.at(0), D, lu.at(1), lu.at(2), 1, None if rows is None else lu.at(3), lu.at(4),
+                                         lu.at(5), lu.at(6), lu.at(7), lu.at(8) if weights else None, lu.at(9) if weights else None, lu.at(10), dtype, lu.at(11), space, None])
+
+
+def test_launches(fake):
+    """Pieces only where compute units would idle, or one long sequence would go on alone."""
+    calls = [scan_call(8, 4096, 4096, 16), scan_call(1, 4096, 2048, 16), scan_call(1, 20, 64, 16), scan_call(37, 2011, 1536, 16, rows=13900),
+             scan_call(8, 4096, 4096, 16, rows=32768), scan_call(2, 0, 64, 8), back_call(8, 2048, 4096, 16), back_call(1, 4096, 2048, 16),
+             back_call(1, 20, 64, 64, weights=False), back_call(2, 0, 64, 8), conv_back_call(2, 9, 64, 4), conv_back_call(2, 9, 64, 2, weights=False),
+             conv_back_call(2, 0, 64, 3)]
+    got = [[e for e in ev if e.kind == "launch"] for ev in lu.events(fake, calls)]
+    assert [[e.base for e in ev] for ev in got] == [
+        ["scan_kernel"], ["scan_pieces_kernel", "scan_kernel"], ["scan_kernel"], ["scan_pieces_kernel", "scan_kernel"], ["scan_kernel"], ["scan_kernel"],
+        ["scan_backward_kernel", "scan_rows_kernel", "scan_weights_kernel"],
+        ["scan_pieces_kernel", "scan_backward_kernel", "scan_rows_kernel", "scan_weights_kernel"], ["scan_backward_kernel", "scan_rows_kernel"],
+        ["scan_backward_kernel", "scan_weights_kernel"], ["conv_backward_kernel", "conv_fold_kernel"], ["conv_backward_kernel"],
+        ["conv_backward_kernel", "conv_fold_kernel"]]
+    assert got[0][0].grid[0] == 512 and got[0][0].block == 256 and got[6][0].grid[0] == 512
+    # nothing to add up: the folds alone
+    none = [back_call(0, 5, 64, 16), conv_back_call(0, 5, 64, 4)]
+    assert [[e.base for e in ev if e.kind == "launch"] for ev in lu.events(fake, none)] == [["scan_weights_kernel"], ["conv_fold_kernel"]]
+
+
+def test_workspace_holds_whatever_the_lengths_are(fake):
+    rng = np.random.default_rng(5)
+    calls = []
+    for _ in range(150):
+        B, D, T, N = int(rng.integers(1, 60)), 8 * int(rng.integers(1, 300)), int(2 ** rng.uniform(0, 14)), int(rng.choice([8, 16, 32, 64]))
+        rows, dtype = int(rng.integers(0, B * T + 100)), int(rng.integers(0, 2))
+        for n in (None, rows, T):
+            calls.append(scan_call(B, T, D, N, n, dtype, dtype, wkv.wkv6_selective_scan_workspace_bytes(B, T, D, N)))
+            m = B * T if n is None else n
+            calls.append(back_call(B, T, D, N, n, dtype, wkv.wkv6_selective_scan_backward_workspace_bytes(B, T, D, N, m)))
+            calls.append(conv_back_call(B, T, D, 4, n, dtype, wkv.wkv6_short_conv_backward_workspace_bytes(B, T, D, 4, m)))
+    for ev in lu.events(fake, calls):
+        assert [e for e in ev if e.kind == "launch"]
+
+
 # ---------------------------------------------------------------------------------------------- oracles
 def _call(rng, rows, spans, D=3, N=4, **over):
     return {**dict(x=rng.standard_normal((rows, D)), delta=rng.standard_normal((rows, D)), a=-rng.random((D, N)), b=rng.standard_normal((rows, N)),
