@@ -30,7 +30,8 @@
  * dtype is the wkv6_dtype of x, delta, z, b, c (and, of the backward call, dout, dx, ddelta, dz, db, dc), out_dtype that of out: bf16 rows with
  * either, fp32 rows with fp32.
  *
- * Arithmetic: fp32 throughout, one rounding of the results.  Values have to be finite: a NaN or infinity in a row reaches other tokens of its
+ * Arithmetic: fp32 throughout, one rounding of the results.  A decay is rounded to fp32 token by token, as the recurrence is written: a state that
+ * remembers M tokens is off by up to M times 2^-24 of itself (where all its tokens have the same step size; by the root of M where they differ).  Values have to be finite: a NaN or infinity in a row reaches other tokens of its
  * sequence, also earlier ones, not other sequences.
  *
  * Workspace: device memory of the caller, 16-byte aligned, as many bytes as the function beside the call says (none where that is 0),
@@ -70,6 +71,7 @@ int wkv6_selective_scan_decode(int B, int D, int N,
 /*
  * Gradients of a prefill: from dout and dstate_out (NULL means zero) those of its inputs.  States and read-outs are formed again from the
  * inputs; nothing has to be kept from the forward call.
+ *   rows      fewer than 2^26
  *   dx, ddelta, db, dc, dz          rows (dz only if there is a z; NULL there: not written)
  *   da [D][N], dskip, ddelta_bias [D] fp32: sums over all tokens; each may be NULL (not written).  Without tokens they are nought.
  *   dstate_in [B][D][N] fp32, may be NULL

@@ -28,8 +28,8 @@ struct ScanArgs {
 //
 // By what a call is modelled to take, in microseconds: a chunk takes a workgroup `alone` if it has a compute unit to itself, and `share` of
 // a unit that is full; the pieces' own states cost three quarters of the walk itself (of gradients, both ways, two fifths), and every piece adds
-// up what the pieces in front of it leave.  Measured, whole and cut: 4 x 4096 x 4096 430 and 394 us, 5 x 4096 x 4096 456 and 498, 8 x 4096 x 4096 459 and 776,
-// 1 x 512 x 1024 33 and 13.4; gradients of 4 x 2048 x 4096 757 and 703, 8 x 2048 x 4096 937 and 1350.
+// up what the pieces in front of it leave.  Measured, whole and cut: 4 x 4096 x 4096 361 and 394 us, 5 x 4096 x 4096 454 and 498, 8 x 4096 x 4096 459 and 776,
+// 1 x 300 x 4096 33 and 19; gradients of 4 x 2048 x 4096 757 and 607, 8 x 2048 x 4096 937 and 1350; 37 packed requests of up to 2011 x 1536 208 and 171.
 struct ScanPlan {
     int segs, seg_len;
 };

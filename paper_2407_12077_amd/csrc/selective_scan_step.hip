@@ -1,4 +1,7 @@
 // The selective scan for one token of every sequence: h = exp(dt a) h_in + dt x b,  out = (sum_n c[n] h[n] + skip x) silu(z).
+//
+// Bound by the states, which are read and written once, past the caches: 1024 x 4096 channels of 16 states 106 us, 5.4 TB/s (a large copy: 5.2).  A lane has
+// four states, so a load takes whole lines; what the lanes of a channel have in common each forms for itself.  One sequence: 3 us, a launch.
 #include "selective_scan_tiles.h"
 
 namespace wkv6 {

@@ -1,4 +1,5 @@
-// What the kernels of the selective scan share: rows as they lie in memory, step sizes, gates, the rows of a workgroup.
+// What the kernels of the selective scan and of the short convolution share: rows as they lie in memory, step sizes, gates, the rows of a workgroup,
+// and the matrix cores' outer products with read-outs beside them.
 #pragma once
 #include "selective_scan.h"
 #include "wkv6_math.h"
@@ -11,11 +12,14 @@ namespace scan {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned uint2v __attribute__((ext_vector_type(2)));
 typedef unsigned uint4v __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ unsigned bf16_of(float v) { return __builtin_bit_cast(unsigned short, static_cast<__bf16>(v)); }
-__device__ __forceinline__ unsigned bf16_pair(float a, float b) { return bf16_of(a) | bf16_of(b) << 16; }
+__device__ __forceinline__ unsigned bf16_pair(float a, float b) {
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((float2v{a, b}), bf16x2));     // (one instruction)
+}
 
 // kCount consecutive values of a row, as they lie in memory; none: zeros.
 template <bool kF32, int kCount>
@@ -132,6 +136,7 @@ __device__ __forceinline__ float softplus_of(float v) {
     const float e = __builtin_amdgcn_exp2f(-fabsf(v) * kLog2e), u = 1.f + e;
     return fmaxf(v, 0.f) + __builtin_fmaf(__builtin_amdgcn_logf(u), 0.6931471805599453f, e - (u - 1.f));
 }
+// (1 / (1 + inf) is nought, so that values far below nought need no care)
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
 __device__ __forceinline__ float step_of(float v, bool softplus) { return softplus ? softplus_of(v) : v; }
 
@@ -142,7 +147,8 @@ __device__ __forceinline__ unsigned softplus_bits(bool softplus) {
     return bits;
 }
 __device__ __forceinline__ float chosen(unsigned bits, float yes, float no) {
-    return __uint_as_float((__float_as_uint(yes) & bits) | (__float_as_uint(no) & ~bits));
+    const unsigned y = __float_as_uint(yes), n = __float_as_uint(no);
+    return __uint_as_float(((y ^ n) & bits) ^ n);              // (one instruction)
 }
 template <bool kF32, int kCount>
 __device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const float (&bias)[kCount], unsigned softplus, float (&dt)[kCount]) {
@@ -153,13 +159,15 @@ __device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const f
     }
 }
 
-// A sequence's first row, and its tokens.
-__device__ __forceinline__ long long first_row_of(const ScanArgs& a, int b) {
+// A sequence's first row, and its tokens; Args has B, T, rows and offsets.
+template <typename Args>
+__device__ __forceinline__ long long first_row_of(const Args& a, int b) {
     if (!a.offsets) return static_cast<long long>(b) * a.T;
     const long long f = a.offsets[b];
     return f < 0 ? 0 : f > a.rows ? a.rows : f;
 }
-__device__ __forceinline__ int tokens_of(const ScanArgs& a, int b) {
+template <typename Args>
+__device__ __forceinline__ int tokens_of(const Args& a, int b) {
     if (!a.offsets) return a.T;
     const long long e = a.offsets[b + 1], len = (e < 0 ? 0 : e > a.rows ? a.rows : e) - first_row_of(a, b);
     return static_cast<int>(len < 0 ? 0 : len > a.T ? a.T : len);

@@ -3,8 +3,11 @@
 //     p_t = bias + sum_j w[j] x_{t-W+1+j}    out = silu(p)
 //     dp_t = dout_t silu'(p_t)    dx_s = sum_j w[j] dp_{s+W-1-j}    dw[j] = sum_t dp_t x_{t-W+1+j}    dbias = sum_t dp_t
 //
-// A thread has eight channels of a run of tokens and keeps the inputs under its taps in registers, so a row is read once, but for the W - 1 rows
-// in front of a run (and behind it, of the gradients), which a neighbour reads too.
+// Bound by memory.  A thread has four channels (eight of a single token) of a run of 16 tokens (32 of the gradients) and keeps the inputs under its
+// taps in registers, so a row is read once, but for the W - 1 rows in front of a run (and behind it, of the gradients), which a neighbour in the same
+// workgroup reads too.  8 x 4096 x 4096 bf16, W = 4: 114 us, 4.7 TB/s (a large copy: 5.2); eight channels a thread 118, runs of 8 or 32 tokens 128 and
+// 120, addresses by multiplication 118.  Gradients of 8 x 2048 x 4096 102 us, 4.0 TB/s, of which the fold is 5: eight channels a thread 117 (240
+// registers), runs of 16 or 64 tokens 127 and 115.  24 x 4096 single tokens 3.7 us: one launch.
 #include "short_conv.h"
 
 #include "selective_scan_tiles.h"
@@ -21,20 +24,11 @@ struct Place {
 // Tokens first .. end - 1 of sequence b for slice `slice` of segment `seg`.
 __device__ __forceinline__ Place place_of(const ConvArgs& a, int b, int seg, int slice, int run) {
     Place p;
-    long long lo = static_cast<long long>(b) * a.T, len = a.T;
-    if (a.offsets) {
-        long long f = a.offsets[b], e = a.offsets[b + 1];
-        f = f < 0 ? 0 : f > a.rows ? a.rows : f;
-        e = e < 0 ? 0 : e > a.rows ? a.rows : e;
-        len = e - f;
-        len = len < 0 ? 0 : len > a.T ? a.T : len;
-        lo = f;
-    }
-    p.row0 = lo;
-    p.len = static_cast<int>(len);
+    p.row0 = first_row_of(a, b);
+    p.len = tokens_of(a, b);
     const long long first = static_cast<long long>(seg) * a.seg_len + slice * run, end = first + run;
-    p.first = static_cast<int>(first < len ? first : len);
-    p.end = static_cast<int>(end < len ? end : len);
+    p.first = static_cast<int>(first < p.len ? first : p.len);
+    p.end = static_cast<int>(end < p.len ? end : p.len);
     return p;
 }
 
@@ -175,7 +169,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvArgs a, cha
 // b has, so no two places meet, and there are rows / seg_len + B of them.  Those that no segment has are set to nought by the last segment in front
 // of them (in front of all: by the first sequence's), so that the fold adds all places without asking whose they are.
 __device__ __forceinline__ long long first_place(const ConvArgs& a, int b) {
-    return static_cast<long long>(static_cast<unsigned>(place_of(a, b, 0, 0, 1).row0) / static_cast<unsigned>(a.seg_len)) + b;     // (fewer than 2^31 rows)
+    return static_cast<long long>(static_cast<unsigned>(first_row_of(a, b)) / static_cast<unsigned>(a.seg_len)) + b;     // (fewer than 2^31 rows)
 }
 
 template <int W, bool kF32, int kG>
@@ -218,7 +212,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
         }
         // Behind this thread's own tokens W - 1 more, whose dp its last inputs have a share in.
         const int stop = p.first + (p.end - p.first) + W - 1;
-        constexpr int kBatch = 4;
+        constexpr int kBatch = 2;
         Row<kF32, kG> xs[2][kBatch], ds[2][kBatch];
         auto ask = [&](int t, int which) {
 #pragma unroll
