@@ -15,7 +15,8 @@
  *   out, dout     [rows][D]
  * Device pointers, 16-byte aligned but for offsets (4); out and the gradients must not alias any input or each other.  dtype: the wkv6_dtype of all but
  * w, bias, dw, dbias.  fp32 arithmetic, one rounding of the results; states are kept as they are.  A NaN or infinity in a row
- * reaches only the tokens that have it under their taps (of the gradients also dw and dbias of its channel).
+ * reaches, of its own channel, only the tokens that have it under their taps; of the gradients dx (and dstate_in) of the W - 1 tokens in front of it
+ * and behind it, dw and dbias.
  * Workspace, ownership, streams, errors before any launch: as in wkv6_selective_scan.h.
  */
 #ifndef WKV6_SHORT_CONV_H

@@ -20,7 +20,8 @@ using namespace scan;
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Sums over lanes: two values become one register with half of the lanes' sums each.  halves<32>: lanes below 32 have p's, the others q's.
+// Sums over lanes: two values become one register with half of the lanes' sums each.  halves<32>: lanes below 32 have p's, the others q's; and so
+// on inside the halves.
 template <int kBy>
 __device__ __forceinline__ float halves(float p, float q, int lane) {
     if constexpr (kBy == 32 || kBy == 16) {
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     constexpr int kG = S::kGroups, kWaves = S::kWaves, kC = S::kC, kCh = kScanChannels, kPer = S::kPer, kItem = kF32 ? 4 : 2;
     __shared__ float2v step[2][kC][kCh];                       // dt, dt x
     __shared__ float grad_out[2][kC][kCh];                     // dy
-    __shared__ float part[kGate ? 3 : 2][kWaves][kC][kCh];                 // shares of g, of sum k rate, of the read-outs
+    __shared__ float part[kGate ? 3 : 2][kWaves][kC][kCh];     // shares of g, of sum k rate, of the read-outs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = blockIdx.x % blocks, at = blockIdx.x / blocks, b = at % a.B, seg = at / a.B;
     const Span span = span_of(a, b, seg);
@@ -70,6 +71,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
             else if (a.state_in) h[q] = *reinterpret_cast<const float4v*>(a.state_in + unit + 4 * q);
             if (r.dstate_out) grad[q] = *reinterpret_cast<const float4v*>(r.dstate_out + unit + 4 * q);
         }
+#pragma unroll 4
         for (int s = 1; s <= seg; ++s) {
             const float sum = a.locals[sums_at + s * seg_sums + channel];
 #pragma unroll
@@ -79,9 +81,9 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
                 for (int i = 0; i < 4; ++i) h[q][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(sum * rate[q][i]), h[q][i], local[i]);
             }
         }
-        if (a.segs > 1 && !span.last) {
-            for (int s = a.segs - 1; s > seg; --s) {
-                if (span_of(a, b, s).tokens == 0) continue;
+        if (!span.last) {
+#pragma unroll 4
+            for (int s = (tokens_of(a, b) - 1) / a.seg_len; s > seg; --s) {
                 const float sum = r.behind[sums_at + s * seg_sums + channel];
 #pragma unroll
                 for (int q = 0; q < kG; ++q) {
@@ -449,8 +451,7 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
         if (err != hipSuccess) return err;
     }
     const auto kernel = a.z ? &scan_backward_kernel<N, kF32, true> : &scan_backward_kernel<N, kF32, false>;
-    hipLaunchKernelGGL(kernel, dim3(units * a.segs), dim3(Shape<N>::kThreads), 0,
-                       stream, a, g, blocks);
+    hipLaunchKernelGGL(kernel, dim3(units * a.segs), dim3(Shape<N>::kThreads), 0, stream, a, g, blocks);
     if ((err = hipGetLastError()) != hipSuccess) return err;
     if (a.rows > 0 && a.T > 0) {
         hipLaunchKernelGGL((scan_rows_kernel<N, kF32>), dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, stream, a, g.rows,

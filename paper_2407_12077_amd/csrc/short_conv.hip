@@ -88,9 +88,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvArgs a, char* ou
                 if (t >= 0) last[j].raw.load(x + t * a.x_row);
             }
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) {
-                last[j].raw.put(state_out + state_at + j * state_row);
-            }
+            for (int j = 0; j < W - 1; ++j) last[j].raw.put(state_out + state_at + j * state_row);
         }
     } else {
 #pragma unroll
@@ -160,9 +158,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvArgs a, cha
     store<kF32>(out + b * row + ch * kItem, y);
     if (!state_out) return;
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-        in[j + 1].raw.put(state_out + state_at + j * row);
-    }
+    for (int j = 0; j < W - 1; ++j) in[j + 1].raw.put(state_out + state_at + j * row);
 }
 
 // Where the first segment of sequence b leaves its sums, the others behind it: a segment of sequence b + 1 starts at least as many rows later as
@@ -211,7 +207,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
             r.get(win[j + 1]);
         }
         // Behind this thread's own tokens W - 1 more, whose dp its last inputs have a share in.
-        const int stop = p.first + (p.end - p.first) + W - 1;
+        const int stop = p.end + W - 1;
         constexpr int kBatch = 2;
         Row<kF32, kG> xs[2][kBatch], ds[2][kBatch];
         auto ask = [&](int t, int which) {
@@ -363,9 +359,14 @@ ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward) {
     const int slices = kConvThreads / p.lanes, across = (groups + p.lanes - 1) / p.lanes;
     int run = backward ? 32 : 16;
     while (run > 4 && rows * across / (slices * run) < 1024) run /= 2;
-    p.seg_len = slices * run;
-    p.segs = T > 0 ? (T - 1) / p.seg_len + 1 : 1;
-    p.workgroups = static_cast<long long>(p.segs) * B * across;
+    // A launch has places for B sequences of T tokens; where packed ones are mostly shorter, longer runs keep the empty workgroups from taking longer than the
+    // others: not more than sixteen for one that has work.
+    for (;; run *= 2) {
+        p.seg_len = slices * run;
+        p.segs = T > 0 ? (T - 1) / p.seg_len + 1 : 1;
+        p.workgroups = static_cast<long long>(p.segs) * B * across;
+        if (p.segs == 1 || p.workgroups <= 65536 || p.workgroups <= 16 * (rows / p.seg_len + B) * across) break;
+    }
     return p;
 }
 

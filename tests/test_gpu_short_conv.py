@@ -77,3 +77,28 @@ def test_nan_stays_under_its_taps(gpu_device):
     c.x[49, 3] = float("nan")
     out, _ = c.prefill()
     assert out[49, 3].isnan() and torch.equal(out[50:], clean[50:]) and torch.equal(out[:49], clean[:49])
+
+
+@pytest.mark.parametrize("where", ["x", "dout"])
+def test_nan_stays_under_its_taps_in_gradients(gpu_device, where):
+    c = Conv(9, D=64, W=4, lengths=[300, 50])
+    clean = c.backward()
+    for row in (150, 299):
+        c.x, c.dout = c.x.clone(), c.dout.clone()
+        given = getattr(c, where)
+        was = given[row, 3].clone()
+        given[row, 3] = float("nan")
+        dx, dw, dbias, ds = c.backward()
+        given[row, 3] = was
+        near = torch.zeros_like(dx, dtype=torch.bool)
+        near[row - 3:min(row + 4, 300), 3] = True
+        assert dx[row, 3].isnan() and dw[3].isnan().any() and dbias[3].isnan()
+        assert torch.equal(dx[~near], clean[0][~near]) and torch.equal(ds, clean[3])
+        assert torch.equal(dw[:3], clean[1][:3]) and torch.equal(dw[4:], clean[1][4:]) and not dbias[4:].isnan().any()
+
+
+def test_many_short_sequences_where_long_ones_may_come(gpu_device):
+    """A launch has places for the longest sequence that may come: threads take more tokens one behind the other, so that most have some."""
+    c = Conv(10, D=16, W=4, lengths=[3, 1, 0, 7] * 511 + [3000, 2, 90, 1], front=1, tail=3, longest=65536)
+    c.check_prefill(*c.prefill())
+    c.check_backward(c.backward())

@@ -231,6 +231,14 @@ def test_launches(fake):
     assert [[e.base for e in ev if e.kind == "launch"] for ev in lu.events(fake, none)] == [["scan_weights_kernel"], ["conv_fold_kernel"]]
 
 
+def test_empty_workgroups_are_few(fake):
+    """Thousands of packed sequences, one of them long: a launch stays a small multiple of the work, and is not refused for its size."""
+    calls = [conv_back_call(4096, 65536, 4096, 4, rows=10 ** 6), conv_back_call(1024, 32768, 2048, 4, rows=500000), conv_back_call(8, 65536, 4096, 4, rows=8 * 65536)]
+    got = [ev[0].grid[0] for ev in lu.events(fake, calls)]
+    for n, (B, D, rows) in zip(got, ((4096, 4096, 10 ** 6), (1024, 2048, 500000), (8, 4096, 8 * 65536))):
+        assert n <= 16 * (rows // 128 + B) * D // 256
+
+
 def test_workspace_holds_whatever_the_lengths_are(fake):
     rng = np.random.default_rng(5)
     calls = []
