@@ -92,6 +92,10 @@ struct ScanCall {
     }
 };
 
+bool step_fits(int B, int D, int N) {
+    return wkv6::fits_a_launch(static_cast<long long>(B) * ((static_cast<long long>(D) * (N / 4) + 255) / 256), 256);
+}
+
 long long four(long long n) { return (n + 3) / 4 * 4; }
 
 // Workspaces in floats, every part a multiple of four; false where a launch would not fit.
@@ -206,6 +210,8 @@ int wkv6_selective_scan_prefill(int B, int T, int D, int N, long long rows, cons
     if ((status = check_workspace(workspace, workspace_bytes, 4 * s.floats)) != WKV6_OK) return status;
     wkv6::ScanArgs args = call.args(s.plan);
     args.locals = static_cast<float*>(workspace);
+    if (T > 0 && T <= wkv6::kScanFewTokens && step_fits(B, D, N))
+        return status_of(wkv6::launch_scan_step(args, out, state_out, dtype == WKV6_DTYPE_F32, out_dtype == WKV6_DTYPE_F32, static_cast<hipStream_t>(stream)));
     return status_of(wkv6::launch_scan(args, out, state_out, dtype == WKV6_DTYPE_F32, out_dtype == WKV6_DTYPE_F32, static_cast<hipStream_t>(stream)));
 }
 
@@ -220,7 +226,7 @@ int wkv6_selective_scan_decode(int B, int D, int N, const void* x, long long x_s
     if ((status = call.check_inputs()) != WKV6_OK) return status;
     if (!out) return WKV6_ERR_NULL;
     if (any_misaligned(out) || any_misaligned(state_out)) return WKV6_ERR_ALIGN;
-    if (!wkv6::fits_a_launch(static_cast<long long>(B) * ((static_cast<long long>(D) * (N / 4) + 255) / 256), 256)) return WKV6_ERR_SHAPE;
+    if (!step_fits(B, D, N)) return WKV6_ERR_SHAPE;
     return status_of(wkv6::launch_scan_step(call.args({1, 1}), out, state_out, dtype == WKV6_DTYPE_F32, out_dtype == WKV6_DTYPE_F32,
                                             static_cast<hipStream_t>(stream)));
 }

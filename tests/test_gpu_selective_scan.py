@@ -60,6 +60,28 @@ def test_single_tokens(gpu_device, B, D, N, dtype, out):
     s.check_prefill(y, h)
 
 
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (BF16, F32), (F32, F32)], ids=["bf16", "bf16-f32", "f32"])
+@pytest.mark.parametrize("N", [8, 16, 32, 64])
+@pytest.mark.parametrize("rows", [dict(B=3, T=2), dict(B=2, T=8), dict(lengths=[8, 0, 1, 5, 3, 4], front=3, tail=2), dict(lengths=[1, 0, 1], front=1),
+                                  dict(lengths=[9, 20], longest=7)], ids=str)
+def test_few_tokens(gpu_device, rows, N, dtype, out):
+    s = Scan(12, D=200, N=N, dtype=dtype, fused=True, gate=N != 32, state=N != 16, **rows)
+    s.check_prefill(*s.prefill(out))
+    if s.state_in is not None:
+        alone, want = s.prefill(out)
+        s.state_in = s.state_in.clone()
+        again, state = s.prefill(out, state_out=s.state_in)
+        assert torch.equal(again, alone) and torch.equal(state, want)
+
+
+def test_a_prompt_of_one_token_is_a_single_token(gpu_device):
+    s = Scan(13, D=136, N=16, B=4, T=1)
+    out, state = s.prefill()
+    y, h = torch.empty_like(out), torch.empty_like(state)
+    wkv.wkv6_selective_scan_decode(4, 136, 16, *s.inputs(), s.state_in, y, h, CODE[BF16], CODE[BF16])
+    assert torch.equal(out, y) and torch.equal(state, h)
+
+
 def test_states_grow(gpu_device):
     s = Scan(7, D=64, N=16, dtype=F32, B=2, T=300, growing=True)
     s.check_prefill(*s.prefill())

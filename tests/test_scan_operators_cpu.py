@@ -231,6 +231,14 @@ def test_launches(fake):
     assert [[e.base for e in ev if e.kind == "launch"] for ev in lu.events(fake, none)] == [["scan_weights_kernel"], ["conv_fold_kernel"]]
 
 
+def test_launches_of_few_tokens(fake):
+    """Up to eight tokens a sequence: no chunks."""
+    calls = [scan_call(3, 1, 4096, 64), scan_call(64, 8, 2048, 32), scan_call(64, 8, 2048, 32, rows=100), scan_call(64, 9, 2048, 32), scan_call(2, 0, 64, 8)]
+    got = [[(e.base, e.grid[0], e.block) for e in ev if e.kind == "launch"] for ev in lu.events(fake, calls)]
+    assert got == [[("scan_step_kernel", 3 * 256, 256)], [("scan_step_kernel", 64 * 64, 256)], [("scan_step_kernel", 64 * 64, 256)], [("scan_kernel", 64 * 32, 512)],
+                   [("scan_kernel", 2, 128)]]
+
+
 def test_empty_workgroups_are_few(fake):
     """Thousands of packed sequences, one of them long: a launch stays a small multiple of the work, and is not refused for its size."""
     calls = [conv_back_call(4096, 65536, 4096, 4, rows=10 ** 6), conv_back_call(1024, 32768, 2048, 4, rows=500000), conv_back_call(8, 65536, 4096, 4, rows=8 * 65536)]
