@@ -71,7 +71,7 @@ int wkv6_selective_scan_decode(int B, int D, int N,
 /*
  * Gradients of a prefill: from dout and dstate_out (NULL means zero) those of its inputs.  States and read-outs are formed again from the
  * inputs; nothing has to be kept from the forward call.
- *   rows      fewer than 2^26
+ *   rows      at most 2^26 - 16
  *   dx, ddelta, db, dc, dz          rows (dz only if there is a z; NULL there: not written)
  *   da [D][N], dskip, ddelta_bias [D] fp32: sums over all tokens; each may be NULL (not written).  Without tokens they are nought.
  *   dstate_in [B][D][N] fp32, may be NULL

@@ -110,7 +110,7 @@ bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, b
     s->locals = four(wkv6::scan_local_floats(plan, B, D, N));
     s->floats = s->locals;
     if (backward) {
-        if (!wkv6::fits_a_launch((rows + 3) / 4, 256)) return false;
+        if (!wkv6::fits_a_launch((rows + wkv6::kScanFoldRows - 1) / wkv6::kScanFoldRows, 64 * wkv6::kScanFoldRows)) return false;
         s->states = (rows / wkv6::scan_back_chunk(N) + B + 1) * D * N;
         s->rows = rows * blocks * 2 * N;
         s->weights = wkv6::scan_places(B, rows, plan.seg_len) * D * (N + 2);

@@ -47,6 +47,8 @@ constexpr int scan_threads(int N) { return 16 * N; }
 // state_out may be null.  With a.segs > 1 the segments' own states first.
 hipError_t launch_scan(const ScanArgs& a, void* out, float* state_out, bool f32_rows, bool f32_out, hipStream_t stream);
 
+constexpr int kScanFoldRows = 16;      // whose shares of db and dc a workgroup adds up, a wave each
+
 // Gradients.  Tokens whose decays and states stay in registers on the way back; the states in front of them are kept in `states`.
 constexpr int scan_back_chunk(int N) { return N == 8 || N == 64 ? 8 : 16; }
 struct ScanGradients {

@@ -221,8 +221,8 @@ def test_launches(fake):
     got = [[e for e in ev if e.kind == "launch"] for ev in lu.events(fake, calls)]
     assert [[e.base for e in ev] for ev in got] == [
         ["scan_kernel"], ["scan_pieces_kernel", "scan_kernel"], ["scan_kernel"], ["scan_pieces_kernel", "scan_kernel"], ["scan_kernel"], ["scan_kernel"],
-        ["scan_backward_kernel", "scan_rows_kernel", "scan_weights_kernel"],
-        ["scan_pieces_kernel", "scan_backward_kernel", "scan_rows_kernel", "scan_weights_kernel"], ["scan_backward_kernel", "scan_rows_kernel"],
+        ["scan_backward_kernel", "scan_folds_kernel"],
+        ["scan_pieces_kernel", "scan_backward_kernel", "scan_folds_kernel"], ["scan_backward_kernel", "scan_folds_kernel"],
         ["scan_backward_kernel", "scan_weights_kernel"], ["conv_backward_kernel", "conv_fold_kernel"], ["conv_backward_kernel"],
         ["conv_backward_kernel", "conv_fold_kernel"]]
     assert got[0][0].grid[0] == 512 and got[0][0].block == 256 and got[6][0].grid[0] == 512
@@ -237,6 +237,15 @@ def test_launches_of_few_tokens(fake):
     got = [[(e.base, e.grid[0], e.block) for e in ev if e.kind == "launch"] for ev in lu.events(fake, calls)]
     assert got == [[("scan_step_kernel", 3 * 256, 256)], [("scan_step_kernel", 64 * 64, 256)], [("scan_step_kernel", 64 * 64, 256)], [("scan_kernel", 64 * 32, 512)],
                    [("scan_kernel", 2, 128)]]
+
+
+def test_folds_of_as_many_rows_as_there_may_be(fake):
+    """One launch for both folds as long as one holds them."""
+    rows = 2 ** 26 - 16
+    fits, whole = lu.events(fake, [back_call(1, 4096, 64, 8), back_call(4096, 2 ** 14, 8, 8, rows=rows)])
+    assert [(e.base, e.grid[0], e.block) for e in fits if e.kind == "launch"][-1] == ("scan_folds_kernel", 64 * 10 // 64 + 4096 // 16, 1024)
+    assert [(e.base, e.grid[0]) for e in whole if e.kind == "launch"][-2:] == [("scan_folds_kernel", rows // 16), ("scan_weights_kernel", 2)]
+    assert [wkv.wkv6_selective_scan_backward_workspace_bytes(4096, 2 ** 14, 8, 8, n) > 0 for n in (rows, rows + 1)] == [True, False]
 
 
 def test_empty_workgroups_are_few(fake):
