@@ -50,7 +50,7 @@ __device__ __forceinline__ void walk(ScanArgs a, char* out, float* state_out, in
 
     float4v rate = {0.f, 0.f, 0.f, 0.f}, h = {0.f, 0.f, 0.f, 0.f};
     if (mine) {
-        rate = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0) * kLog2e;
+        rate = rate_of(a.a + static_cast<long long>(ch) * N + n0);
         if (!kStates && a.segs > 1) {
             h = *reinterpret_cast<const float4v*>(a.locals + unit);
 #pragma unroll 4
@@ -185,7 +185,7 @@ __device__ __forceinline__ void walk_behind(const ScanArgs& a, const char* dout,
     const int D = a.D, c0 = block * kCh, ch = c0 + lane, n0 = 4 * wave;
     const bool mine = ch < D;
     float4v rate = {0.f, 0.f, 0.f, 0.f}, g = {0.f, 0.f, 0.f, 0.f};
-    if (mine) rate = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0) * kLog2e;
+    if (mine) rate = rate_of(a.a + static_cast<long long>(ch) * N + n0);
     const int token = threadIdx.x / kAcross, own = c0 + threadIdx.x % kAcross * kPer, in_block = own - c0;
     const bool there = own < D;
     const unsigned softplus = softplus_bits(a.softplus);

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     if (mine) {
 #pragma unroll
         for (int q = 0; q < kG; ++q) {
-            rate[q] = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0 + 4 * q) * kLog2e;
+            rate[q] = rate_of(a.a + static_cast<long long>(ch) * N + n0 + 4 * q);
             if (a.segs > 1) h[q] = *reinterpret_cast<const float4v*>(a.locals + unit + 4 * q);
             else if (a.state_in) h[q] = *reinterpret_cast<const float4v*>(a.state_in + unit + 4 * q);
             if (r.dstate_out) grad[q] = *reinterpret_cast<const float4v*>(r.dstate_out + unit + 4 * q);

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, void* out, f
     const int tokens = kAtOnce == 1 ? 1 : tokens_of(a, b);
     float4v h = {0.f, 0.f, 0.f, 0.f};
     if (a.state_in) h = __builtin_nontemporal_load(reinterpret_cast<const float4v*>(a.state_in + unit));
-    const float4v rate = *reinterpret_cast<const float4v*>(a.a + static_cast<long long>(ch) * N + n0) * kLog2e;
+    const float4v rate = rate_of(a.a + static_cast<long long>(ch) * N + n0);
     const float bias = a.bias ? a.bias[ch] : 0.f, skip = a.skip ? a.skip[ch] : 0.f;
     for (int t = 0; t < tokens; t += kAtOnce) {
         Raw<kF32, 1> x[kAtOnce], delta[kAtOnce], z[kAtOnce];

@@ -82,6 +82,15 @@ def test_a_prompt_of_one_token_is_a_single_token(gpu_device):
     assert torch.equal(out, y) and torch.equal(state, h)
 
 
+@pytest.mark.parametrize("T", [5, 19, 700])
+def test_states_of_one_token(gpu_device, T):
+    """a as low as fp32 goes: a state forgets everything, and the rows behind a sequence's end change nothing."""
+    s = Scan(14, D=72, N=16, dtype=F32, lengths=[T, 3, 0])
+    s.a[:, 1] = s.a[5] = -torch.finfo(F32).max
+    s.check_prefill(*s.prefill())
+    s.check_backward(s.backward())
+
+
 def test_states_grow(gpu_device):
     s = Scan(7, D=64, N=16, dtype=F32, B=2, T=300, growing=True)
     s.check_prefill(*s.prefill())
