@@ -138,11 +138,12 @@ __device__ __forceinline__ float softplus_of(float v) {
 }
 // (1 / (1 + inf) is nought, so that values far below nought need no care)
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-v * kLog2e)); }
-// a log2(e) of four states, finite: a step size of nought (behind a sequence's end too) leaves a state as it is, whatever a
+// a log2(e) of four states, no infinity: a step size of nought (behind a sequence's end too) leaves a state as it is, however large a.  By comparisons, as
+// minima, maxima and medians take the other operand for a NaN, and a weight that is none has to show.
 __device__ __forceinline__ float4v rate_of(const float* a) {
     float4v rate = *reinterpret_cast<const float4v*>(a) * kLog2e;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) rate[i] = __builtin_amdgcn_fmed3f(rate[i], -__FLT_MAX__, __FLT_MAX__);
+    for (int i = 0; i < 4; ++i) rate[i] = rate[i] < -__FLT_MAX__ ? -__FLT_MAX__ : rate[i] > __FLT_MAX__ ? __FLT_MAX__ : rate[i];
     return rate;
 }
 __device__ __forceinline__ float step_of(float v, bool softplus) { return softplus ? softplus_of(v) : v; }

@@ -1,0 +1,47 @@
+"""Calls of the selective scan and the short convolution at the edges of what their headers allow, on the GPU."""
+import pytest
+import torch
+
+import paper_2407_12077_amd as wkv
+from scan_util import BF16, CODE, F32, Scan
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("N", [8, 16, 32, 64])
+@pytest.mark.parametrize("T", [1, 5, 19, 700])
+def test_a_weight_that_is_no_number_shows(gpu_device, T, N):
+    """A NaN in a[d][n] reaches channel d's read-outs and state n, its da and the gradients of its rows; other channels keep their bits."""
+    s, d, n = Scan(1, D=72, N=N, lengths=[T, 3, 0]), 5, N - 1
+    rows, others = slice(0, T + 3), [i for i in range(72) if i != d]
+    clean_out, clean_state = s.prefill()
+    clean = s.backward()
+    s.a[d, n] = float("nan")
+    out, state = s.prefill()
+    assert bool(out[rows, d].isnan().all()) and torch.equal(out[:, others], clean_out[:, others])
+    assert bool(state[:2, d, n].isnan().all())
+    state[:2, d, n] = clean_state[:2, d, n]
+    assert torch.equal(state, clean_state)                     # the sequence of no tokens among them
+    g = s.backward()
+    assert bool(g["da"][d, n].isnan()) and torch.equal(g["da"][others], clean["da"][others])
+    assert bool(g["ddelta"][rows, d].isnan().all()) and bool(g["dbias"][d].isnan()) and bool(g["dstate_in"][:2, d, n].isnan().all())
+    for name in ("dx", "ddelta", "dz"):
+        assert torch.equal(g[name][:, others], clean[name][:, others])
+    assert torch.equal(g["dstate_in"][2], clean["dstate_in"][2])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("N", [8, 16, 32, 64])
+def test_a_weight_that_is_no_number_shows_in_single_tokens(gpu_device, N, dtype):
+    s = Scan(2, D=72, N=N, dtype=dtype, B=3, T=1)
+    results = []
+    for value in (None, float("nan")):
+        if value is not None:
+            s.a[7, 2] = value
+        out, state = s.blank(72, dtype), torch.empty_like(s.state_in)
+        wkv.wkv6_selective_scan_decode(3, 72, N, *s.inputs(), s.state_in, out, state, CODE[dtype], CODE[dtype])
+        results.append((out, state))
+    (clean_out, clean_state), (out, state) = results
+    assert bool(out[:, 7].isnan().all()) and bool(state[:, 7, 2].isnan().all())
+    out[:, 7], state[:, 7, 2] = clean_out[:, 7], clean_state[:, 7, 2]
+    assert torch.equal(out, clean_out) and torch.equal(state, clean_state)
