@@ -22,8 +22,9 @@
  *   x, delta, z   [rows][D], rows x_stride, delta_stride, z_stride ELEMENTS apart (at least D, at most 2^22, a multiple of 16 bytes), so that they may be
  *                 parts of a projection's rows.  z may be NULL: no gate.  dx, ddelta, dz likewise, with the same strides
  *   b, c          [rows][N], rows bc_stride elements apart (at least N, at most 2^22, a multiple of 16 bytes).  db, dc likewise
- *   a             [D][N] fp32: negative numbers as a rule; positive ones (states grow) are taken as they are, as far as states stay inside fp32's range; an infinity counts
- *                 as fp32's largest number, a NaN reaches all that its state has a part in
+ *   a             [D][N] fp32: negative numbers as a rule; positive ones (states grow) are taken as they are, as far as a token's exp(dt a), states (and, of the
+ *                 backward call, their gradients) and what each token leaves in them stay inside fp32's range; an infinity counts as fp32's largest number,
+ *                 a NaN reaches all that its state has a part in
  *   delta_bias, skip   [D] fp32, may be NULL (nought)
  *   state_in      [B][D][N] fp32, NULL means zero.  state_out the same, NULL means "do not write"; it may equal state_in
  *   out, dout     [rows][D]

@@ -53,13 +53,14 @@ __device__ __forceinline__ void walk(ScanArgs a, char* out, float* state_out, in
         rate = rate_of(a.a + static_cast<long long>(ch) * N + n0);
         if (!kStates && a.segs > 1) {
             h = *reinterpret_cast<const float4v*>(a.locals + unit);
+            auto pieces_in_front = [&](auto grows) {
 #pragma unroll 4
-            for (int q = 1; q <= seg; ++q) {
-                const float sum = a.locals[sums_at + q * seg_sums + static_cast<long long>(b) * D + ch];
-                const float4v local = *reinterpret_cast<const float4v*>(a.locals + q * seg_states + unit);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) h[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(sum * rate[i]), h[i], local[i]);
-            }
+                for (int q = 1; q <= seg; ++q)
+                    pass_on<decltype(grows)::value>(h, a.locals[sums_at + q * seg_sums + static_cast<long long>(b) * D + ch], rate,
+                                                    *reinterpret_cast<const float4v*>(a.locals + q * seg_states + unit));
+            };
+            if (may_grow(rate, a.softplus)) pieces_in_front(std::true_type());
+            else pieces_in_front(std::false_type());
         } else if (!kStates && a.state_in) {
             h = *reinterpret_cast<const float4v*>(a.state_in + unit);
         }

@@ -71,28 +71,26 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
             else if (a.state_in) h[q] = *reinterpret_cast<const float4v*>(a.state_in + unit + 4 * q);
             if (r.dstate_out) grad[q] = *reinterpret_cast<const float4v*>(r.dstate_out + unit + 4 * q);
         }
+        auto pieces_around = [&](auto grows) {
+            constexpr bool kGrows = decltype(grows)::value;
 #pragma unroll 4
-        for (int s = 1; s <= seg; ++s) {
-            const float sum = a.locals[sums_at + s * seg_sums + channel];
+            for (int s = 1; s <= seg; ++s) {
+                const float sum = a.locals[sums_at + s * seg_sums + channel];
 #pragma unroll
-            for (int q = 0; q < kG; ++q) {
-                const float4v local = *reinterpret_cast<const float4v*>(a.locals + s * seg_states + unit + 4 * q);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) h[q][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(sum * rate[q][i]), h[q][i], local[i]);
+                for (int q = 0; q < kG; ++q) pass_on<kGrows>(h[q], sum, rate[q], *reinterpret_cast<const float4v*>(a.locals + s * seg_states + unit + 4 * q));
             }
-        }
-        if (!span.last) {
+            if (span.last) return;
 #pragma unroll 4
             for (int s = (tokens_of(a, b) - 1) / a.seg_len; s > seg; --s) {
                 const float sum = r.behind[sums_at + s * seg_sums + channel];
 #pragma unroll
-                for (int q = 0; q < kG; ++q) {
-                    const float4v local = *reinterpret_cast<const float4v*>(r.behind + s * seg_states + unit + 4 * q);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) grad[q][i] = __builtin_fmaf(__builtin_amdgcn_exp2f(sum * rate[q][i]), grad[q][i], local[i]);
-                }
+                for (int q = 0; q < kG; ++q) pass_on<kGrows>(grad[q], sum, rate[q], *reinterpret_cast<const float4v*>(r.behind + s * seg_states + unit + 4 * q));
             }
-        }
+        };
+        bool grows = may_grow(rate[0], a.softplus);
+        if constexpr (kG > 1) grows = grows || may_grow(rate[1], a.softplus);
+        if (grows) pieces_around(std::true_type());
+        else pieces_around(std::false_type());
     }
 
     const int token = threadIdx.x / S::kAcross, own = c0 + threadIdx.x % S::kAcross * kPer, in_block = own - c0;

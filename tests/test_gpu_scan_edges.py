@@ -45,3 +45,25 @@ def test_a_weight_that_is_no_number_shows_in_single_tokens(gpu_device, N, dtype)
     assert bool(out[:, 7].isnan().all()) and bool(state[:, 7, 2].isnan().all())
     out[:, 7], state[:, 7, 2] = clean_out[:, 7], clean_state[:, 7, 2]
     assert torch.equal(out, clean_out) and torch.equal(state, clean_state)
+
+
+@pytest.mark.parametrize("N", [8, 16, 32, 64])
+@pytest.mark.parametrize("rows", [dict(B=1, T=700), dict(lengths=[3, 700, 40], front=1)], ids=str)
+@pytest.mark.parametrize("state", ["nought", "small"])
+def test_a_piece_may_grow_more_than_fp32_holds(gpu_device, state, rows, N):
+    """Every other state grows, over 32 tokens by more than fp32's largest number (exp(7) a token, or exp(2.9)), but from nought, or from 1e-25 to 1e16, and no gradient comes
+    from there: whatever pieces the tokens are cut into, states and gradients are as token by token, within the bounds for growing states (scan_util)."""
+    s = Scan(3, D=72, N=N, dtype=F32, softplus=False, bias=False, state=False, gate=True, **rows)
+    s.scale = 4                                                # as for `growing`
+    first, end = max(s.spans, key=lambda span: span[1] - span[0])
+    s.a[:, ::2] = 0.70 + 0.04 * torch.rand(72, N // 2, device="cuda")
+    grows = slice(first + 320, first + 352)
+    s.delta[:] = 0.02
+    s.delta[grows] = 10.0 if state == "nought" else 4.0
+    if state == "nought":
+        s.x[first:first + 352] = 0
+    else:
+        s.x *= 1e-25
+    s.dout[first + 320:end] = 0
+    s.check_prefill(*s.prefill())
+    s.check_backward(s.backward())
