@@ -53,14 +53,11 @@ __device__ __forceinline__ void walk(ScanArgs a, char* out, float* state_out, in
         rate = rate_of(a.a + static_cast<long long>(ch) * N + n0);
         if (!kStates && a.segs > 1) {
             h = *reinterpret_cast<const float4v*>(a.locals + unit);
-            auto pieces_in_front = [&](auto grows) {
+            const float4v third = rate * (1.f / 3);
 #pragma unroll 4
-                for (int q = 1; q <= seg; ++q)
-                    pass_on<decltype(grows)::value>(h, a.locals[sums_at + q * seg_sums + static_cast<long long>(b) * D + ch], rate,
-                                                    *reinterpret_cast<const float4v*>(a.locals + q * seg_states + unit));
-            };
-            if (may_grow(rate, a.softplus)) pieces_in_front(std::true_type());
-            else pieces_in_front(std::false_type());
+            for (int q = 1; q <= seg; ++q)
+                pass_on(h, a.locals[sums_at + q * seg_sums + static_cast<long long>(b) * D + ch], third,
+                        *reinterpret_cast<const float4v*>(a.locals + q * seg_states + unit));
         } else if (!kStates && a.state_in) {
             h = *reinterpret_cast<const float4v*>(a.state_in + unit);
         }

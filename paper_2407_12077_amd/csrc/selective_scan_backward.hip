@@ -64,33 +64,29 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
 #pragma unroll
     for (int q = 0; q < kG; ++q) rate[q] = h[q] = grad[q] = da[q] = float4v{0.f, 0.f, 0.f, 0.f};
     if (mine) {
+        float4v third[kG];
 #pragma unroll
         for (int q = 0; q < kG; ++q) {
             rate[q] = rate_of(a.a + static_cast<long long>(ch) * N + n0 + 4 * q);
+            third[q] = rate[q] * (1.f / 3);
             if (a.segs > 1) h[q] = *reinterpret_cast<const float4v*>(a.locals + unit + 4 * q);
             else if (a.state_in) h[q] = *reinterpret_cast<const float4v*>(a.state_in + unit + 4 * q);
             if (r.dstate_out) grad[q] = *reinterpret_cast<const float4v*>(r.dstate_out + unit + 4 * q);
         }
-        auto pieces_around = [&](auto grows) {
-            constexpr bool kGrows = decltype(grows)::value;
 #pragma unroll 4
-            for (int s = 1; s <= seg; ++s) {
-                const float sum = a.locals[sums_at + s * seg_sums + channel];
+        for (int s = 1; s <= seg; ++s) {
+            const float sum = a.locals[sums_at + s * seg_sums + channel];
 #pragma unroll
-                for (int q = 0; q < kG; ++q) pass_on<kGrows>(h[q], sum, rate[q], *reinterpret_cast<const float4v*>(a.locals + s * seg_states + unit + 4 * q));
-            }
-            if (span.last) return;
+            for (int q = 0; q < kG; ++q) pass_on(h[q], sum, third[q], *reinterpret_cast<const float4v*>(a.locals + s * seg_states + unit + 4 * q));
+        }
+        if (!span.last) {
 #pragma unroll 4
             for (int s = (tokens_of(a, b) - 1) / a.seg_len; s > seg; --s) {
                 const float sum = r.behind[sums_at + s * seg_sums + channel];
 #pragma unroll
-                for (int q = 0; q < kG; ++q) pass_on<kGrows>(grad[q], sum, rate[q], *reinterpret_cast<const float4v*>(r.behind + s * seg_states + unit + 4 * q));
+                for (int q = 0; q < kG; ++q) pass_on(grad[q], sum, third[q], *reinterpret_cast<const float4v*>(r.behind + s * seg_states + unit + 4 * q));
             }
-        };
-        bool grows = may_grow(rate[0], a.softplus);
-        if constexpr (kG > 1) grows = grows || may_grow(rate[1], a.softplus);
-        if (grows) pieces_around(std::true_type());
-        else pieces_around(std::false_type());
+        }
     }
 
     const int token = threadIdx.x / S::kAcross, own = c0 + threadIdx.x % S::kAcross * kPer, in_block = own - c0;
