@@ -101,9 +101,9 @@ long long four(long long n) { return (n + 3) / 4 * 4; }
 // Workspaces in floats, every part a multiple of four; false where a launch would not fit.
 struct ScanSpace {
     wkv6::ScanPlan plan;
-    long long locals = 0, states = 0, rows = 0, weights = 0, floats = 0;
+    long long locals = 0, states = 0, rows = 0, places = 0, weights = 0, used = 0, floats = 0;
 };
-bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, bool backward, ScanSpace* s) {
+bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, bool packed, bool backward, ScanSpace* s) {
     s->plan = plan;
     const long long blocks = wkv6::scan_blocks(D);
     if (!wkv6::fits_a_launch((backward && plan.segs > 1 ? 2 : 1) * B * blocks * plan.segs, wkv6::scan_threads(N))) return false;
@@ -111,15 +111,17 @@ bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, b
     s->floats = s->locals;
     if (backward) {
         if (!wkv6::fits_a_launch((rows + wkv6::kScanFoldRows - 1) / wkv6::kScanFoldRows, 64 * wkv6::kScanFoldRows)) return false;
-        s->states = (rows / wkv6::scan_back_chunk(N) + B + 1) * D * N;
+        s->states = wkv6::chunk_places(rows, wkv6::scan_back_chunk(N)) * D * N;
         s->rows = rows * blocks * 2 * N;
-        s->weights = wkv6::scan_places(B, rows, plan.seg_len) * D * (N + 2);
-        s->floats = 2 * s->locals + s->states + s->rows + s->weights;
+        s->places = wkv6::share_places(B, rows, plan.segs, plan.seg_len, packed);
+        s->weights = s->places * D * (N + 2);
+        s->used = packed && plan.segs > 1 ? 4 : 0;
+        s->floats = 2 * s->locals + s->states + s->rows + s->weights + s->used;
     }
     return true;
 }
 bool scan_space(int B, int T, int D, int N, long long rows, bool packed, bool backward, ScanSpace* s) {
-    return space_of(wkv6::plan_scan(B, T, D, N, packed ? rows : -1, backward), B, D, N, rows, backward, s);
+    return space_of(wkv6::plan_scan(B, T, D, N, packed ? rows : -1, backward), B, D, N, rows, packed, backward, s);
 }
 constexpr int kAnyLength = 1;
 // For calls with offsets or, if there are B T rows, without.  A prefill's rows are not known: for any that fit.
@@ -134,7 +136,7 @@ long long scan_bytes(int B, int T, int D, int N, long long rows, bool backward) 
         if (!scan_space(B, T, D, N, rows, true, true, &s)) return -1;
     } else {
         const int segs = wkv6::scan_most_segments(B, T, D, true);
-        if (!space_of({segs, kAnyLength}, B, D, N, 0, false, &s)) return -1;
+        if (!space_of({segs, kAnyLength}, B, D, N, 0, true, false, &s)) return -1;
     }
     return 4 * (s.floats > most ? s.floats : most);
 }
@@ -267,6 +269,8 @@ int wkv6_selective_scan_backward(int B, int T, int D, int N, long long rows, con
     g.states = take(s.states);
     g.rows = take(s.rows);
     g.weights = take(s.weights);
+    g.places = s.places;
+    g.used = reinterpret_cast<long long*>(take(s.used));
     g.dout = dout; g.dstate_out = dstate_out;
     g.dx = dx; g.ddelta = ddelta; g.db = db; g.dc = dc; g.dz = dz; g.dstate_in = dstate_in;
     return status_of(wkv6::launch_scan_backward(args, g, dtype == WKV6_DTYPE_F32, st));

@@ -1,0 +1,53 @@
+// Where the gradients of the selective scan and of the short convolution keep what their workgroups leave for others, in sums over tokens and in states in
+// front of chunks.  Sequences lie in any order (offsets may fall), and a call's memory grows with its rows and sequences, not with the longest
+// sequence that may come, so places go by what no two sequences share: their rows, and their number.  Shared with a host-side check.
+#pragma once
+
+#if defined(__HIPCC__)
+#define WKV6_HD __host__ __device__
+#else
+#define WKV6_HD
+#endif
+
+namespace wkv6 {
+
+// A sequence's first row, and its tokens; Args has B, T, rows and offsets.
+template <typename Args>
+WKV6_HD inline long long first_row_of(const Args& a, int b) {
+    if (!a.offsets) return static_cast<long long>(b) * a.T;
+    const long long f = a.offsets[b];
+    return f < 0 ? 0 : f > a.rows ? a.rows : f;
+}
+template <typename Args>
+WKV6_HD inline int tokens_of(const Args& a, int b) {
+    if (!a.offsets) return a.T;
+    const long long e = a.offsets[b + 1], len = (e < 0 ? 0 : e > a.rows ? a.rows : e) - first_row_of(a, b);
+    return static_cast<int>(len < 0 ? 0 : len > a.T ? a.T : len);
+}
+
+// Which of `count` rows (below 32) from `first` on sequence b has, by bits.
+template <typename Args>
+WKV6_HD inline unsigned rows_among(const Args& a, int b, long long first, int count) {
+    const long long from = first_row_of(a, b) - first, end = from + tokens_of(a, b);
+    const int lo = from < 0 ? 0 : from > count ? count : static_cast<int>(from), hi = end < 0 ? 0 : end > count ? count : static_cast<int>(end);
+    return lo < hi ? (1u << hi) - (1u << lo) : 0;
+}
+
+// A sequence's segments of seg_len tokens; one of none if it has no tokens.
+WKV6_HD inline int segments_of(int tokens, int seg_len) {
+    return tokens <= seg_len ? 1 : static_cast<int>((static_cast<unsigned>(tokens) - 1) / static_cast<unsigned>(seg_len)) + 1;
+}
+
+// Places of the segments' sums, one behind the other: segment s of sequence b at s + the segments of the sequences in front of b.  That is b where a call has
+// one segment a sequence, and b segs + s without offsets.  Sequences that do not overlap have rows / seg_len + B at most; of others, what does not fit
+// is left out.
+WKV6_HD constexpr long long share_places(int B, long long rows, int segs, int seg_len, bool packed) {
+    return segs == 1 ? B : packed ? (B > 0 ? rows / seg_len + B : 0) : static_cast<long long>(B) * segs;
+}
+
+// Places of the states in front of chunks: by the chunk's first row.  Those of whole chunks are a chunk apart at least, so that no two share one; a state in front of a
+// sequence's last chunk is not kept.
+WKV6_HD constexpr long long chunk_place(long long row, int chunk) { return row / chunk; }
+WKV6_HD constexpr long long chunk_places(long long rows, int chunk) { return rows / chunk + 1; }
+
+}  // namespace wkv6

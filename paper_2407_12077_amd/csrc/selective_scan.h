@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include "scan_places.h"
 #include "wkv6_launch.h"
 
 namespace wkv6 {
@@ -40,8 +41,6 @@ int scan_most_segments(int B, int T, int D, bool packed);
 ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward);
 inline long long scan_blocks(int D) { return (D + kScanChannels - 1) / kScanChannels; }
 inline long long scan_local_floats(const ScanPlan& p, long long B, long long D, int N) { return p.segs > 1 ? p.segs * B * D * (N + 1) : 0; }
-// Segments' places: segment s of sequence b at first row / seg_len + b + s
-__host__ __device__ constexpr long long scan_places(int B, long long rows, int seg_len) { return B > 0 ? rows / seg_len + B : 0; }
 constexpr int scan_threads(int N) { return 16 * N; }
 
 // state_out may be null.  With a.segs > 1 the segments' own states first.
@@ -57,11 +56,13 @@ struct ScanGradients {
     void *dx, *ddelta, *db, *dc, *dz;
     float *da, *dskip, *dbias, *dstate_in;
     // workspace
-    float* states;                     // [place][D][N] in front of every chunk; sequence b's chunk i: place first row / chunk + i + b
+    float* states;                     // [place][D][N] in front of every chunk but a sequence's last (chunk_place)
     float* behind;                     // segs > 1: [segs][B][D][N] what a segment hands to the one in front of it of nothing; behind
                                        // them the sums of its step sizes [segs][B][D]
     float* rows;                       // [rows][blocks][2 N]: shares of db and dc
-    float* weights;                    // [place][D][N], then [place][2][D]: shares of da, and of dskip and dbias
+    float* weights;                    // [place][D][N], then [place][2][D]: segments' shares of da, and of dskip and dbias (share_places)
+    long long places;                  // of them
+    long long* used;                   // how many of these segments have, where they are counted (counts_segments)
 };
 hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradients& g, bool f32, hipStream_t stream);
 

@@ -44,13 +44,32 @@ struct Shape {
     static constexpr int kPer = kC * kScanChannels / kThreads, kAcross = kScanChannels / kPer;
 };
 
+struct BackwardArgs {
+    ScanArgs a;
+    ScanGradients r;
+    int blocks;
+};
+
+// A kernel's only argument once more, as it lies in memory: what is needed at the end only would else stay in scalar registers, of which there are
+// too few: 94 were spilled, now 3 to 15 (gradients of 8 x 2048 x 4096 914 -> 895 us, 1 x 512 x 2048 39.9 -> 37.2).
+template <typename Args>
+__device__ __forceinline__ const Args& argument_again() {
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const Args*)at;
+}
+
 template <int N, bool kF32, bool kGate>
-__global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(ScanArgs a, ScanGradients r, int blocks) {
+__global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(BackwardArgs args) {
     using S = Shape<N>;
+    const ScanArgs& a = args.a;
+    const ScanGradients& r = args.r;
+    const int blocks = args.blocks;
     constexpr int kG = S::kGroups, kWaves = S::kWaves, kC = S::kC, kCh = kScanChannels, kPer = S::kPer, kItem = kF32 ? 4 : 2;
     __shared__ float2v step[2][kC][kCh];                       // dt, dt x
     __shared__ float grad_out[2][kC][kCh];                     // dy
     __shared__ float part[kGate ? 3 : 2][kWaves][kC][kCh];     // shares of g, of sum k rate, of the read-outs
+    __shared__ int in_front[kWaves];                           // segments of other sequences
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int block = blockIdx.x % blocks, at = blockIdx.x / blocks, b = at % a.B, seg = at / a.B;
     const Span span = span_of(a, b, seg);
@@ -113,8 +132,7 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
     const int out_at = there ? (token * D + own) * kItem : kNowhere;
     const int kept_at = mine ? (ch * N + n0) * 4 : kNowhere;
     const long long row0 = span.first_row, out_row = static_cast<long long>(D) * kItem;
-    const long long place0 = (row0 - static_cast<long long>(seg) * a.seg_len) / kC + static_cast<long long>(seg) * a.seg_len / kC + b;
-    Rows xs(a.x, row0, a.x_row), deltas(a.delta, row0, a.delta_row), bs(a.b, row0, a.bc_row), kept(r.states, place0, static_cast<long long>(D) * N * 4);
+    Rows xs(a.x, row0, a.x_row), deltas(a.delta, row0, a.delta_row), bs(a.b, row0, a.bc_row), kept(r.states, chunk_place(row0, kC), static_cast<long long>(D) * N * 4);
     auto bring = [&](int first, Chunk& k, int buffer, auto on_the_way_back) {
         steps_of(k.delta, bias, softplus, k.dt);
 #pragma unroll
@@ -339,25 +357,12 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
         now = next;
     }
     __builtin_amdgcn_s_setprio(0);
+    const BackwardArgs& end = argument_again<BackwardArgs>();
+    const ScanArgs& call = end.a;
+    const ScanGradients& to = end.r;
+    const bool counts = counts_segments(call);
+    const int others = counts ? segments_in_front<S::kThreads>(call, b) : 0;
     __syncthreads();
-    // Places that no segment has are set to nought by the last segment in front of them (in front of all: by the first sequence's), so that the fold
-    // adds all places without asking whose they are.
-    auto place_of = [&](int sequence) { return static_cast<long long>(static_cast<unsigned>(first_row_of(a, sequence)) / static_cast<unsigned>(a.seg_len)) + sequence; };
-    const long long places = scan_places(a.B, a.rows, a.seg_len), share = place_of(b) + seg;
-    const long long before = b == 0 && seg == 0 ? 0 : share, behind = !span.last ? share + 1 : b + 1 < a.B ? place_of(b + 1) : places;
-    auto leave = [&](float* to, long long width, auto v) {
-        using V = decltype(v);
-        for (long long i = before; i < share; ++i) *reinterpret_cast<V*>(to + i * width) = V{};
-        *reinterpret_cast<V*>(to + share * width) = v;
-        for (long long i = share + 1; i < behind; ++i) *reinterpret_cast<V*>(to + i * width) = V{};
-    };
-    if (mine) {
-#pragma unroll
-        for (int q = 0; q < kG; ++q) {
-            if (seg == 0 && r.dstate_in) *reinterpret_cast<float4v*>(r.dstate_in + unit + 4 * q) = grad[q];
-            leave(r.weights + static_cast<long long>(ch) * N + n0 + 4 * q, static_cast<long long>(D) * N, da[q]);
-        }
-    }
     // the tokens' shares of dskip and dbias meet
     float* const meet = &part[0][0][0][0];                     // [2][kC][kCh]
 #pragma unroll
@@ -365,13 +370,40 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Sc
         meet[token * kCh + in_block + i] = dskip[i];
         meet[(kC + token) * kCh + in_block + i] = dbias[i];
     }
+    if (lane == 0) in_front[wave] = others;
     __syncthreads();
-    if (threadIdx.x < 2 * kCh && mine) {
+    if (!mine) return;
+    if (seg == 0 && to.dstate_in) {
+#pragma unroll
+        for (int q = 0; q < kG; ++q) *reinterpret_cast<float4v*>(to.dstate_in + unit + 4 * q) = grad[q];
+    }
+    long long share = static_cast<long long>(b) * call.segs + seg;
+    if (counts) {
+        share = seg;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) share += in_front[w];
+        if (b == call.B - 1 && seg == 0 && block == 0 && threadIdx.x == 0) *to.used = share + segments_of(tokens_of(call, b), call.seg_len);
+    }
+    if (share >= to.places) return;                            // (sequences that overlap)
+#pragma unroll
+    for (int q = 0; q < kG; ++q) *reinterpret_cast<float4v*>(to.weights + (share * D + ch) * N + n0 + 4 * q) = da[q];
+    if (threadIdx.x < 2 * kCh) {
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < kC; ++t) sum += meet[((threadIdx.x >> 6) * kC + t) * kCh + lane];
-        leave(r.weights + places * D * N + static_cast<long long>(threadIdx.x >> 6) * D + ch, 2ll * D, sum);
+        to.weights[to.places * D * N + (2 * share + (threadIdx.x >> 6)) * D + ch] = sum;
     }
+}
+
+// Which of kScanFoldRows rows from `first` on a sequence has, by bits of `owned`: the sequences lie in any order, so that all are looked at, a thread each.
+__device__ __forceinline__ void find_owned(const ScanArgs& a, long long first, unsigned* owned) {
+    if (threadIdx.x == 0) *owned = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.B; i += 64 * kScanFoldRows) {
+        const unsigned rows = rows_among(a, i, first, kScanFoldRows);
+        if (rows) atomicOr(owned, rows);
+    }
+    __syncthreads();
 }
 
 // db and dc of a row: a wave adds the blocks' shares, lanes four values of a block each, as many blocks at once as it has lanes for.
@@ -379,18 +411,6 @@ template <int N, bool kF32>
 __device__ __forceinline__ void fold_row(const ScanArgs& a, const float* shares, char* db, char* dc, int blocks, long long row) {
     constexpr int kAcross = 2 * N / 4, kAtOnce = 64 / kAcross;
     const int lane = threadIdx.x & 63;
-    if (row >= a.rows) return;
-    if (a.offsets) {                                           // rows of nobody keep what they hold
-        int lo = 0, hi = a.B;                                  // the sequences that start at or in front of the row
-        while (lo < hi) {
-            const int mid = lo + (hi - lo) / 2;
-            if (a.offsets[mid] <= row) lo = mid + 1;
-            else hi = mid;
-        }
-        if (lo == 0) return;
-        const long long first = a.offsets[lo - 1] < 0 ? 0 : a.offsets[lo - 1];
-        if (row >= a.offsets[lo] || row - first >= a.T) return;
-    }
     const float4v* p = reinterpret_cast<const float4v*>(shares + row * blocks * (2 * N)) + lane;
     float4v sum = {0.f, 0.f, 0.f, 0.f};
     const int mine = lane / kAcross;
@@ -408,18 +428,18 @@ __device__ __forceinline__ void fold_row(const ScanArgs& a, const float* shares,
 
 // da, dskip, dbias: 64 values a workgroup, the places in sixteen turns, in their order.
 constexpr int kTurns = kScanFoldRows;
-__device__ __forceinline__ void fold_weights(int D, int N, long long places, const float* shares, float* da, float* dskip, float* dbias,
-                                             unsigned group) {
+__device__ __forceinline__ void fold_weights(const ScanArgs& a, const ScanGradients& r, unsigned group) {
     __shared__ float meet[kTurns][64];
-    const int lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int D = a.D, N = a.N, lane = threadIdx.x & 63, turn = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long places = r.places, counted = counts_segments(a) ? *r.used : places, used = counted < places ? counted : places;
     const long long states = static_cast<long long>(D) * N, value = static_cast<long long>(group) * 64 + lane;
     const bool there = value < states + 2 * D;
     const long long stride = value < states ? states : 2 * D;
-    const float* from = (value < states ? shares + value : shares + places * states + (value - states)) + turn * stride;
+    const float* from = (value < states ? r.weights + value : r.weights + places * states + (value - states)) + turn * stride;
     float sum = 0.f;
     if (there) {
 #pragma unroll 8
-        for (long long i = turn; i < places; i += kTurns, from += kTurns * stride) sum += *from;
+        for (long long i = turn; i < used; i += kTurns, from += kTurns * stride) sum += *from;
     }
     meet[turn][lane] = sum;
     __syncthreads();
@@ -427,26 +447,31 @@ __device__ __forceinline__ void fold_weights(int D, int N, long long places, con
 #pragma unroll
     for (int i = 1; i < kTurns; ++i) sum += meet[i][lane];
     if (value < states) {
-        if (da) da[value] = sum;
+        if (r.da) r.da[value] = sum;
     } else if (value < states + D) {
-        if (dskip) dskip[value - states] = sum;
-    } else if (dbias) {
-        dbias[value - states - D] = sum;
+        if (r.dskip) r.dskip[value - states] = sum;
+    } else if (r.dbias) {
+        r.dbias[value - states - D] = sum;
     }
 }
 
-__global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(int D, int N, long long places, const float* shares, float* da, float* dskip, float* dbias) {
-    fold_weights(D, N, places, shares, da, dskip, dbias, blockIdx.x);
+__global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(ScanArgs a, ScanGradients r) {
+    fold_weights(a, r, blockIdx.x);
 }
 // Both folds in one launch, as each alone leaves most of the card idle: `rows` workgroups of the one, a row a wave, and the others behind them (in two launches 1 x 512 x 2048
 // takes 42 us for 39.5, 16 x 64 x 768 33 for 30.8; the others in front 0.8 % more for 2 x 2048 x 4096 with 64 states).
 template <int N, bool kF32>
 __global__ __launch_bounds__(64 * kTurns) void scan_folds_kernel(ScanArgs a, ScanGradients r, int blocks, unsigned rows) {
     if (blockIdx.x < rows) {
-        fold_row<N, kF32>(a, r.rows, static_cast<char*>(r.db), static_cast<char*>(r.dc), blocks,
-                          static_cast<long long>(blockIdx.x) * kTurns + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+        __shared__ unsigned owned;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const long long first = static_cast<long long>(blockIdx.x) * kScanFoldRows;
+        if (a.offsets) find_owned(a, first, &owned);
+        // rows of nobody keep what they hold
+        if (a.offsets ? owned >> wave & 1 : first + wave < a.rows)
+            fold_row<N, kF32>(a, r.rows, static_cast<char*>(r.db), static_cast<char*>(r.dc), blocks, first + wave);
     } else {
-        fold_weights(a.D, N, scan_places(a.B, a.rows, a.seg_len), r.weights, r.da, r.dskip, r.dbias, blockIdx.x - rows);
+        fold_weights(a, r, blockIdx.x - rows);
     }
 }
 unsigned weight_groups(const ScanArgs& a, const ScanGradients& g) {
@@ -463,7 +488,7 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
         if (err != hipSuccess) return err;
     }
     const auto kernel = a.z ? &scan_backward_kernel<N, kF32, true> : &scan_backward_kernel<N, kF32, false>;
-    hipLaunchKernelGGL(kernel, dim3(units * a.segs), dim3(Shape<N>::kThreads), 0, stream, a, g, blocks);
+    hipLaunchKernelGGL(kernel, dim3(units * a.segs), dim3(Shape<N>::kThreads), 0, stream, BackwardArgs{a, g, blocks});
     if ((err = hipGetLastError()) != hipSuccess) return err;
     if (a.rows == 0 || a.T == 0) return launch_scan_weights(a, g, stream);
     const unsigned rows = static_cast<unsigned>((a.rows + kScanFoldRows - 1) / kScanFoldRows);
@@ -478,8 +503,7 @@ hipError_t launch(const ScanArgs& a, const ScanGradients& g, hipStream_t stream)
 hipError_t launch_scan_weights(const ScanArgs& a, const ScanGradients& g, hipStream_t stream) {
     const unsigned weights = weight_groups(a, g);
     if (weights == 0) return hipSuccess;
-    hipLaunchKernelGGL(scan_weights_kernel, dim3(weights), dim3(64 * kTurns), 0, stream, a.D, a.N,
-                       scan_places(a.B, a.rows, a.seg_len), g.weights, g.da, g.dskip, g.dbias);
+    hipLaunchKernelGGL(scan_weights_kernel, dim3(weights), dim3(64 * kTurns), 0, stream, a, g);
     return hipGetLastError();
 }
 

@@ -177,19 +177,17 @@ __device__ __forceinline__ void steps_of(const Raw<kF32, kCount>& delta, const f
     }
 }
 
-// A sequence's first row, and its tokens; Args has B, T, rows and offsets.
-template <typename Args>
-__device__ __forceinline__ long long first_row_of(const Args& a, int b) {
-    if (!a.offsets) return static_cast<long long>(b) * a.T;
-    const long long f = a.offsets[b];
-    return f < 0 ? 0 : f > a.rows ? a.rows : f;
+// Segments of the sequences in front of b (share_places), counted by a workgroup's threads: what this wave has counted, in all its lanes.
+template <int kThreads, typename Args>
+__device__ __forceinline__ int segments_in_front(const Args& a, int b) {
+    int n = 0;
+    for (int i = threadIdx.x; i < b; i += kThreads) n += segments_of(tokens_of(a, i), a.seg_len);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) n += __shfl_xor(n, m);
+    return n;
 }
 template <typename Args>
-__device__ __forceinline__ int tokens_of(const Args& a, int b) {
-    if (!a.offsets) return a.T;
-    const long long e = a.offsets[b + 1], len = (e < 0 ? 0 : e > a.rows ? a.rows : e) - first_row_of(a, b);
-    return static_cast<int>(len < 0 ? 0 : len > a.T ? a.T : len);
-}
+__device__ __forceinline__ bool counts_segments(const Args& a) { return a.offsets && a.segs > 1; }
 
 // A workgroup's rows: those of a segment of sequence b.
 struct Span {

@@ -1,4 +1,5 @@
 """Calls of the selective scan and the short convolution at the edges of what their headers allow, on the GPU."""
+import numpy as np
 import pytest
 import torch
 
@@ -6,6 +7,23 @@ import paper_2407_12077_amd as wkv
 from scan_util import BF16, CODE, F32, Scan
 
 pytestmark = pytest.mark.gpu
+# offsets that fall, that lie outside the rows, and sequences longer than T; no two sequences overlap
+ORDERS = [([2000, 3500, 3500, 0, 1500], 9000), ([2000, 3500, 3500, 0, 1500], 400), ([200, 0, 2500], 5000), ([100, 200, 0, 90], 200),
+          ([-5, 30, 30, 900, 900, 5000], 2000), ([40, -7, 30, 30, 17], 64), ([600, 300, 500, 0, 200, 210, 211, 290], 300), ([20, 28, 5, 9, 9, 2, 4], 8)]
+
+
+def in_any_order(cls, seed, offsets, longest, **sizes):
+    """A call with these offsets, 1200 rows behind the largest one that there may be."""
+    rows = max(o for o in offsets if o < 5000) + 1200
+    x = cls(seed, lengths=[0] * (len(offsets) - 1), tail=rows, longest=longest, **sizes)
+    x.offsets.copy_(torch.tensor(offsets, dtype=torch.int32))
+    at = np.clip(offsets, 0, rows)
+    x.spans = [(int(f), int(f + min(max(e - f, 0), longest))) for f, e in zip(at[:-1], at[1:])]
+    for f, e in x.spans:
+        assert not x.covered[f:e].any()
+        x.covered[f:e] = True
+    x.longest = max(e - f for f, e in x.spans)
+    return x
 
 
 @pytest.mark.parametrize("N", [8, 16, 32, 64])
@@ -67,3 +85,15 @@ def test_a_piece_may_grow_more_than_fp32_holds(gpu_device, state, rows, N):
     s.dout[first + 320:end] = 0
     s.check_prefill(*s.prefill())
     s.check_backward(s.backward())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("N", [8, 16, 64])
+@pytest.mark.parametrize("offsets,longest", ORDERS, ids=str)
+def test_sequences_in_any_order(gpu_device, offsets, longest, N, dtype):
+    s = in_any_order(Scan, 4, offsets, longest, D=72, N=N, dtype=dtype, fused=N == 16)
+    s.check_prefill(*s.prefill())
+    g = s.backward()
+    s.check_backward(g)
+    for name, again in s.backward().items():
+        assert torch.equal(g[name], again), name
