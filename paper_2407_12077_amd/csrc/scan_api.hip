@@ -178,9 +178,6 @@ struct ConvCall {
     }
 };
 
-// in floats
-long long conv_partials(int B, int D, int W, long long rows, const wkv6::ConvPlan& p) { return wkv6::conv_places(B, rows, p.seg_len) * (W + 1) * D; }
-
 }  // namespace
 
 extern "C" {
@@ -279,7 +276,7 @@ int wkv6_selective_scan_backward(int B, int T, int D, int N, long long rows, con
 long long wkv6_short_conv_backward_workspace_bytes(int B, int T, int D, int W, long long rows) {
     if (W < 2 || W > 4 || !channels_fit(D) || !sizes_fit(B, T, D, rows)) return -1;
     const wkv6::ConvPlan p = wkv6::plan_conv(B, T, D, rows, true);
-    return wkv6::fits_a_launch(p.workgroups, wkv6::kConvThreads) ? 4 * conv_partials(B, D, W, rows, p) : -1;
+    return wkv6::fits_a_launch(p.workgroups, wkv6::kConvThreads) ? 4 * wkv6::conv_partial_floats(B, D, W, rows, p, true) : -1;     // (without offsets fewer)
 }
 
 int wkv6_short_conv_prefill(int B, int T, int D, int W, long long rows, const void* x, long long x_stride, const float* w, const float* bias,
@@ -322,7 +319,8 @@ int wkv6_short_conv_backward(int B, int T, int D, int W, long long rows, const v
     if (call.any_rows() && any_null(dout, dx)) return WKV6_ERR_NULL;
     if (any_misaligned(dout, dstate_out) || any_misaligned(dx, dstate_in)) return WKV6_ERR_ALIGN;
     if (!wkv6::fits_a_launch(p.workgroups, wkv6::kConvThreads)) return WKV6_ERR_SHAPE;
-    if (dw && (status = check_workspace(workspace, workspace_bytes, 4 * conv_partials(B, D, W, rows, p))) != WKV6_OK) return status;
+    if (dw && (status = check_workspace(workspace, workspace_bytes, 4 * wkv6::conv_partial_floats(B, D, W, rows, p, offsets != nullptr))) != WKV6_OK)
+        return status;
     return status_of(wkv6::launch_conv_backward(call.args(p), dout, dstate_out, dx, dw, dbias, dstate_in, static_cast<float*>(workspace),
                                                 dtype == WKV6_DTYPE_F32, st));
 }

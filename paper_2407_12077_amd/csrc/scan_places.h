@@ -45,6 +45,18 @@ WKV6_HD constexpr long long share_places(int B, long long rows, int segs, int se
     return segs == 1 ? B : packed ? (B > 0 ? rows / seg_len + B : 0) : static_cast<long long>(B) * segs;
 }
 
+// The same without counting, for short workgroups: a sequence's last segment at `whole` + its number, the others, which are whole, by their first row: whole rows of
+// segments are one apart at least, so that no two share a place.  Of the places by row some are nobody's; whoever comes in front of them in the order of rows
+// sets them to nought: a sequence with rows those behind its own, up to the first of the sequence that starts next, and number 0 those in front of all.
+WKV6_HD constexpr long long whole_places(long long rows, int segs, int seg_len) { return segs == 1 ? 0 : rows / seg_len; }
+WKV6_HD inline long long place_of_row(long long row, int seg_len) { return static_cast<unsigned>(row) / static_cast<unsigned>(seg_len); }   // (fewer than 2^31 rows)
+// The first row from `row` on at which sequence b starts, if it has rows; else `rows`.
+template <typename Args>
+WKV6_HD inline long long start_behind(const Args& a, int b, long long row) {
+    const long long first = first_row_of(a, b);
+    return first >= row && tokens_of(a, b) > 0 ? first : a.rows;
+}
+
 // Places of the states in front of chunks: by the chunk's first row.  Those of whole chunks are a chunk apart at least, so that no two share one; a state in front of a
 // sequence's last chunk is not kept.
 WKV6_HD constexpr long long chunk_place(long long row, int chunk) { return row / chunk; }

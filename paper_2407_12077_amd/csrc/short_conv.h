@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include "scan_places.h"
 #include "wkv6_launch.h"
 
 namespace wkv6 {
@@ -32,8 +33,10 @@ ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward);
 hipError_t launch_conv(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream);
 hipError_t launch_conv_step(const ConvArgs& a, void* out, void* state_out, bool f32, hipStream_t stream);
 
-// dw and dbias (both or neither) through `partials`: [place][W + 1][D]
-__host__ __device__ constexpr long long conv_places(int B, long long rows, int seg_len) { return B > 0 ? rows / seg_len + B : 0; }
+// dw and dbias (both or neither) through `partials`: segments' sums [place][W + 1][D], of packed sequences by row (whole_places).
+inline long long conv_partial_floats(int B, int D, int W, long long rows, const ConvPlan& p, bool packed) {
+    return share_places(B, rows, p.segs, p.seg_len, packed) * (W + 1) * D;
+}
 hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void* dstate_out, void* dx, float* dw, float* dbias, void* dstate_in,
                                 float* partials, bool f32, hipStream_t stream);
 

@@ -12,6 +12,8 @@
 
 #include "selective_scan_tiles.h"
 
+#include <algorithm>
+
 namespace wkv6 {
 namespace {
 
@@ -161,18 +163,12 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvArgs a, cha
     for (int j = 0; j < W - 1; ++j) in[j + 1].raw.put(state_out + state_at + j * row);
 }
 
-// Where the first segment of sequence b leaves its sums, the others behind it: a segment of sequence b + 1 starts at least as many rows later as
-// b has, so no two places meet, and there are rows / seg_len + B of them.  Those that no segment has are set to nought by the last segment in front
-// of them (in front of all: by the first sequence's), so that the fold adds all places without asking whose they are.
-__device__ __forceinline__ long long first_place(const ConvArgs& a, int b) {
-    return static_cast<long long>(static_cast<unsigned>(first_row_of(a, b)) / static_cast<unsigned>(a.seg_len)) + b;     // (fewer than 2^31 rows)
-}
-
 template <int W, bool kF32, int kG>
 __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a, const char* dout, const char* dstate_out, char* dx, char* dstate_in,
-                                                                     float* partials, int across, int run) {
+                                                                     float* partials, unsigned whole, int across, int run) {
     constexpr int kItem = kF32 ? 4 : 2;
     __shared__ float meet[kConvThreads / 2][(W + 1) * kG + 1];
+    __shared__ int starts[kConvThreads / 64];
     const int column = threadIdx.x % a.lanes, slice = threadIdx.x / a.lanes;
     const int block = blockIdx.x % across, at = blockIdx.x / across, b = at % a.B, seg = at / a.B;
     const int ch = (block * a.lanes + column) * kG;
@@ -180,6 +176,8 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
     const Place p = place_of(a, b, seg, slice, run);
     const bool head = seg == 0 && slice == 0;
     if (static_cast<long long>(seg) * a.seg_len >= p.len && seg > 0) return;      // (the whole workgroup)
+    // (whether the next sequence starts where this one ends is asked here, with the other offsets, and not at the end: 2000 sequences of up to 40 x 512 66.6 -> 64.4 us)
+    const bool by_row = a.offsets && a.segs > 1, followed = by_row && b + 1 < a.B && start_behind(a, b + 1, p.row0 + p.len) == p.row0 + p.len;
     float sums[W + 1][kG];
 #pragma unroll
     for (int j = 0; j <= W; ++j)
@@ -298,23 +296,51 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
                 for (int e = 0; e < kG; ++e) sums[j][e] += meet[threadIdx.x][j * kG + e];
         __syncthreads();
     }
-    if (slice != 0 || !there) return;
-    const long long mine = first_place(a, b) + seg, values = static_cast<long long>(W + 1) * a.D;
-    float* const to = partials + ch;
+    // where the sums go, and the places that are nobody's (whole_places)
+    const bool last = static_cast<long long>(seg + 1) * a.seg_len >= p.len;
+    auto next_start = [&](long long row) {                     // of all sequences
+        long long start = a.rows;
+        for (int i = threadIdx.x; i < a.B; i += kConvThreads) start = std::min(start, start_behind(a, i, row));
+        int first = static_cast<int>(start);
 #pragma unroll
-    for (int j = 0; j <= W; ++j)
+        for (int m = 1; m < 64; m *= 2) first = std::min(first, __shfl_xor(first, m));
+        if (threadIdx.x % 64 == 0) starts[threadIdx.x / 64] = first;
+        __syncthreads();
+        first = starts[0];
 #pragma unroll
-        for (int e = 0; e < kG; e += 4)
-            *reinterpret_cast<float4v*>(to + mine * values + static_cast<long long>(j) * a.D + e) = float4v{sums[j][e], sums[j][e + 1], sums[j][e + 2], sums[j][e + 3]};
-    auto none = [&](long long from, long long end) {
-        for (; from < end; ++from)
-#pragma unroll
-            for (int j = 0; j <= W; ++j)
-#pragma unroll
-                for (int e = 0; e < kG; e += 4) *reinterpret_cast<float4v*>(to + from * values + static_cast<long long>(j) * a.D + e) = float4v{0.f, 0.f, 0.f, 0.f};
+        for (int w = 1; w < kConvThreads / 64; ++w) first = std::min(first, starts[w]);
+        __syncthreads();
+        return place_of_row(first, a.seg_len);
     };
-    if (b == 0 && seg == 0) none(0, mine);
-    if (static_cast<long long>(seg + 1) * a.seg_len >= p.len) none(mine + 1, b + 1 < a.B ? first_place(a, b + 1) : conv_places(a.B, a.rows, a.seg_len));
+    long long mine = static_cast<long long>(b) * a.segs + seg, front = 0, behind = 0, next = 0;
+    if (by_row) {
+        const long long own = place_of_row(p.row0, a.seg_len) + seg;
+        mine = last ? static_cast<long long>(whole) + b : own;
+        if (b == 0 && seg == 0 && (p.len == 0 || own > 0)) front = next_start(0);
+        if (last && p.len > 0) {
+            const long long end = p.row0 + p.len;
+            behind = own;
+            next = place_of_row(end, a.seg_len);
+            if (next < whole && !followed) {                   // most often there are some without tokens in between
+                int other = b + 2;
+                while (other < a.B && other < b + 8 && tokens_of(a, other) == 0) ++other;
+                if (other >= a.B || start_behind(a, other, end) != end) next = next_start(end);
+            }
+        }
+    }
+    if (slice != 0 || !there) return;
+    const long long values = static_cast<long long>(W + 1) * a.D;
+    auto leave = [&](long long place, auto v) {
+#pragma unroll
+        for (int j = 0; j <= W; ++j)
+#pragma unroll
+            for (int e = 0; e < kG; e += 4)
+                *reinterpret_cast<float4v*>(partials + place * values + static_cast<long long>(j) * a.D + ch + e) = float4v{v(j, e), v(j, e + 1), v(j, e + 2), v(j, e + 3)};
+    };
+    leave(mine, [&](int j, int e) { return sums[j][e]; });
+    auto none = [](int, int) { return 0.f; };
+    for (long long i = 0; i < front; ++i) leave(i, none);
+    for (long long i = behind; i < next; ++i) leave(i, none);
 }
 
 // dw [D][W] and dbias [D]: 64 values a workgroup, the places in sixteen turns, in their order.
@@ -395,7 +421,8 @@ hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void*
     const hipError_t err = by_taps(a.W, f32, [&](auto w, auto wide) {
         hipLaunchKernelGGL((conv_backward_kernel<decltype(w)::value, decltype(wide)::value, kConvGroup>), dim3(static_cast<unsigned>(a.segs) * a.B * across),
                            dim3(kConvThreads), 0, stream, a, static_cast<const char*>(dout), static_cast<const char*>(dstate_out), static_cast<char*>(dx),
-                           static_cast<char*>(dstate_in), dw ? partials : nullptr, across, a.seg_len / (kConvThreads / a.lanes));
+                           static_cast<char*>(dstate_in), dw ? partials : nullptr,
+                           static_cast<unsigned>(whole_places(a.rows, a.segs, a.seg_len)), across, a.seg_len / (kConvThreads / a.lanes));
         return hipGetLastError();
     });
     return err != hipSuccess || !dw ? err : launch_conv_fold(a, dw, dbias, partials, stream);
@@ -403,7 +430,7 @@ hipError_t launch_conv_backward(const ConvArgs& a, const void* dout, const void*
 
 hipError_t launch_conv_fold(const ConvArgs& a, float* dw, float* dbias, const float* partials, hipStream_t stream) {
     hipLaunchKernelGGL(conv_fold_kernel, dim3((static_cast<unsigned>(a.D) * (a.W + 1) + 63) / 64), dim3(64 * kFoldTurns), 0, stream, a.D, a.W,
-                       conv_places(a.B, a.rows, a.seg_len), partials, dw, dbias);
+                       share_places(a.B, a.rows, a.segs, a.seg_len, a.offsets != nullptr), partials, dw, dbias);
     return hipGetLastError();
 }
 

@@ -1,6 +1,7 @@
 // Host-side check of where the gradients of the selective scan and the short convolution keep what their workgroups leave (csrc/scan_places.h): for random
 // offsets, rising or falling, outside the rows or not, that let no two sequences overlap, no two segments' sums and no two kept states share a place, all places are inside
 // what a call asks memory for, and the rows that are found to be somebody's are those of the sequences.  Of offsets that overlap, that places stay inside.
+#include <algorithm>
 #include <cstdio>
 #include <random>
 #include <vector>
@@ -44,6 +45,31 @@ static int check(const Call& a, long long* apart) {
             used += mine;
         }
         if (!overlap && used > places) return fail("sums outside their memory", a, seg_len);
+        if (a.offsets && segs > 1) {                           // without counting
+            const long long whole = wkv6::whole_places(a.rows, segs, seg_len);
+            std::vector<int> left(static_cast<size_t>(places));
+            auto next_start = [&](long long row) {
+                long long start = a.rows;
+                for (int i = 0; i < a.B; ++i) start = std::min(start, wkv6::start_behind(a, i, row));
+                return wkv6::place_of_row(start, seg_len);
+            };
+            auto leave = [&](long long place) { return place >= 0 && place < places && ++left[static_cast<size_t>(place)] > 0; };
+            bool inside = true;
+            for (int b = 0; b < a.B; ++b) {
+                const long long first = wkv6::first_row_of(a, b);
+                const int tokens = wkv6::tokens_of(a, b), mine = wkv6::segments_of(tokens, seg_len);
+                for (int seg = 0; seg < mine; ++seg) inside &= leave(seg == mine - 1 ? whole + b : wkv6::place_of_row(first, seg_len) + seg);
+                if (b == 0)
+                    for (long long i = 0, end = next_start(0); i < end; ++i) inside &= leave(i) && i < whole;
+                if (tokens == 0) continue;
+                const long long end = first + tokens, next = next_start(end);
+                if (!overlap && b + 1 < a.B && wkv6::start_behind(a, b + 1, end) == end && next != wkv6::place_of_row(end, seg_len)) return fail("who comes next", a, seg_len);
+                for (long long i = wkv6::place_of_row(first, seg_len) + mine - 1; i < next; ++i) inside &= leave(i) && i < whole;
+            }
+            if (!inside) return fail("a segment outside its memory", a, seg_len);
+            for (const int n : left)
+                if (n != 1 && !overlap) return fail("a place left by none or by two", a, seg_len);
+        }
         for (const int chunk : {8, 16}) {
             if (segs > 1 && seg_len % chunk != 0) continue;
             const long long kept = wkv6::chunk_places(a.rows, chunk);

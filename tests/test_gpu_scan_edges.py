@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2407_12077_amd as wkv
-from scan_util import BF16, CODE, F32, Scan
+from scan_util import BF16, CODE, F32, Conv, Scan
 
 pytestmark = pytest.mark.gpu
 # offsets that fall, that lie outside the rows, and sequences longer than T; no two sequences overlap
@@ -97,3 +97,32 @@ def test_sequences_in_any_order(gpu_device, offsets, longest, N, dtype):
     s.check_backward(g)
     for name, again in s.backward().items():
         assert torch.equal(g[name], again), name
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D,W", [(72, 4), (520, 2)])
+@pytest.mark.parametrize("offsets,longest", ORDERS, ids=str)
+def test_convolutions_in_any_order(gpu_device, offsets, longest, D, W, dtype):
+    c = in_any_order(Conv, 5, offsets, longest, D=D, W=W, dtype=dtype, fused=D == 72)
+    c.check_prefill(*c.prefill())
+    g = c.backward()
+    c.check_backward(g)
+    for a, b in zip(g, c.backward()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [0, 9, 70000])
+def test_weights_of_no_sequence(gpu_device, T):
+    """No sequence, however long one may be: sums over nothing are nought, without a workspace."""
+    D, rows, offsets = 72, 5, torch.zeros(1, dtype=torch.int32, device="cuda")
+    t, dx = torch.full((rows, D), 7.0, dtype=BF16, device="cuda"), torch.full((rows, D), 7.0, dtype=BF16, device="cuda")
+    w, dw, db = torch.ones(D, 4, device="cuda"), torch.full((D, 4), 7.0, device="cuda"), torch.full((D,), 7.0, device="cuda")
+    assert wkv.wkv6_short_conv_backward_workspace_bytes(0, T, D, 4, rows) == 0 == wkv.wkv6_selective_scan_backward_workspace_bytes(0, T, D, 16, rows)
+    wkv.wkv6_short_conv_backward(0, T, D, 4, rows, t, D, w, None, 1, offsets, None, t, None, dx, dw, db, None, CODE[BF16], None, 0)
+    assert not dw.any() and not db.any() and bool((dx == 7).all())
+    a, bc = -torch.ones(D, 16, device="cuda"), torch.ones(rows, 16, dtype=BF16, device="cuda")
+    da, dskip, dbias = torch.full((D, 16), 7.0, device="cuda"), torch.full((D,), 7.0, device="cuda"), torch.full((D,), 7.0, device="cuda")
+    dbc = bc.clone()
+    wkv.wkv6_selective_scan_backward(0, T, D, 16, rows, t, D, t, D, None, 1, a, bc, bc, 16, None, None, 0, offsets, None, t, None, dx, dx, dbc, dbc, None, da, dskip, dbias, None,
+                                     CODE[BF16], None, 0)
+    assert not da.any() and not dskip.any() and not dbias.any() and bool((dx == 7).all()) and torch.equal(dbc, bc)
