@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvArgs a,
             const bool own = t < p.end;
 #pragma unroll
             for (int e = 0; e < kG; ++e) {
-                if (a.silu) {
+                if (a.silu && t < p.len) {           // (behind the end dp is nought, whatever is under the taps)
                     float v = taps.bias[e];
 #pragma unroll
                     for (int j = 0; j < W; ++j) v = __builtin_fmaf(taps.w[j][e], win[j][e], v);

@@ -126,3 +126,17 @@ def test_weights_of_no_sequence(gpu_device, T):
     wkv.wkv6_selective_scan_backward(0, T, D, 16, rows, t, D, t, D, None, 1, a, bc, bc, 16, None, None, 0, offsets, None, t, None, dx, dx, dbc, dbc, None, da, dskip, dbias, None,
                                      CODE[BF16], None, 0)
     assert not da.any() and not dskip.any() and not dbias.any() and bool((dx == 7).all()) and torch.equal(dbc, bc)
+
+
+def test_a_state_that_is_no_number_passes_a_sequence_of_no_tokens(gpu_device):
+    """It comes out as it is, its gradient is that of the state behind, and nothing else changes."""
+    c = Conv(6, D=72, W=4, lengths=[3, 0, 40, 1], front=2)
+    clean_out, clean_state = c.prefill()
+    clean = c.backward()
+    c.state_in[1, 1, 3], c.state_in[1, 2, 9] = float("nan"), float("inf")
+    out, state = c.prefill()
+    assert torch.equal(out, clean_out) and bool(state[1, 1, 3].isnan()) and bool(state[1, 2, 9].isinf())
+    state[1, 1, 3], state[1, 2, 9] = clean_state[1, 1, 3], clean_state[1, 2, 9]
+    assert torch.equal(state, clean_state)
+    for got, want in zip(c.backward(), clean):
+        assert torch.equal(got, want)
