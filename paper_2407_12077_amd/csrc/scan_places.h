@@ -49,7 +49,7 @@ WKV6_HD constexpr long long share_places(int B, long long rows, int segs, int se
 // segments are one apart at least, so that no two share a place.  Of the places by row some are nobody's; whoever comes in front of them in the order of rows
 // sets them to nought: a sequence with rows those behind its own, up to the first of the sequence that starts next, and number 0 those in front of all.
 WKV6_HD constexpr long long whole_places(long long rows, int segs, int seg_len) { return segs == 1 ? 0 : rows / seg_len; }
-WKV6_HD inline long long place_of_row(long long row, int seg_len) { return static_cast<unsigned>(row) / static_cast<unsigned>(seg_len); }   // (fewer than 2^31 rows)
+WKV6_HD inline long long place_of_row(long long row, int seg_len) { return row >> __builtin_ctz(static_cast<unsigned>(seg_len)); }   // (the convolution's are powers of two)
 // The first row from `row` on at which sequence b starts, if it has rows; else `rows`.
 template <typename Args>
 WKV6_HD inline long long start_behind(const Args& a, int b, long long row) {
