@@ -101,7 +101,7 @@ long long four(long long n) { return (n + 3) / 4 * 4; }
 // Workspaces in floats, every part a multiple of four; false where a launch would not fit.
 struct ScanSpace {
     wkv6::ScanPlan plan;
-    long long locals = 0, states = 0, rows = 0, places = 0, weights = 0, used = 0, floats = 0;
+    long long locals = 0, states = 0, rows = 0, owners = 0, places = 0, weights = 0, used = 0, floats = 0;
 };
 bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, bool packed, bool backward, ScanSpace* s) {
     s->plan = plan;
@@ -113,10 +113,11 @@ bool space_of(const wkv6::ScanPlan& plan, int B, int D, int N, long long rows, b
         if (!wkv6::fits_a_launch((rows + wkv6::kScanFoldRows - 1) / wkv6::kScanFoldRows, 64 * wkv6::kScanFoldRows)) return false;
         s->states = wkv6::chunk_places(rows, wkv6::scan_back_chunk(N)) * D * N;
         s->rows = rows * blocks * 2 * N;
+        s->owners = packed ? four(rows) : 0;
         s->places = wkv6::share_places(B, rows, plan.segs, plan.seg_len, packed);
         s->weights = s->places * D * (N + 2);
         s->used = packed && plan.segs > 1 ? 4 : 0;
-        s->floats = 2 * s->locals + s->states + s->rows + s->weights + s->used;
+        s->floats = 2 * s->locals + s->states + s->rows + s->owners + s->weights + s->used;
     }
     return true;
 }
@@ -265,6 +266,7 @@ int wkv6_selective_scan_backward(int B, int T, int D, int N, long long rows, con
     g.behind = take(s.locals);
     g.states = take(s.states);
     g.rows = take(s.rows);
+    g.owners = reinterpret_cast<int*>(take(s.owners));
     g.weights = take(s.weights);
     g.places = s.places;
     g.used = reinterpret_cast<long long*>(take(s.used));

@@ -25,12 +25,13 @@ WKV6_HD inline int tokens_of(const Args& a, int b) {
     return static_cast<int>(len < 0 ? 0 : len > a.T ? a.T : len);
 }
 
-// Which of `count` rows (below 32) from `first` on sequence b has, by bits.
+// Whether b is a sequence, and a row its own.  Whoever walks a sequence leaves its number beside its rows; what stands there of rows of nobody, whatever
+// it is, is not the number of a sequence that has them.
 template <typename Args>
-WKV6_HD inline unsigned rows_among(const Args& a, int b, long long first, int count) {
-    const long long from = first_row_of(a, b) - first, end = from + tokens_of(a, b);
-    const int lo = from < 0 ? 0 : from > count ? count : static_cast<int>(from), hi = end < 0 ? 0 : end > count ? count : static_cast<int>(end);
-    return lo < hi ? (1u << hi) - (1u << lo) : 0;
+WKV6_HD inline bool owns(const Args& a, int b, long long row) {
+    if (b < 0 || b >= a.B) return false;
+    const long long at = row - first_row_of(a, b);
+    return at >= 0 && at < tokens_of(a, b);
 }
 
 // A sequence's segments of seg_len tokens; one of none if it has no tokens.

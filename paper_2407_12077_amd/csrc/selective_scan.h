@@ -60,6 +60,7 @@ struct ScanGradients {
     float* behind;                     // segs > 1: [segs][B][D][N] what a segment hands to the one in front of it of nothing; behind
                                        // them the sums of its step sizes [segs][B][D]
     float* rows;                       // [rows][blocks][2 N]: shares of db and dc
+    int* owners;                       // with offsets [rows]: the number of the sequence that has the row (owns)
     float* weights;                    // [place][D][N], then [place][2][D]: segments' shares of da, and of dskip and dbias (share_places)
     long long places;                  // of them
     long long* used;                   // how many of these segments have, where they are counted (counts_segments)

@@ -372,6 +372,10 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Ba
     }
     if (lane == 0) in_front[wave] = others;
     __syncthreads();
+    if (call.offsets && block == 0) {
+        const Span rows = span_of(call, b, seg);
+        for (int t = threadIdx.x; t < rows.tokens; t += S::kThreads) to.owners[rows.first_row + t] = b;
+    }
     if (!mine) return;
     if (seg == 0 && to.dstate_in) {
 #pragma unroll
@@ -395,22 +399,14 @@ __global__ __launch_bounds__(Shape<N>::kThreads, 2) void scan_backward_kernel(Ba
     }
 }
 
-// Which of kScanFoldRows rows from `first` on a sequence has, by bits of `owned`: the sequences lie in any order, so that all are looked at, a thread each.
-__device__ __forceinline__ void find_owned(const ScanArgs& a, long long first, unsigned* owned) {
-    if (threadIdx.x == 0) *owned = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.B; i += 64 * kScanFoldRows) {
-        const unsigned rows = rows_among(a, i, first, kScanFoldRows);
-        if (rows) atomicOr(owned, rows);
-    }
-    __syncthreads();
-}
-
 // db and dc of a row: a wave adds the blocks' shares, lanes four values of a block each, as many blocks at once as it has lanes for.
 template <int N, bool kF32>
-__device__ __forceinline__ void fold_row(const ScanArgs& a, const float* shares, char* db, char* dc, int blocks, long long row) {
+__device__ __forceinline__ void fold_row(const ScanArgs& a, const ScanGradients& r, int blocks, long long row) {
     constexpr int kAcross = 2 * N / 4, kAtOnce = 64 / kAcross;
     const int lane = threadIdx.x & 63;
+    if (row >= a.rows) return;
+    const int owner = a.offsets ? r.owners[row] : 0;
+    const float* const shares = r.rows;
     const float4v* p = reinterpret_cast<const float4v*>(shares + row * blocks * (2 * N)) + lane;
     float4v sum = {0.f, 0.f, 0.f, 0.f};
     const int mine = lane / kAcross;
@@ -420,10 +416,10 @@ __device__ __forceinline__ void fold_row(const ScanArgs& a, const float* shares,
     for (int m = kAcross; m < 64; m *= 2)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], m);
-    if (mine != 0) return;
+    if (mine != 0 || (a.offsets && !owns(a, owner, row))) return;      // (rows of nobody keep what they hold)
     const int value = 4 * (lane % kAcross);
     const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    store<kF32>((value < N ? db : dc) + row * a.bc_row + value % N * (kF32 ? 4 : 2), v);
+    store<kF32>(static_cast<char*>(value < N ? r.db : r.dc) + row * a.bc_row + value % N * (kF32 ? 4 : 2), v);
 }
 
 // da, dskip, dbias: 64 values a workgroup, the places in sixteen turns, in their order.
@@ -463,13 +459,7 @@ __global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(ScanArgs a, S
 template <int N, bool kF32>
 __global__ __launch_bounds__(64 * kTurns) void scan_folds_kernel(ScanArgs a, ScanGradients r, int blocks, unsigned rows) {
     if (blockIdx.x < rows) {
-        __shared__ unsigned owned;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const long long first = static_cast<long long>(blockIdx.x) * kScanFoldRows;
-        if (a.offsets) find_owned(a, first, &owned);
-        // rows of nobody keep what they hold
-        if (a.offsets ? owned >> wave & 1 : first + wave < a.rows)
-            fold_row<N, kF32>(a, r.rows, static_cast<char*>(r.db), static_cast<char*>(r.dc), blocks, first + wave);
+        fold_row<N, kF32>(a, r, blocks, static_cast<long long>(blockIdx.x) * kTurns + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
     } else {
         fold_weights(a, r, blockIdx.x - rows);
     }

@@ -27,11 +27,13 @@ static int check(const Call& a, long long* apart) {
     for (int b = 0; b < a.B; ++b)
         for (int t = 0; t < wkv6::tokens_of(a, b); ++t) overlap |= owners[static_cast<size_t>(wkv6::first_row_of(a, b) + t)]++ > 0;
     *apart += !overlap;
-    for (long long first = 0; first < a.rows; first += 16) {
-        unsigned got = 0, want = 0;
-        for (int b = 0; b < a.B; ++b) got |= wkv6::rows_among(a, b, first, 16);
-        for (int i = 0; i < 16 && first + i < a.rows; ++i) want |= (owners[static_cast<size_t>(first + i)] ? 1u : 0u) << i;
-        if (got != want) return fail("rows of somebody", a, 0);
+    for (long long row = 0; row < a.rows && !overlap; ++row) {
+        int owner = -1;                                        // as the walks leave it
+        for (int b = 0; b < a.B; ++b)
+            if (row >= wkv6::first_row_of(a, b) && row < wkv6::first_row_of(a, b) + wkv6::tokens_of(a, b)) owner = b;
+        if ((owner >= 0) != (owners[static_cast<size_t>(row)] > 0)) return fail("rows", a, 0);
+        for (int b = -1; b <= a.B; ++b)                        // whatever an earlier call has left
+            if (wkv6::owns(a, b, row) != (b >= 0 && b == owner)) return fail("rows of somebody", a, 0);
     }
     for (const int seg_len : {16, 32, 128, a.T > 0 ? a.T : 1}) {
         const int segs = a.T > 0 ? (a.T - 1) / seg_len + 1 : 1;
