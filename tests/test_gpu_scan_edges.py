@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2407_12077_amd as wkv
-from scan_util import BF16, CODE, F32, Conv, Scan
+from scan_util import BF16, CODE, F32, Conv, Scan, Workspace
 
 pytestmark = pytest.mark.gpu
 # offsets that fall, that lie outside the rows, and sequences longer than T; no two sequences overlap
@@ -140,3 +140,35 @@ def test_a_state_that_is_no_number_passes_a_sequence_of_no_tokens(gpu_device):
     assert torch.equal(state, clean_state)
     for got, want in zip(c.backward(), clean):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("longest", [60, 2000])
+def test_a_captured_call_follows_its_offsets(gpu_device, longest):
+    """One graph and one workspace, replayed with other offsets each time: every replay as a call of its own, whatever the one before has left in the workspace."""
+    orders = [[0, 300, 620, 900, 901], [901, 40, 100, 0, 33], [100, 200, 200, 260, 700], [1500, -3, 5, 70, 2000], [0, 0, 0, 0, 0], [0, 300, 620, 900, 901]]
+    s = in_any_order(Scan, 7, orders[0], longest, D=72, N=16)
+    c = in_any_order(Conv, 8, orders[0], longest, D=72, W=4)
+    s.offsets = c.offsets
+    own = Workspace(wkv.wkv6_selective_scan_backward_workspace_bytes(s.B, s.T, s.D, s.N, s.rows))
+    conv_own = Workspace(wkv.wkv6_short_conv_backward_workspace_bytes(c.B, c.T, c.D, c.W, c.rows))
+
+    def calls(space, conv_space):
+        dx = torch.full((c.rows, c.stride), 77.0, dtype=c.dtype, device="cuda")
+        dw, db, ds = torch.zeros_like(c.w), torch.zeros_like(c.bias), torch.zeros_like(c.state_in)
+        wkv.wkv6_short_conv_backward(c.B, c.T, c.D, c.W, c.rows, c.x, c.stride, c.w, c.bias, 1, c.offsets, c.state_in, c.dout, c.dstate_out, dx, dw, db, ds, CODE[c.dtype],
+                                     conv_space, conv_own.n)
+        return [*s.backward(workspace=space).values(), dx, dw, db, ds]
+    calls(own, conv_own)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        kept = calls(own, conv_own)
+    for offsets in orders:
+        c.offsets.copy_(torch.tensor(offsets, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = calls(Workspace(own.n), Workspace(conv_own.n))
+        for a, b in zip(kept, want):
+            assert torch.equal(a, b), offsets
+    own.check()
+    conv_own.check()
