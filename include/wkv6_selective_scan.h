@@ -16,8 +16,8 @@
  *   rows          rows of the tensors below
  *   offsets       [B + 1] int32, device: sequence b has the rows offsets[b] .. offsets[b+1] - 1, as in wkv6_head_decay.h: rows that belong to
  *                 nobody are not read and keep what they hold; an offset outside 0 .. rows is taken as the nearer of the
- *                 two, a longer sequence ends after T tokens, one that ends in front of its start has none; where sequences overlap, what their
- *                 rows get is not defined.  NULL: B sequences of T rows each, and rows must be B T.  A sequence of no tokens has
+ *                 two, a longer sequence ends after T tokens, one that ends in front of its start has none, and sequences may lie in any order;
+ *                 where they overlap, what their rows and the sums over tokens get is not defined.  NULL: B sequences of T rows each, and rows must be B T.  A sequence of no tokens has
  *                 state_out = state_in.
  *   x, delta, z   [rows][D], rows x_stride, delta_stride, z_stride ELEMENTS apart (at least D, at most 2^22, a multiple of 16 bytes), so that they may be
  *                 parts of a projection's rows.  z may be NULL: no gate.  dx, ddelta, dz likewise, with the same strides
@@ -32,8 +32,9 @@
  * dtype is the wkv6_dtype of x, delta, z, b, c (and, of the backward call, dout, dx, ddelta, dz, db, dc), out_dtype that of out: bf16 rows with
  * either, fp32 rows with fp32.
  *
- * Arithmetic: fp32 throughout, one rounding of the results.  A decay is rounded to fp32 token by token, as the recurrence is written: a state that
- * remembers M tokens is off by up to M times 2^-24 of itself (where all its tokens have the same step size; by the root of M where they differ).  Values have to be finite: a NaN or infinity in a row reaches other tokens of its
+ * Arithmetic: fp32 throughout, one rounding of the results.  A decay is rounded to fp32 token by token, as the recurrence is written, and its exponent, its product
+ * and the sum with it: a state that remembers M tokens is off by (250 + 8 M) 2^-24 of its terms' magnitudes at most (one that grows by four times that), and by M 2^-24 or so where all its tokens have
+ * the same step size, by the root of M where they differ.  Values have to be finite: a NaN or infinity in a row reaches other tokens of its
  * sequence, also earlier ones, not other sequences.
  *
  * Workspace: device memory of the caller, 16-byte aligned, as many bytes as the function beside the call says (none where that is 0),

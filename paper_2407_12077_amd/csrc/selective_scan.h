@@ -29,13 +29,17 @@ struct ScanArgs {
 //
 // By what a call is modelled to take, in microseconds: a chunk takes a workgroup `alone` if it has a compute unit to itself, and `share` of
 // a unit that is full; the pieces' own states cost three quarters of the walk itself (of gradients, both ways, two fifths), and every piece adds
-// up what the pieces in front of it leave.  Measured, whole and cut: 4 x 4096 x 4096 361 and 394 us, 5 x 4096 x 4096 454 and 498, 8 x 4096 x 4096 459 and 776,
-// 1 x 300 x 4096 33 and 19; gradients of 4 x 2048 x 4096 757 and 607, 8 x 2048 x 4096 937 and 1350; 37 packed requests of up to 2011 x 1536 208 and 171.
+// up what the pieces in front of it leave.  Measured, whole and cut: 4 x 4096 x 4096 359 and 335 us (the model takes it whole), 5 x 4096 x 4096 450 and 497, 8 x 4096 x 4096 452 and 659,
+// 1 x 300 x 4096 30 and 19; gradients of 4 x 2048 x 4096 672 and 588, 8 x 2048 x 4096 893 and 1120; 37 packed requests of up to 2011 x 1536 206 and 171, gradients of
+// nine of up to 1531 x 768 465 and 90.
 struct ScanPlan {
     int segs, seg_len;
 };
 constexpr int kScanMostSegments = 64;
-// of a packed call with a workgroup for every compute unit, whose pieces' states would be as many times the states: 16, and no more workgroups than these
+// Of a packed call with a workgroup for every compute unit, whose pieces' states take as many times the states' memory: 16, and no more workgroups than these, empty ones
+// among them.  Microseconds with at most 1, 8, 16 and 32 pieces: 37 of up to 2011 x 1536 210, 189, 175, 200 (64 states 356, 356, 494, 710: there the model cuts too
+// much), 100 of up to 4096 x 1024 427, 369, 349, 354, 20 of up to 8192 x 2048 713, 474, 420, 372; gradients of 37 of up to 2011 x 1536 815, 506, 525, 524.  With twice and four times the
+// workgroups 63 of 200 and one of 20000 x 2048 take 560 and 511 instead of 803, for 143 and 285 MB of workspace instead of 71; 255 of one and one of 8192 x 4096 stay at 955.
 constexpr int kScanPackedSegments = 16, kScanPackedWorkgroups = 16384;
 int scan_most_segments(int B, int T, int D, bool packed);
 ScanPlan plan_scan(int B, int T, int D, int N, long long packed_rows, bool backward);

@@ -4,9 +4,9 @@
 //
 // Bound by instruction slots: every token, channel and state has an exponential of its own (two slots), a product for its argument, a multiply-add
 // into the state and one into the read-out, twenty cycles of a SIMD for a wave; nothing of it is a matrix product, as each decay belongs to one
-// (channel, state).  What a token and channel have in common (softplus, gate, types) takes a third more.  8 x 4096 x 4096, N = 16, bf16 with a gate: 454 us; the
-// slots of its instructions (a chunk and wave: 388 vector ones, 76 of them double, and 16 matrix instructions of two) are 460 at 2.19 GHz, and its bytes would
-// take 207 at a copy's rate.
+// (channel, state).  What a token and channel have in common (softplus, gate, types) takes a third more.  8 x 4096 x 4096, N = 16, bf16 with a gate: 453 us, of
+// which a vector instruction issues in 90 % (0.994 M of 1.103 M cycles of a SIMD, at 2.43 GHz 409 us; a chunk and wave: some 388 vector instructions, 76 of them double, and 16 matrix ones of
+// two slots); its bytes would take 207 at a copy's rate.
 //
 // A workgroup has 64 channels, a lane each, and a wave four states, so that states stay in registers and neither dt x b nor c h crosses lanes.  Tokens come in
 // chunks of 16: their dt and dt x are formed once, by all waves, and lie in LDS as fp32 (two chunks of them); the waves' shares of the read-outs
@@ -16,7 +16,7 @@
 //
 // Where there are fewer workgroups than the compute units hold, or one sequence is much longer than the others, the token axis is cut (plan_scan): the
 // pieces' states from nothing are formed first (scan_pieces_kernel, three quarters of the walk's time), and a piece adds up those in front of it.
-// 1 x 131072 x 2048: 1516 us, of which the pieces' states 675; whole it took 15 ms.
+// 1 x 131072 x 2048: 1499 us, of which the pieces' states 674; whole it took 15 ms.
 #include "selective_scan_tiles.h"
 
 #include <algorithm>

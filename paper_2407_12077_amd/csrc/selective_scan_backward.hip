@@ -3,14 +3,14 @@
 //     G_t[n] = c_t[n] dy_t + exp(dt_{t+1} a[n]) G_{t+1}[n]        k_t[n] = G_t[n] exp(dt_t a[n]) h_{t-1}[n]        g_t = sum_n G_t[n] b_t[n]
 //     dx = g dt + skip dy    ddelta = (g x + sum_n k[n] a[n]) dt'    db[n] = sum_d G[n] dt x    dc[n] = sum_d dy h[n]    da[n] = sum_t k[n] dt
 //
-// Divided as the forward walk (selective_scan.hip) and bound by instruction slots like it: 8 x 2048 x 4096, N = 16, bf16 with a gate: 905 us, of which 790 are the slots
-// that its instructions take, and 22 and 5 for the two folds; its bytes would take 180.  A workgroup walks its segment forwards once, leaving the
+// Divided as the forward walk (selective_scan.hip) and bound by instruction slots like it: 8 x 2048 x 4096, N = 16, bf16 with a gate: 893 us, of which the folds are 23;
+// a vector instruction issues in 93 % of the walk's cycles (1.952 M of 2.090 M of a SIMD, at 2.40 GHz 813 us); its bytes would take 180.  A workgroup walks its segment forwards once, leaving the
 // state in front of every chunk in the workspace (a quarter of the work), and back: a chunk's decays and states are formed again and stay in
 // registers, 16 tokens of both (8 of many states), for the way from its last token to its first.  k needs no product of its own, as G exp(dt a) is what
 // the token in front takes over.  db and dc are sums over channels, that is over lanes: products are added in pairs, each pair in one register with half
 // of the lanes' sums, so that eight tokens' sixty-four values end as one register, after 141 instructions (a quarter of the way back).  Letting
-// lanes exchange factors in front of the products saved instructions on paper and cost copies: 976 us.  Sums over tokens are formed by chunks, the workgroups' are folded
-// in a fixed order.
+// lanes exchange factors in front of the products saved instructions on paper and cost copies: 976 us.  da is summed by chunks,
+// dskip and dbias by every sixteenth (or eighth) token of a segment, and the workgroups' sums are folded in a fixed order.
 #include "selective_scan_tiles.h"
 
 namespace wkv6 {
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(64 * kTurns) void scan_weights_kernel(ScanArgs a, S
     fold_weights(a, r, blockIdx.x);
 }
 // Both folds in one launch, as each alone leaves most of the card idle: `rows` workgroups of the one, a row a wave, and the others behind them (in two launches 1 x 512 x 2048
-// takes 42 us for 39.5, 16 x 64 x 768 33 for 30.8; the others in front 0.8 % more for 2 x 2048 x 4096 with 64 states).
+// took 42 us for 39.5, 16 x 64 x 768 33 for 30.8; the others in front 0.8 % more for 2 x 2048 x 4096 with 64 states).
 template <int N, bool kF32>
 __global__ __launch_bounds__(64 * kTurns) void scan_folds_kernel(ScanArgs a, ScanGradients r, int blocks, unsigned rows) {
     if (blockIdx.x < rows) {

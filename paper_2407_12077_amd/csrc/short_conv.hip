@@ -5,8 +5,8 @@
 //
 // Bound by memory.  A thread has four channels (eight of a single token) of a run of 16 tokens (32 of the gradients) and keeps the inputs under its
 // taps in registers, so a row is read once, but for the W - 1 rows in front of a run (and behind it, of the gradients), which a neighbour in the same
-// workgroup reads too.  8 x 4096 x 4096 bf16, W = 4: 114 us, 4.7 TB/s (a large copy: 5.2); eight channels a thread 118, runs of 8 or 32 tokens 128 and
-// 120, addresses by multiplication 118.  Gradients of 8 x 2048 x 4096 102 us, 4.0 TB/s, of which the fold is 5: eight channels a thread 117 (240
+// workgroup reads too.  8 x 4096 x 4096 bf16, W = 4: 113 us, 4.75 TB/s (a large copy: 5.2); eight channels a thread 118, runs of 8 or 32 tokens 128 and
+// 120, addresses by multiplication 118.  Gradients of 8 x 2048 x 4096 101 us, 4.0 TB/s, of which the fold is 5: eight channels a thread 117 (240
 // registers), runs of 16 or 64 tokens 127 and 115.  24 x 4096 single tokens 3.7 us: one launch.
 #include "short_conv.h"
 
@@ -381,6 +381,9 @@ ConvPlan plan_conv(int B, int T, int D, long long rows, bool backward) {
     const int groups = D / kConvGroup;
     p.lanes = 64;
     while (p.lanes > 1 && p.lanes / 2 >= groups) p.lanes /= 2;
+    // Half as many where that leaves fewer without a group; of 256 groups and more few are without one anyway.  With 64 and with 32, microseconds of prompts of 16384 rows x 264, 384, 640,
+    // 896: 8.9, 8.8, 10.9, 13.2 and 7.6, 8.2, 10.2, 12.6; x 1056, 2056: 15.3, 39.2 and 16.2, 41.9.  Gradients of 4000 rows 13.4, 13.1, 14.6, 16.6 and 11.3, 11.4, 13.0, 14.7; of
+    // 65536 45.0, 45.1, 72.9, 91.1 and 45.0, 47.0, 72.8, 87.2; of 16384, where the runs are short, 19.6, 19.0, 25.4, 27.5 and 20.2, 20.3, 24.4, 30.6.
     if (groups > 32 && groups < 256 && groups % 64 != 0 && groups % 64 <= 32) p.lanes = 32;
     const int slices = kConvThreads / p.lanes, across = (groups + p.lanes - 1) / p.lanes;
     int run = backward ? 32 : 16;
