@@ -172,3 +172,11 @@ def test_a_captured_call_follows_its_offsets(gpu_device, longest):
             assert torch.equal(a, b), offsets
     own.check()
     conv_own.check()
+
+
+@pytest.mark.parametrize("D", [136, 264, 384, 896, 1056, 2056])
+def test_convolutions_of_widths_that_leave_lanes_idle(gpu_device, D):
+    """As many threads side by side as there are groups of four channels, or half or a quarter as many, and some without one."""
+    c = Conv(9, D=D, W=4, lengths=[70, 3, 0, 130], front=1, tail=2)
+    c.check_prefill(*c.prefill())
+    c.check_backward(c.backward())
