@@ -46,8 +46,8 @@ WKV6_HD constexpr long long share_places(int B, long long rows, int segs, int se
     return segs == 1 ? B : packed ? (B > 0 ? rows / seg_len + B : 0) : static_cast<long long>(B) * segs;
 }
 
-// The same without counting, for short workgroups: a sequence's last segment at `whole` + its number, the others, which are whole, by their first row: whole rows of
-// segments are one apart at least, so that no two share a place.  Of the places by row some are nobody's; whoever comes in front of them in the order of rows
+// The same without counting, for short workgroups: a sequence's last segment at `whole` + its number, the others, which are whole, by their first row: whole
+// segments start a segment apart at least, so that no two share a place.  Of the places by row some are nobody's; whoever comes in front of them in the order of rows
 // sets them to nought: a sequence with rows those behind its own, up to the first of the sequence that starts next, and number 0 those in front of all.
 WKV6_HD constexpr long long whole_places(long long rows, int segs, int seg_len) { return segs == 1 ? 0 : rows / seg_len; }
 WKV6_HD inline long long place_of_row(long long row, int seg_len) { return row >> __builtin_ctz(static_cast<unsigned>(seg_len)); }   // (the convolution's are powers of two)
